@@ -1,0 +1,417 @@
+"""The operators of a model behind walks and joined sets, as measurable cases.
+
+A case is a dict of plain values; its ``op`` says which operator one pass runs:
+
+  attend        attention of packed query rows to packed keys (offsets as ``join_queries`` lays
+                them out), grouped heads, with or without a learned bias by distance buckets
+  attend_train  the same, and the gradients of queries, keys, values and bias
+  loss          softmax cross entropy of rows against the table of all nodes
+  loss_train    the same, and the gradients of rows and table
+
+``run`` computes them either in their plain form (elementary torch operations in 32 bits, packed
+sequences padded to the longest) or by the calls of this package.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+import torch.nn.functional as F
+
+own = False
+
+_context = None
+_TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def _ctx():
+    """The one context that a program keeps."""
+    global _context
+    if _context is None:
+        from paper_2202_13538_amd import binding
+        _context = binding.Context()
+    return _context
+
+
+# --------------------------------------------------------------------------- #
+# cases
+# --------------------------------------------------------------------------- #
+def _attend(name, op, dtype, seqs, q_len, k_len, heads, kv_heads, dim, causal, reach, buckets):
+    """q_len / k_len: (shortest, longest) of the packed sequences; equal shortest and longest are
+    the length of all.  k_len None: the sequences attend to themselves.  reach 0: no bias."""
+    return dict(name=name, op=op, dtype=dtype, seqs=seqs, q_lo=q_len[0], q_hi=q_len[1],
+                k_lo=k_len[0] if k_len else 0, k_hi=k_len[1] if k_len else 0, heads=heads,
+                kv_heads=kv_heads, dim=dim, causal=causal, reach=reach, buckets=buckets)
+
+
+def _loss(name, op, dtype, rows, nodes, dim):
+    return dict(name=name, op=op, dtype=dtype, rows=rows, nodes=nodes, dim=dim)
+
+
+def listed() -> list[dict]:
+    return [
+        # a batch of 32 link queries (the paper's default) answered online: one pooling row a query
+        # over its joined set of a graph sampled with M = 50, m = 4; launches count
+        _attend("readout_online", "attend", "bf16", 32, (1, 1), (20, 402), 4, 4, 64, False, 0, 0),
+        # the same for 8,192 queries of M = 200, m = 4 (joined sets of up to 1,602 nodes), heads shared
+        _attend("readout_sets", "attend", "bf16", 8192, (1, 1), (1, 1602), 8, 2, 64, False, 0, 0),
+        # serving: one new token each for a few long sequences whose keys and values are kept
+        _attend("continue_long", "attend", "fp16", 6, (1, 1), (9_001, 65_536), 32, 4, 128, True, 128, 32),
+        # walks of the longest kind (m = 15) as sequences of 16 steps, the bias by step distance
+        _attend("walks_train", "attend_train", "bf16", 16_384, (16, 16), None, 8, 8, 64, True, 15, 16),
+        # all walks of a seed behind one another (up to 2,048 entries), both directions, odd width
+        _attend("tables_train", "attend_train", "fp16", 24, (1, 2048), None, 12, 4, 80, False, 128, 32),
+        # packed long sequences of a causal model, shared heads, the bias by logarithmic distance
+        _attend("packed_train", "attend_train", "bf16", 5, (333, 4096), None, 16, 4, 128, True, 128, 32),
+        # a whole long sequence taken in at once before it is continued
+        _attend("prompt_long", "attend", "bf16", 1, (16_384, 16_384), None, 16, 2, 128, True, 0, 0),
+        # a handful of held-out steps scored on the smallest graph; launches count
+        _loss("loss_few", "loss", "fp16", 7, 4096, 64),
+        # 16 steps scored against every node of the 2.9M-node graph: reads the table once
+        _loss("score_citation", "loss", "bf16", 16, 2_900_000, 128),
+        # one training step of next-node prediction on the 235,000-node graph
+        _loss("collab_train", "loss_train", "bf16", 8192, 235_000, 128),
+        # the same on the 2.9M-node graph, narrower rows
+        _loss("citation_train", "loss_train", "fp16", 2048, 2_900_000, 64),
+        # odd numbers of rows and nodes, wide rows
+        _loss("odd_train", "loss_train", "bf16", 15_001, 99_991, 200),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng) -> dict:
+    dtype = rng.choice(["bf16", "fp16"])
+    kind = rng.choice(["readout", "continue", "chunk", "walks", "packed", "loss", "loss_train"])
+    if kind == "loss":
+        rows, nodes, dim = _log_int(rng, 1, 4096), _log_int(rng, 4096, 2_900_000), 8 * rng.randint(4, 32)
+        rows = max(1, min(rows, 6_000_000_000 // nodes))
+        case = _loss(None, "loss", dtype, rows, nodes, dim)
+    elif kind == "loss_train":
+        rows, nodes, dim = _log_int(rng, 64, 16_384), _log_int(rng, 4096, 2_900_000), 8 * rng.randint(4, 32)
+        rows = max(1, min(rows, 250_000_000_000 // (nodes * dim)))
+        case = _loss(None, "loss_train", dtype, rows, nodes, dim)
+    else:
+        kv_heads = rng.choice([1, 2, 4])
+        heads = kv_heads * rng.choice([1, 2, 3, 4, 8])
+        dim = 8 * rng.randint(4, 16)
+        reach = rng.choice([0, 16, 64, 128])
+        buckets = rng.choice([8, 16, 32]) if reach else 0
+        if kind == "readout":
+            k_hi = _log_int(rng, 20, 1602)
+            seqs = _log_int(rng, 16, min(8192, max(16, 1_500_000_000 // (k_hi * kv_heads * dim))))
+            case = _attend(None, "attend", dtype, seqs, (1, 1), (rng.choice([0, 1]), k_hi), heads, kv_heads,
+                           dim, False, reach, buckets)
+        elif kind == "continue":
+            k_hi = _log_int(rng, 1000, 65_536)
+            case = _attend(None, "attend", dtype, _log_int(rng, 1, 32), (1, 1), (k_hi // 8 + 1, k_hi),
+                           heads, kv_heads, dim, True, reach, buckets)
+        elif kind == "chunk":
+            q_hi = _log_int(rng, 2, 1024)
+            k_hi = max(q_hi, _log_int(rng, 1000, 16_384))
+            seqs = min(_log_int(rng, 1, 8), max(1, 2_000_000_000 // (heads * q_hi * k_hi)))
+            case = _attend(None, "attend", dtype, seqs, (1, q_hi), (q_hi, k_hi), heads, kv_heads, dim,
+                           True, reach, buckets)
+        elif kind == "walks":
+            steps = rng.randint(4, 16)
+            case = _attend(None, "attend_train", dtype, _log_int(rng, 64, 16_384), (steps, steps), None,
+                           min(heads, 8), min(heads, 8), dim, rng.random() < 0.7, reach, buckets)
+        else:
+            hi = _log_int(rng, 100, 4096)
+            seqs = min(_log_int(rng, 1, 64), max(1, 900_000_000 // (heads * hi * hi)))
+            case = _attend(None, rng.choice(["attend", "attend_train"]), dtype, seqs, (rng.choice([0, 1]), hi), None,
+                           heads, kv_heads, dim, rng.random() < 0.5, reach, buckets)
+    del case["name"]
+    return case
+
+
+# --------------------------------------------------------------------------- #
+# inputs
+# --------------------------------------------------------------------------- #
+def _lengths(lo, hi, n, seed):
+    """n lengths on the host, spread over lo .. hi, the longest among them; their order is the seed's, so
+    that outputs have one shape."""
+    out = torch.randint(lo, hi + 1, (n,), generator=torch.Generator().manual_seed(n + hi))
+    out[0] = hi
+    return out[torch.randperm(n, generator=torch.Generator().manual_seed(seed))]
+
+
+def _packed_lengths(case, seed):
+    q = _lengths(case["q_lo"], case["q_hi"], case["seqs"], 2 * seed)
+    k = q if not case["k_hi"] else _lengths(case["k_lo"], case["k_hi"], case["seqs"], 2 * seed + 1)
+    return q, k
+
+
+def _bucket_map(reach, buckets, causal):
+    """The bucket of every distance -reach .. reach: one for each near distance, then ever wider ones
+    (whole-number arithmetic); where all distances count, forward ones have buckets of their own."""
+    half = buckets if causal else buckets // 2
+    near = max(1, half // 2)
+    out = []
+    for d in range(-reach, reach + 1):
+        a = abs(d)
+        if a < near:
+            b = a
+        else:   # thresholds near * (reach / near)^(i / (half - near)), compared as whole powers
+            b = near
+            while b + 1 < half and a ** (half - near) * near ** (b + 1 - near) >= \
+                    reach ** (b + 1 - near) * near ** (half - near):
+                b += 1
+        out.append(b if d <= 0 or causal else half + b)
+    return out
+
+
+def prepare(case, seed):
+    dev, t = "cuda", _TYPES[case["dtype"]]
+    g = torch.Generator(device=dev).manual_seed(seed)
+
+    def normal(*shape, std=1.0):
+        x = torch.empty(shape, dtype=t, device=dev)
+        return x.normal_(0.0, std, generator=g)
+
+    if case["op"].startswith("loss"):
+        n, v, d = case["rows"], case["nodes"], case["dim"]
+        h = normal(n, d)
+        w = normal(v, d, std=2.0 / math.sqrt(d))
+        # next nodes of walks: few nodes are met often; a few rows count for nothing
+        u = torch.rand(n, device=dev, generator=g)
+        labels = (v * u ** 3).long().clamp_(max=v - 1)
+        perm = torch.randint(1, v, (1,), device=dev, generator=g)
+        labels = ((labels + perm) % v).int()
+        labels[torch.rand(n, device=dev, generator=g) < 0.03] = -1
+        dloss = torch.full((n,), 1.0 / n, device=dev) * (labels >= 0)
+        return dict(case=case, h=h, w=w, labels=labels, dloss=dloss)
+    ql, kl = _packed_lengths(case, seed)
+    off = lambda x: F.pad(torch.cumsum(x, 0), (1, 0)).to(dev)  # noqa: E731
+    tq, tk = int(ql.sum()), int(kl.sum())
+    state = dict(case=case, q_off=off(ql), k_off=off(kl), max_q=int(ql.max()), max_k=int(kl.max()),
+                 q=normal(tq, case["heads"], case["dim"]), k=normal(tk, case["kv_heads"], case["dim"]),
+                 v=normal(tk, case["kv_heads"], case["dim"]), bias=None, bucket=None)
+    if case["reach"]:
+        state["bucket"] = torch.tensor(_bucket_map(case["reach"], case["buckets"], case["causal"]),
+                                       dtype=torch.int32, device=dev)
+        state["bias"] = normal(case["buckets"], case["heads"], std=0.5)
+    if case["op"] == "attend_train":
+        state["dout"] = normal(tq, case["heads"], case["dim"], std=0.05)
+    return state
+
+
+# --------------------------------------------------------------------------- #
+# one pass
+# --------------------------------------------------------------------------- #
+def _plain_attention(st):
+    case, t = st["case"], st["q"].dtype
+    H, Hk, D = case["heads"], case["kv_heads"], case["dim"]
+    G, Lq, Lk, scale = H // Hk, st["max_q"], st["max_k"], D ** -0.5
+    S = case["seqs"]
+    nq, nk = st["q_off"].diff()[:, None], st["k_off"].diff()[:, None]
+    i, j = torch.arange(Lq, device="cuda")[None], torch.arange(Lk, device="cuda")[None]
+    q_in, k_in = i < nq, j < nk
+    q_at, k_at = (st["q_off"][:-1, None] + i)[q_in], (st["k_off"][:-1, None] + j)[k_in]
+
+    def padded(x, inside, length):   # packed rows -> [S, heads of keys, heads of a group * length, D]
+        y = x.new_zeros((S, length, *x.shape[1:]), dtype=torch.float32)
+        y[inside] = x.float()
+        return y.view(S, length, Hk, -1, D).permute(0, 2, 3, 1, 4).reshape(S, Hk, -1, D)
+
+    def packed(y, inside, at, like, length):
+        y = y.view(S, Hk, -1, length, D).permute(0, 3, 1, 2, 4).reshape(S, length, -1, D)
+        out = torch.zeros(like.shape, dtype=torch.float32, device="cuda")
+        out[at] = y[inside]
+        return out.to(t)
+
+    q, k, v = padded(st["q"], q_in, Lq), padded(st["k"], k_in, Lk), padded(st["v"], k_in, Lk)
+    s = (q @ k.transpose(-1, -2)).mul_(scale).view(S, Hk, G, Lq, Lk)
+    last = (i + nk - nq)[:, :, None]                       # the key that a row stands at
+    dist = j[:, None, :] - last                            # [S, Lq, Lk]
+    if st["bias"] is not None:
+        R = case["reach"]
+        of = st["bucket"].long()[dist.clamp(-R, R) + R]
+        s += st["bias"].float()[of].permute(0, 3, 1, 2).view(S, Hk, G, Lq, Lk)
+    seen = (k_in[:, None, :] & q_in[:, :, None] & (dist <= 0 if case["causal"] else True))[:, None, None]
+    s.masked_fill_(~seen, -math.inf)
+    top = s.amax(-1, keepdim=True)
+    top = torch.where(torch.isinf(top), torch.zeros_like(top), top)
+    p = s.sub_(top).exp_()
+    total = p.sum(-1, keepdim=True)
+    lse = (top + total.log()).view(S, Hk * G, Lq).permute(0, 2, 1)[q_in]
+    p = (p / total.clamp(min=1e-37)).view(S, Hk, G * Lq, Lk)
+    out = packed(p @ v, q_in, q_at, st["q"], Lq)
+    if case["op"] == "attend":
+        return out, lse
+    do = padded(st["dout"], q_in, Lq)
+    dv = packed(p.transpose(-1, -2) @ do, k_in, k_at, st["v"], Lk)
+    dp = do @ v.transpose(-1, -2)
+    ds = p * (dp - (p * dp).sum(-1, keepdim=True))
+    dq = packed((ds @ k) * scale, q_in, q_at, st["q"], Lq)
+    dk = packed((ds.transpose(-1, -2) @ q) * scale, k_in, k_at, st["k"], Lk)
+    if st["bias"] is None:
+        return out, lse, dq, dk, dv
+    # sums along the diagonals of every sequence (rows from the last to the first, each one place further
+    # right than the row above), then the diagonals of every bucket
+    skew = F.pad(ds.view(S, H, Lq, Lk).flip(2), (0, Lq)).view(S, H, -1)[..., :Lq * (Lk + Lq - 1)]
+    diag = skew.reshape(S, H, Lq, Lk + Lq - 1).sum(2)      # [S, H, j - i + Lq - 1]
+    dd = torch.arange(1 - Lq, Lk, device="cuda")[None] - (nk - nq)
+    of = st["bucket"].long()[dd.clamp(-R, R) + R]
+    in_bucket = (of[..., None] == torch.arange(case["buckets"], device="cuda")).float()
+    dbias = (diag @ in_bucket).sum(0).t()
+    return out, lse, dq, dk, dv, dbias.to(t)
+
+
+def _plain_loss(st):
+    h, w, t = st["h"].float(), st["w"].float(), st["h"].dtype
+    counts = st["labels"] >= 0
+    at = st["labels"].long().clamp(min=0)[:, None]
+    z = h @ w.t()
+    top = z.amax(1, keepdim=True)
+    hit = z.gather(1, at)
+    p = z.sub_(top).exp_()
+    total = p.sum(1, keepdim=True)
+    lse = (top + total.log())[:, 0]
+    loss = torch.where(counts, lse - hit[:, 0], torch.zeros_like(lse))
+    if st["case"]["op"] == "loss":
+        return loss, lse
+    g = p.div_(total).scatter_add_(1, at, torch.full_like(hit, -1.0)).mul_(st["dloss"][:, None])
+    return loss, lse, (g @ w).to(t), (g.t() @ h).to(t)
+
+
+def run(st):
+    case = st["case"]
+    if not own:
+        return _plain_loss(st) if case["op"].startswith("loss") else _plain_attention(st)
+    from paper_2202_13538_amd import binding
+    ctx = _ctx()
+    if case["op"].startswith("loss"):
+        loss, lse = binding.softmax_loss(ctx, st["h"], st["w"], st["labels"])
+        if case["op"] == "loss":
+            return loss, lse
+        return loss, lse, *binding.softmax_loss_grad(ctx, st["dloss"], st["h"], st["w"], st["labels"], lse)
+    how = dict(causal=case["causal"], bias=st["bias"], bucket=st["bucket"])
+    out, lse = binding.attention(ctx, st["q"], st["k"], st["v"], st["q_off"], st["k_off"], **how)
+    if case["op"] == "attend":
+        return out, lse
+    dq, dk, dv, dbias = binding.attention_grad(ctx, st["dout"], st["q"], st["k"], st["v"], out, lse,
+                                               st["q_off"], st["k_off"], **how)
+    return (out, lse, dq, dk, dv) if dbias is None else (out, lse, dq, dk, dv, dbias)
+
+
+# --------------------------------------------------------------------------- #
+# what a pass cannot do without
+# --------------------------------------------------------------------------- #
+def work(case) -> dict:
+    """Bytes: every input and output once.  Operations: of the products over what the masks leave (a
+    training pass: the scores, the values' sum and the five products of the gradient; or the logits, the
+    logits again, as they are not kept, and the two products of the gradient).  Where queries and keys have
+    lengths of their own, which of them meet depends on the seed: those of one seed are counted."""
+    e = 2
+    if case["op"].startswith("loss"):
+        n, v, d = case["rows"], case["nodes"], case["dim"]
+        train = case["op"] == "loss_train"
+        return dict(bytes=e * (n + v) * d * (2 if train else 1) + n * (4 + 8 + (4 if train else 0)),
+                    flops=2 * n * v * d * (4 if train else 1))
+    ql, kl = _packed_lengths(case, 1)
+    tq, tk = int(ql.sum()), int(kl.sum())
+    if case["causal"]:   # row i sees i + 1 + nk - nq keys, none where that is negative
+        first = kl - ql + 1
+        rows = torch.minimum(ql, kl)
+        pairs = int((rows * (first.clamp(min=1) + kl) // 2).sum())
+    else:
+        pairs = int((ql * kl).sum())
+    H, Hk, D = case["heads"], case["kv_heads"], case["dim"]
+    size = e * D * (2 * tq * H + 2 * tk * Hk) + 4 * tq * H + 16 * (case["seqs"] + 1)
+    size += e * case["buckets"] * H
+    flops = 4 * D * H * pairs
+    if case["op"] == "attend_train":
+        size += e * D * (2 * tq * H + 2 * tk * Hk) + e * case["buckets"] * H
+        flops = 14 * D * H * pairs
+    return dict(bytes=size, flops=flops)
+
+
+# --------------------------------------------------------------------------- #
+# the definitions, in 64 bits
+# --------------------------------------------------------------------------- #
+def exact(case, seed):
+    st = prepare(case, seed)
+    if case["op"].startswith("loss"):
+        return _exact_loss(st)
+    train, H, Hk, D = case["op"] == "attend_train", case["heads"], case["kv_heads"], case["dim"]
+    G, R = H // Hk, case["reach"]
+    wide = lambda x: x.double().transpose(0, 1).contiguous()  # noqa: E731  [heads, rows, D]
+    q, k, v = wide(st["q"]), wide(st["k"]), wide(st["v"])
+    do = wide(st["dout"]) if train else None
+    out, lse = torch.zeros_like(q), torch.full(q.shape[:2], -math.inf, dtype=torch.float64, device="cuda")
+    dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    bias = st["bias"].double() if R else None
+    dbias = torch.zeros_like(bias) if R else None
+    qo, ko = st["q_off"].tolist(), st["k_off"].tolist()
+    # sequences of equal lengths in one step
+    alike = {}
+    for n in range(case["seqs"]):
+        alike.setdefault((qo[n + 1] - qo[n], ko[n + 1] - ko[n]), []).append(n)
+    for (nq, nk), which in alike.items():
+        if not nq or not nk:
+            continue
+        i, j = torch.arange(nq, device="cuda"), torch.arange(nk, device="cuda")
+        d = j[None] - i[:, None] - (nk - nq)
+        hidden = (d > 0) if case["causal"] else None
+        of = st["bucket"].long()[d.clamp(-R, R) + R] if R else None
+        step = max(1, 100_000_000 // (nq * nk))
+        for a in range(0, len(which), step):
+            rows = torch.tensor([qo[n] for n in which[a:a + step]], device="cuda")[:, None] + i
+            keys = torch.tensor([ko[n] for n in which[a:a + step]], device="cuda")[:, None] + j
+            for head in range(H):
+                hk = head // G
+                Q, K, V = q[head][rows], k[hk][keys], v[hk][keys]
+                s = torch.matmul(Q, K.transpose(1, 2)) / math.sqrt(D)
+                if R:
+                    s += bias[:, head][of]
+                if hidden is not None:
+                    s.masked_fill_(hidden, -math.inf)
+                total = torch.logsumexp(s, 2)
+                lse[head, rows] = total
+                p = torch.exp(s - total[..., None]).nan_to_num_(0.0)
+                out[head, rows] = torch.matmul(p, V)
+                if not train:
+                    continue
+                E = do[head][rows]
+                dv[hk].index_add_(0, keys.view(-1), torch.matmul(p.transpose(1, 2), E).view(-1, D))
+                e = torch.matmul(E, V.transpose(1, 2))
+                ds = p * (e - (p * e).sum(2, keepdim=True))
+                dq[head, rows] = torch.matmul(ds, K) / math.sqrt(D)
+                dk[hk].index_add_(0, keys.view(-1),
+                                  torch.matmul(ds.transpose(1, 2), Q).view(-1, D) / math.sqrt(D))
+                if R:
+                    flat, total_ds = of.view(-1), ds.sum(0).view(-1)
+                    for b in range(case["buckets"]):
+                        dbias[b, head] += total_ds[flat == b].sum()
+    back = lambda x: x.transpose(0, 1).contiguous()  # noqa: E731
+    if not train:
+        return back(out), back(lse)
+    got = (back(out), back(lse), back(dq), back(dk), back(dv))
+    return (*got, dbias) if R else got
+
+
+def _exact_loss(st):
+    h, w = st["h"].double(), st["w"].double()
+    n, v = h.shape[0], w.shape[0]
+    loss, lse = torch.zeros(n, dtype=torch.float64, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+    train = st["case"]["op"] == "loss_train"
+    dh, dw = torch.zeros_like(h), torch.zeros_like(w) if train else None
+    step = max(1, 2_000_000_000 // v)
+    for a in range(0, n, step):
+        rows, lab = h[a:a + step], st["labels"][a:a + step].long()
+        z = torch.matmul(rows, w.t())
+        total = torch.logsumexp(z, 1)
+        lse[a:a + step] = total
+        keep = lab >= 0
+        at = torch.arange(len(lab), device="cuda")[keep]
+        loss[a:a + step][keep] = total[keep] - z[at, lab[keep]]
+        if train:
+            g = z.sub_(total[:, None]).exp_()
+            g[at, lab[keep]] -= 1.0
+            g *= st["dloss"][a:a + step].double()[:, None]
+            dh[a:a + step] = torch.matmul(g, w)
+            dw += torch.matmul(g.t(), rows)
+    return (loss, lse, dh, dw) if train else (loss, lse)
