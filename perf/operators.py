@@ -186,7 +186,8 @@ def prepare(case, seed):
     ql, kl = _packed_lengths(case, seed)
     off = lambda x: F.pad(torch.cumsum(x, 0), (1, 0)).to(dev)  # noqa: E731
     tq, tk = int(ql.sum()), int(kl.sum())
-    state = dict(case=case, q_off=off(ql), k_off=off(kl), max_q=int(ql.max()), max_k=int(kl.max()),
+    q_off = off(ql)
+    state = dict(case=case, q_off=q_off, k_off=off(kl) if case["k_hi"] else q_off, max_q=int(ql.max()), max_k=int(kl.max()),
                  q=normal(tq, case["heads"], case["dim"]), k=normal(tk, case["kv_heads"], case["dim"]),
                  v=normal(tk, case["kv_heads"], case["dim"]), bias=None, bucket=None)
     if case["reach"]:
