@@ -17,6 +17,8 @@
  * surel_join_query_ids (the union join over those RPE-IDs), and
  * surel_query_incidence + surel_bfs_batches (Sec. 3.6 "Mini-batching for Training";
  * Algorithm 2: mini-batches of queries that share nodes, by breadth-first search).
+ * Behind them, for a model that reads walks or joined sets: surel_attention (rows packed with the
+ * offsets that the join and the RPE table are laid out by).
  *
  * Conventions
  *   - Plain C ABI.  Pointers named d_* are DEVICE memory owned by the caller, on the
@@ -102,6 +104,9 @@ extern "C" {
                                           or surel_prune_rpe ran out (see surel_set_spin_limit), or
                                           a bounded probe of a hash table of surel_bfs_batches;
                                           outputs are incomplete                             */
+#define SUREL_DEV_BAD_OFFSETS   0x200u /* packed offsets are not non-decreasing from 0 to the number
+                                          of rows; rows of such a sequence are empty or unwritten */
+#define SUREL_DEV_BAD_BUCKET    0x400u /* a bucket number is not in [0, n_buckets): taken as 0 */
 
 /* limits */
 #define SUREL_MAX_NODES   268435455   /* 2^28 - 1: node id and step share one 32-bit sort key */
@@ -112,6 +117,10 @@ extern "C" {
 #define SUREL_MAX_TUPLE   3           /* join: k                                             */
 #define SUREL_MAX_DISTINCT 16777216   /* prune: cap_T (2^24 distinct count vectors)          */
 #define SUREL_MAX_BATCH   1048576     /* mini-batching: B1, B2 and the seed-set size (2^20)   */
+#define SUREL_MAX_ROWS    1073741824  /* attention: packed rows of queries or keys (2^30)    */
+#define SUREL_MAX_HEAD_DIM 128        /* attention: elements of a head's row                 */
+#define SUREL_MAX_REACH   1024        /* attention: largest distance with a bucket of its own */
+#define SUREL_MAX_STRIDE  16777208    /* attention: elements between rows or heads (2^24 - 8) */
 #define SUREL_NOALLOC_MAX_QUERIES 1048576  /* surel_join_queries_noalloc: n_queries (2^20)    */
 
 /* kernel groups for surel_profile_read */
@@ -128,7 +137,12 @@ extern "C" {
 #define SUREL_K_QUERY_IDS   8   /* surel_query_rpe_ids                                */
 #define SUREL_K_PRUNE       9   /* surel_prune_rpe (all its launches)                 */
 #define SUREL_K_BATCH       10  /* surel_query_incidence and surel_bfs_batches        */
-#define SUREL_K_COUNT       11
+#define SUREL_K_ATTENTION   11  /* surel_attention                                    */
+#define SUREL_K_COUNT       12
+
+/* 16-bit element types of a model's tensors */
+#define SUREL_BF16          0
+#define SUREL_FP16          1
 
 typedef struct surel_ctx surel_ctx;
 
@@ -411,6 +425,48 @@ int surel_bfs_batches(surel_ctx* ctx, const int32_t* d_queries, int64_t n_querie
                       const int32_t* d_start, int64_t n_batches, int32_t n_start, int32_t B1,
                       int32_t B2, int32_t* d_vbar, int32_t* d_batch, int32_t* d_tuples,
                       int32_t* d_counts);
+
+/* What surel_attention attends to what with.  Rows of several sequences lie behind one another:
+ * sequence s has the query rows d_q_off[s] .. d_q_off[s+1]-1 and the keys d_k_off[s] ..
+ * d_k_off[s+1]-1 (d_join_off and d_rpe_off are such offsets; for walks they are multiples of m+1).
+ *   d_q            [n_q][heads][dim], d_k and d_v [n_k][kv_heads][dim] of `type` (device, read-only);
+ *                  q_row, q_head, ... are the elements between rows and between heads, so that parts
+ *                  of one larger tensor serve.  A head's row is contiguous.  Every head's row starts on a
+ *                  16-byte boundary: pointers are multiples of 16 bytes, strides of 8 elements.
+ *   heads          a multiple of kv_heads: query head h reads key head h / (heads / kv_heads).
+ *   d_q_off, d_k_off  int64[n_seqs+1] (device, read-only), from 0 to n_q and n_k; may be one array.
+ *   causal         0, or 1: a sequence's last query row stands at its last key, and a row sees the keys
+ *                  up to the one that it stands at.  (One query row: a new token over kept keys.)
+ *   scale          of the products q . k, > 0.
+ *   d_bias         NULL, or [n_buckets][heads] of `type` (device, read-only): a learned bias by distance.
+ *                  A score gets d_bias[d_bucket[min(max(d, -reach), reach) + reach]][head], d the key's
+ *                  place minus the place that the query row stands at.
+ *   d_bucket       int32[2 * reach + 1] (device, read-only), entries in [0, n_buckets).
+ * Limits: n_seqs >= 0, n_q and n_k up to SUREL_MAX_ROWS, dim a multiple of 8 up to SUREL_MAX_HEAD_DIM, strides
+ * >= 0 up to SUREL_MAX_STRIDE, 0 <= reach <= SUREL_MAX_REACH, 1 <= heads <= 65535. */
+typedef struct surel_attention_args {
+    const void *d_q, *d_k, *d_v;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    const int64_t *d_q_off, *d_k_off;
+    int64_t n_seqs, n_q, n_k;
+    int32_t type, heads, kv_heads, dim, causal;
+    float scale;
+    const void* d_bias;
+    const int32_t* d_bucket;
+    int32_t n_buckets, reach;
+} surel_attention_args;
+
+/* Attention: for every query row i and head, out_i = sum_j p_ij v_j with p_i the softmax over the keys j
+ * that row i sees of scale (q_i . k_j) + bias.  Scores, softmax and sums are 32-bit; the weights are
+ * rounded to `type` for their product with the values, the result once more.
+ *   d_out   [n_q][heads][dim] of `type`, dense, on a 16-byte boundary (device, written).
+ *   d_lse   float[n_q][heads] (device, written): the logarithm of the sum of exponentials.
+ * A row that sees no key gets zeros, and a d_lse of minus infinity.  What a row does not see, another
+ * sequence's rows or later keys, has no influence on it, whatever it holds.
+ * Where few rows meet many keys the keys are split over workgroups and the context's workspace grows
+ * by 4 (dim + 2) bytes a row, head and part (128 parts at most).  Results are the same every time.
+ * Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
+int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_out, float* d_lse);
 
 /* Every wait inside the fused kernel of surel_sample_walks_rpe and surel_sample_walks_rpe_ids (a
  * wave waiting for an offset, the offset scan waiting for a row count) and inside the pruning (a

@@ -18,22 +18,37 @@ LIB_PATH = os.path.join(_PKG_DIR, "libsurel.so")
 OK, E_NULL, E_RANGE, E_HIP, E_CAPACITY, E_CTX, E_DEVICE = 0, -1, -2, -3, -4, -5, -6
 DEV_BAD_SEED, DEV_BAD_GRAPH, DEV_BAD_WALK, DEV_BAD_QUERY = 0x01, 0x02, 0x04, 0x08
 DEV_SET_TOO_LARGE, DEV_CAPACITY, DEV_BAD_TABLE, DEV_BAD_SIZES = 0x10, 0x20, 0x40, 0x80
-DEV_STALL = 0x100
+DEV_STALL, DEV_BAD_OFFSETS, DEV_BAD_BUCKET = 0x100, 0x200, 0x400
 MAX_NODES, MAX_STEPS, MAX_WALKS = 268435455, 15, 65535
 MAX_WALK_ENTRIES, MAX_SET, MAX_TUPLE = 2048, 2048, 3
 MAX_DISTINCT = 1 << 24
 MAX_BATCH = 1 << 20
+MAX_ROWS, MAX_HEAD_DIM, MAX_REACH, MAX_STRIDE = 1 << 30, 128, 1024, (1 << 24) - 8
 NOALLOC_MAX_QUERIES = 1 << 20
+BF16, FP16 = 0, 1
 
 (K_WALK, K_RPE_COUNT, K_RPE_FILL, K_JOIN_COUNT, K_JOIN_FILL, K_SCAN, K_WALK_RPE,
- K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_COUNT) = range(12)
+ K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_ATTENTION, K_COUNT) = range(13)
 KERNEL_NAMES = {K_WALK: "walk", K_RPE_COUNT: "rpe_count", K_RPE_FILL: "rpe_fill",
                 K_JOIN_COUNT: "join_count", K_JOIN_FILL: "join_fill", K_SCAN: "scan",
                 K_WALK_RPE: "walk_rpe", K_EDGE_RECORDS: "edge_records",
-                K_QUERY_IDS: "query_ids", K_PRUNE: "prune", K_BATCH: "batch"}
+                K_QUERY_IDS: "query_ids", K_PRUNE: "prune", K_BATCH: "batch",
+                K_ATTENTION: "attention"}
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
+
+
+class AttentionArgs(ctypes.Structure):
+    """surel_attention_args"""
+    _fields_ = [(n, _vp) for n in ("d_q", "d_k", "d_v")] + \
+               [(n, _i64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] + \
+               [(n, _vp) for n in ("d_q_off", "d_k_off")] + \
+               [(n, _i64) for n in ("n_seqs", "n_q", "n_k")] + \
+               [(n, _i32) for n in ("type", "heads", "kv_heads", "dim", "causal")] + \
+               [("scale", ctypes.c_float), ("d_bias", _vp), ("d_bucket", _vp), ("n_buckets", _i32),
+                ("reach", _i32)]
+
 
 # name -> (restype, argtypes); the order and types of include/surel.h
 SIGNATURES = {
@@ -71,6 +86,7 @@ SIGNATURES = {
     "surel_query_incidence": (ctypes.c_int, [_vp, _vp, _i64, _i32, _i32, _vp, _vp]),
     "surel_bfs_batches": (ctypes.c_int, [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _i64, _i32,
                                          _i32, _i32, _vp, _vp, _vp, _vp]),
+    "surel_attention": (ctypes.c_int, [_vp, ctypes.POINTER(AttentionArgs), _vp, _vp]),
     "surel_set_spin_limit": (ctypes.c_int, [_vp, ctypes.c_uint32]),
     "surel_check": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "surel_profile_enable": (ctypes.c_int, [_vp, ctypes.c_int]),
@@ -555,3 +571,87 @@ def bfs_batches(ctx: Context, queries: torch.Tensor, n_nodes: int, inc_off: torc
     if rc != OK:
         raise SurelError(rc, "surel_bfs_batches")
     return vbar, batch, tuples, counts
+
+
+_TYPES = {torch.bfloat16: BF16, torch.float16: FP16}
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor, what: str):
+    """(address, elements between rows, elements between heads) of a [rows][heads][dim] tensor, whose rows
+    and heads may lie apart."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{what} must be {like.dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must live on the GPU")
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [rows][heads][dim]")
+    row, head, one = t.stride()
+    if one != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what}'s last dimension must be contiguous")
+    return t.data_ptr(), row, head
+
+
+def _attention_args(q, k, v, q_off, k_off, causal, scale, bias, bucket) -> AttentionArgs:
+    if q.dtype not in _TYPES:
+        raise TypeError(f"q must be torch.bfloat16 or torch.float16, got {q.dtype}")
+    q_ptr, q_row, q_head = _rows(q, q, "q")
+    k_ptr, k_row, k_head = _rows(k, q, "k")
+    v_ptr, v_row, v_head = _rows(v, q, "v")
+    n_q, heads, dim = q.shape
+    if k.shape != v.shape or k.shape[2] != dim:
+        raise ValueError("k and v must have one shape, and q's last dimension")
+    if k_off is None:
+        k_off = q_off
+    if q_off.numel() != k_off.numel() or q_off.numel() < 1:
+        raise ValueError("q_off and k_off must have one entry more than there are sequences")
+    if (bias is None) != (bucket is None):
+        raise ValueError("bias and bucket go together")
+    if bias is not None and (bias.dim() != 2 or bias.shape[1] != heads or bucket.numel() % 2 != 1):
+        raise ValueError("bias must be [buckets][heads], bucket have 2 * reach + 1 entries")
+    return AttentionArgs(
+        q_ptr, k_ptr, v_ptr, q_row, q_head, k_row, k_head, v_row, v_head,
+        _ptr(q_off, torch.int64, "q_off"), _ptr(k_off, torch.int64, "k_off"), q_off.numel() - 1, n_q,
+        k.shape[0], _TYPES[q.dtype], heads, k.shape[1], dim, 1 if causal else 0,
+        dim ** -0.5 if scale is None else scale, _ptr(bias, q.dtype, "bias"),
+        _ptr(bucket, torch.int32, "bucket"), 0 if bias is None else bias.shape[0],
+        0 if bucket is None else bucket.numel() // 2)
+
+
+def attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_off: torch.Tensor,
+              k_off: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
+              bias: torch.Tensor | None = None, bucket: torch.Tensor | None = None):
+    """(out [n_q][heads][dim], lse float32[n_q][heads]) on the GPU: attention of packed query rows
+    q [n_q][heads][dim] to packed keys k, v [n_k][kv_heads][dim] (bfloat16 or float16; views of a larger
+    tensor will do).  Sequence s has rows q_off[s] .. q_off[s+1]-1 and keys k_off[s] .. k_off[s+1]-1 (int64,
+    like join_off and rpe_off; k_off None: the same as q_off).  causal: a sequence's last row stands at its
+    last key, rows see keys up to their own.  scale None: 1 / sqrt(dim).  bias [buckets][heads] and bucket
+    int32[2 * reach + 1] (see distance_buckets): a learned bias by the distance of key and row."""
+    args = _attention_args(q, k, v, q_off, k_off, causal, scale, bias, bucket)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    rc = load().surel_attention(ctx.handle, ctypes.byref(args), out.data_ptr(), lse.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_attention")
+    return out, lse
+
+
+def distance_buckets(reach: int, buckets: int, causal: bool = False) -> list[int]:
+    """The bucket of every distance -reach .. reach: near distances have one each, farther ones share ever
+    wider ones up to reach.  Where all distances count, keys ahead have the upper half of the buckets; a
+    causal row sees none of them.  (torch.tensor(..., dtype=torch.int32) of it is a `bucket` for attention.)"""
+    half = buckets if causal else buckets // 2
+    if reach < 0 or half < 1:
+        raise ValueError("reach must not be negative, and each direction needs a bucket")
+    near = max(1, half // 2)
+    out = []
+    for d in range(-reach, reach + 1):
+        b = abs(d)
+        if b >= near:
+            # bucket b starts at near * (reach / near) ** ((b - near) / (half - near)), whole numbers compared
+            b, far = near, half - near
+            while b + 1 < half and abs(d) ** far * near ** (b + 1 - near) >= \
+                    reach ** (b + 1 - near) * near ** far:
+                b += 1
+            b = min(b, half - 1)
+        out.append(b if d <= 0 or causal else half + b)
+    return out

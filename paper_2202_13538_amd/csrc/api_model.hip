@@ -1,0 +1,82 @@
+// The C ABI of libsurel, continued: the operators of a model behind walks and joined sets.  See
+// include/surel.h for the contract of every entry point.
+#include "../../include/surel.h"
+
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include "attention.h"
+#include "context.h"
+#include "kernels.h"
+
+namespace {
+
+bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+bool bad_stride(int64_t elements) { return elements < 0 || elements > SUREL_MAX_STRIDE || elements % 8 != 0; }
+
+// Checks what an attention call was given, and says it in the kernels' words.
+int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::AttentionArgs* a) {
+    if (!x) return SUREL_E_NULL;
+    if (x->type != SUREL_BF16 && x->type != SUREL_FP16) return SUREL_E_RANGE;
+    if (x->n_seqs < 0 || x->n_seqs > SUREL_MAX_ROWS || x->n_q < 0 || x->n_q > SUREL_MAX_ROWS || x->n_k < 0 ||
+        x->n_k > SUREL_MAX_ROWS)
+        return SUREL_E_RANGE;
+    if (x->dim < 8 || x->dim > SUREL_MAX_HEAD_DIM || x->dim % 8 != 0) return SUREL_E_RANGE;
+    if (x->heads < 1 || x->heads > 65535 || x->kv_heads < 1 || x->heads % x->kv_heads != 0) return SUREL_E_RANGE;
+    if (bad_stride(x->q_row) || bad_stride(x->q_head) || bad_stride(x->k_row) || bad_stride(x->k_head) ||
+        bad_stride(x->v_row) || bad_stride(x->v_head))
+        return SUREL_E_RANGE;
+    if (!(x->scale > 0.f) || !isfinite(x->scale)) return SUREL_E_RANGE;
+    if (x->causal != 0 && x->causal != 1) return SUREL_E_RANGE;
+    if ((x->d_bias == nullptr) != (x->d_bucket == nullptr)) return SUREL_E_NULL;
+    if (x->d_bias && (x->n_buckets < 1 || x->n_buckets > 2 * SUREL_MAX_REACH + 1 || x->reach < 0 ||
+                      x->reach > SUREL_MAX_REACH))
+        return SUREL_E_RANGE;
+    if (x->n_seqs > 0 && (!x->d_q_off || !x->d_k_off)) return SUREL_E_NULL;
+    if (x->n_q > 0 && !x->d_q) return SUREL_E_NULL;
+    if (x->n_k > 0 && (!x->d_k || !x->d_v)) return SUREL_E_NULL;
+    if (misaligned16(x->d_q) || misaligned16(x->d_k) || misaligned16(x->d_v)) return SUREL_E_RANGE;
+    if (x->n_seqs == 0 && (x->n_q > 0 || x->n_k > 0)) return SUREL_E_RANGE;
+    if (!ctx) return SUREL_E_CTX;
+    a->q = static_cast<const char*>(x->d_q);
+    a->k = static_cast<const char*>(x->d_k);
+    a->v = static_cast<const char*>(x->d_v);
+    a->q_row = (uint32_t)(2 * x->q_row), a->q_head = (uint32_t)(2 * x->q_head);
+    a->k_row = (uint32_t)(2 * x->k_row), a->k_head = (uint32_t)(2 * x->k_head);
+    a->v_row = (uint32_t)(2 * x->v_row), a->v_head = (uint32_t)(2 * x->v_head);
+    a->q_off = x->d_q_off, a->k_off = x->d_k_off;
+    a->n_seqs = (int32_t)x->n_seqs, a->n_q = (int32_t)x->n_q, a->n_k = (int32_t)x->n_k;
+    a->heads = x->heads, a->kv_heads = x->kv_heads, a->dim = x->dim;
+    a->causal = x->causal;
+    a->scale = x->scale;
+    a->bias = x->d_bias, a->bucket = x->d_bucket;
+    a->n_buckets = x->d_bias ? x->n_buckets : 0;
+    a->reach = x->d_bias ? x->reach : 0;
+    a->err = ctx->d_err;
+    return SUREL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_out, float* d_lse) {
+    surel::AttentionArgs a;
+    if (int rc = attention_args(ctx, args, &a)) return rc;
+    if (a.n_q > 0 && (!d_out || !d_lse)) return SUREL_E_NULL;
+    if (misaligned16(d_out)) return SUREL_E_RANGE;
+    if (a.n_q == 0) return SUREL_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SUREL_E_HIP;
+    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::attention_scratch_bytes(ctx->n_cu, a)))
+        return rc;
+    KernelSpan span(ctx, SUREL_K_ATTENTION);
+    if (surel::launch_attention(ctx->stream, ctx->n_cu, a, args->type == SUREL_FP16, d_out, d_lse, ctx->d_model) !=
+        hipSuccess)
+        return SUREL_E_HIP;
+    return SUREL_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,127 @@
+// What the attention kernels share: how a call's tensors lie, and which rows meet.
+#pragma once
+
+#include "matrix_tile.h"
+
+namespace surel {
+
+struct AttentionArgs {
+    const char *q = nullptr, *k = nullptr, *v = nullptr;
+    uint32_t q_row = 0, q_head = 0, k_row = 0, k_head = 0, v_row = 0, v_head = 0;  // bytes
+    const int64_t *q_off = nullptr, *k_off = nullptr;
+    int32_t n_seqs = 0, n_q = 0, n_k = 0;
+    int32_t heads = 0, kv_heads = 0, dim = 0;
+    int32_t causal = 0;
+    float scale = 0.f;            // of q . k
+    const void* bias = nullptr;   // [n_buckets][heads] or null
+    const int32_t* bucket = nullptr;
+    int32_t n_buckets = 0, reach = 0;
+    uint32_t* err = nullptr;
+};
+
+// The rows of a sequence's part of `off` that hold row t: the last s with off[s] <= t.  Looks around the
+// place where equally long sequences have it, in steps that double, then halves what is left: one load where
+// they are equally long.
+__device__ __forceinline__ int segment_of(const int64_t* __restrict__ off, int n, int64_t total, int64_t t) {
+    int lo = total > 0 ? (int)((double)t * (double)n / (double)total) : 0;
+    lo = min(max(lo, 0), n - 1);
+    int hi, step = 1;
+    if (off[lo] <= t) {
+        hi = lo + 1;
+        while (hi < n && off[hi] <= t) {
+            lo = hi;
+            hi = min(hi + step, n);
+            step = min(2 * step, 1 << 29);
+        }
+        hi = min(hi, n);
+    } else {
+        hi = lo;
+        lo = max(hi - 1, 0);
+        while (lo > 0 && off[lo] > t) {
+            hi = lo;
+            lo = max(lo - step, 0);
+            step = min(2 * step, 1 << 29);
+        }
+    }
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (off[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// A sequence's query rows and keys.  Offsets that do not lie in order inside the tensors make it
+// empty and raise kDevBadOffsets.
+struct Sequence {
+    int q0, q1, k0, k1;
+};
+__device__ __forceinline__ Sequence sequence_at(const AttentionArgs& a, int s) {
+    const int64_t q0 = a.q_off[s], q1 = a.q_off[s + 1], k0 = a.k_off[s], k1 = a.k_off[s + 1];
+    if (q0 < 0 || q1 < q0 || q1 > a.n_q || k0 < 0 || k1 < k0 || k1 > a.n_k) {
+        atomicOr(a.err, kDevBadOffsets);
+        return Sequence{0, 0, 0, 0};
+    }
+    return Sequence{(int)q0, (int)q1, (int)k0, (int)k1};
+}
+
+// Where the last row or key is in no sequence, or the first; one thread of a launch looks.
+__device__ __forceinline__ void check_ends(const AttentionArgs& a) {
+    if (a.q_off[0] != 0 || a.q_off[a.n_seqs] != a.n_q || a.k_off[0] != 0 || a.k_off[a.n_seqs] != a.n_k)
+        atomicOr(a.err, kDevBadOffsets);
+}
+
+// Rows of packed sequences in tiles of `rows`: tile by tile through everything (`across`), or each
+// sequence in tiles of its own.  Sequence s then has the tiles from off[s] / rows + s on: as many numbers as it
+// may need, and at most one too many, without a sum over the sequences before it.
+struct TileOfRows {
+    int first, last;  // rows
+    int seq;          // or -1: of several
+};
+__device__ __forceinline__ TileOfRows tile_of_rows(const int64_t* __restrict__ off, int n, int total, int rows,
+                                                   bool across, int tile) {
+    if (across) return TileOfRows{min(tile * rows, total), (int)min((int64_t)(tile + 1) * rows, (int64_t)total), -1};
+    // the last s with off[s] / rows + s <= tile
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        // (a wave's lanes could look at 64 places at once; with the 13 steps of 8,192 sequences in the caches
+        // this is not what a tile waits for)
+        const int mid = lo + (hi - lo) / 2;
+        if (off[mid] / rows + mid <= tile) lo = mid;
+        else hi = mid;
+    }
+    int64_t r0 = off[lo], r1 = off[lo + 1];
+    if (r0 < 0 || r1 < r0 || r1 > total) return TileOfRows{0, 0, lo};
+    const int64_t at = r0 + (tile - (r0 / rows + lo)) * rows;
+    if (at < r0 || at >= r1) return TileOfRows{0, 0, lo};
+    return TileOfRows{(int)at, (int)min(at + rows, r1), lo};
+}
+inline int64_t tiles_of_rows(int64_t n, int64_t total, int64_t rows, bool across) {
+    return across ? (total + rows - 1) / rows : total / rows + n;
+}
+
+// A bucket's bias, in units of log 2, for every distance -reach .. reach of one head.
+template <class T>
+__device__ __forceinline__ void fill_bias(float* table, const AttentionArgs& a, int head, int tid, int threads) {
+    for (int d = tid; d < 2 * a.reach + 1; d += threads) {
+        int b = a.bucket[d];
+        if (b < 0 || b >= a.n_buckets) {
+            atomicOr(a.err, kDevBadBucket);
+            b = 0;
+        }
+        table[d] = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head] * kLog2e;
+    }
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) x = min(x, __shfl_xor(x, m));
+    return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) x = max(x, __shfl_xor(x, m));
+    return x;
+}
+
+}  // namespace surel

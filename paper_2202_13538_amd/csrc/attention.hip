@@ -1,0 +1,407 @@
+// Attention of packed query rows to packed keys (surel_attention).
+#include "attention.h"
+#include "kernels.h"
+
+namespace surel {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kSlack = 8.f;  // see the running maximum below
+
+struct AttentionOut {
+    void* out = nullptr;        // [n_q][heads][dim]
+    float* lse = nullptr;       // [n_q][heads]
+    float* part_o = nullptr;    // splits > 1: [split][n_q][heads][dim], not divided by the sum
+    float* part_ml = nullptr;   //             [split][n_q][heads][2]: maximum (base 2), sum
+    int splits = 1;
+    int pack = 1;               // heads of a group that share a tile
+    int across = 0;
+};
+
+template <int DP, int WR>
+struct ForwardShape {
+    static constexpr int WK = 4 / WR;
+    static constexpr int kKeys = WK == 1 ? 64 : 32;  // keys that a wave takes at a time
+    static constexpr int kTileKeys = kKeys * WK;
+    static constexpr int kBuffers = 2;
+    static constexpr int kTileBytes = kTileKeys * Tile<DP>::kRowBytes;
+    static constexpr int kLds = 2 * kBuffers * kTileBytes;
+};
+
+// One workgroup: 32 WR rows of queries, a row being a token and one of `pack` heads of a group, against
+// the keys that any of them sees.  The keys stream through LDS, 64 at a time; a wave holds its 32 query
+// rows in registers and computes scores^T = K q^T, so that a row's scores lie in one lane and its partner, the
+// softmax runs inside lanes, and the weights are the operand of out^T += V^T p^T as they come.
+//   WR = 4: four waves, 128 rows, all waves take every key tile.
+//   WR = 1: 32 rows (single tokens, a pooling row a set); the four waves take different keys of a tile of 128
+//           and join their sums at the end.
+template <class T, int DP, int WR>
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionArgs a, AttentionOut o) {
+    using Shape = ForwardShape<DP, WR>;
+    constexpr int WK = Shape::WK, kBlocks = Shape::kKeys / 32, NB = DP / 32;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int range[2][4];
+    char* const k_tile = lds;
+    char* const v_tile = lds + Shape::kBuffers * Shape::kTileBytes;
+    float* const bias = reinterpret_cast<float*>(lds + Shape::kLds);
+
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int wr = WR == 1 ? 0 : wave, wk = WR == 1 ? wave : 0;
+    const int n_head_tiles = a.heads / o.pack;
+    int block = blockIdx.x;
+    const int head0 = block % n_head_tiles * o.pack;
+    block /= n_head_tiles;
+    const int split = block % o.splits;
+    block /= o.splits;
+    const int n_tiles = gridDim.x / (n_head_tiles * o.splits);
+    if (blockIdx.x == 0 && tid == 0) check_ends(a);
+    // a causal sequence's last rows see the most keys: they come first
+    const int tile_no = a.causal ? n_tiles - 1 - block : block;
+    const int tokens = 32 * WR / o.pack;
+    const TileOfRows tile = tile_of_rows(a.q_off, a.n_seqs, a.n_q, tokens, o.across, tile_no);
+    if (tile.first >= tile.last) return;
+
+    // the lane's row, and the keys that it sees: lo <= key < hi; `diag` is the key that it stands at
+    const int row = 32 * wr + col;
+    const int token = tile.first + row / o.pack, head = head0 + row % o.pack;
+    const bool counts = token < tile.last && row < tokens * o.pack;
+    int lo = 0, hi = 0x7FFFFFFF, diag = 0;
+    if (counts) {
+        const int s = tile.seq >= 0 ? tile.seq : segment_of(a.q_off, a.n_seqs, a.n_q, token);
+        const Sequence seq = sequence_at(a, s);
+        diag = seq.k1 - (seq.q1 - token);
+        lo = seq.k0;
+        hi = a.causal ? min(seq.k1, diag + 1) : seq.k1;
+        if (hi <= lo || token < seq.q0 || token >= seq.q1) lo = hi = 0;
+    }
+    const bool sees = counts && hi > lo;
+    const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
+    const int all_lo = wave_max(lo), all_hi = wave_min(hi);   // every row sees what lies between
+    const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x7FFFFFFF);
+    int tile_lo = wave_lo, tile_hi = wave_hi;
+    if (WR > 1) {
+        if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) tile_lo = min(tile_lo, range[0][w]), tile_hi = max(tile_hi, range[1][w]);
+    }
+    int key_begin = tile_lo, key_end = tile_hi;
+    if (o.splits > 1 && tile_hi > tile_lo) {
+        const int n = (tile_hi - tile_lo + Shape::kTileKeys - 1) / Shape::kTileKeys;
+        const int each = (n + o.splits - 1) / o.splits * Shape::kTileKeys;
+        key_begin = (int)min((int64_t)tile_lo + (int64_t)split * each, (int64_t)tile_hi);
+        key_end = (int)min((int64_t)key_begin + each, (int64_t)tile_hi);
+    }
+
+    Stationary<DP> q;
+    q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
+    const float c = a.scale * kLog2e;   // scores in units of log 2
+    const int width = 2 * a.reach + 1;
+    if (a.bias != nullptr)
+        for (int p = 0; p < o.pack; ++p) fill_bias<T>(bias + p * width, a, head0 + p, tid, kThreads);
+    const float* const my_bias = bias + (row % o.pack) * width;
+    __syncthreads();
+    float bias_behind = 0.f, bias_ahead = 0.f;
+    if (a.bias != nullptr) bias_behind = my_bias[0], bias_ahead = my_bias[2 * a.reach];
+
+    const int kv_head = head0 / (a.heads / a.kv_heads);
+    const char* const k_src = a.k + (int64_t)kv_head * a.k_head;
+    const char* const v_src = a.v + (int64_t)kv_head * a.v_head;
+    f32x16 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+    float top = -INFINITY, sum = 0.f;
+
+    auto fetch = [&](int key, int buffer) {
+        const int rows = key_end - key;
+        copy_tile<DP, Shape::kTileKeys, kThreads>(k_tile + buffer * Shape::kTileBytes, k_src + (int64_t)key * a.k_row,
+                                                  a.k_row, rows, a.dim, tid);
+        copy_tile<DP, Shape::kTileKeys, kThreads>(v_tile + buffer * Shape::kTileBytes, v_src + (int64_t)key * a.v_row,
+                                                  a.v_row, rows, a.dim, tid);
+    };
+    // The maximum that weights are taken relative to may lag by 2^8: 32-bit sums and 16-bit floats (of at
+    // most 256 here) are as exact at that size, and most tiles need no rescaling.
+    auto raise_top = [&](float most) {
+        if (__any(most > top + kSlack)) {
+            const float now = fmaxf(top, most);
+            const float shrink = now == top ? 1.f : exp2_fast(top - now);
+            top = now;
+            sum *= shrink;
+#pragma unroll
+            for (int db = 0; db < NB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] *= shrink;
+        }
+    };
+    auto bias_at = [&](int key) {
+        return a.bias == nullptr ? 0.f : my_bias[min(max(key - diag, -a.reach), a.reach) + a.reach];
+    };
+
+    if (key_begin < key_end) fetch(key_begin, 0);
+    tile_arrived();
+    __syncthreads();
+    const int last = min(hi, key_end);
+    int buffer = 0;
+#pragma unroll 1
+    for (int key = key_begin; key < key_end; key += Shape::kTileKeys, buffer ^= 1) {
+        if (key + Shape::kTileKeys < key_end) fetch(key + Shape::kTileKeys, buffer ^ 1);
+        const int key0 = key + wk * Shape::kKeys;
+        if (key0 < min(wave_hi, key_end) && key0 + Shape::kKeys > wave_lo) {
+            const char* const kt = k_tile + buffer * Shape::kTileBytes + wk * Shape::kKeys * Tile<DP>::kRowBytes;
+            const char* const vt = v_tile + buffer * Shape::kTileBytes + wk * Shape::kKeys * Tile<DP>::kRowBytes;
+            f32x16 s[kBlocks];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) s[b] = scores<T, DP>(kt, 32 * b, q, lane);
+            const bool whole = key0 >= all_lo && key0 + Shape::kKeys <= min(all_hi, key_end);
+            const bool behind = key0 + Shape::kKeys - 1 - diag_min <= -a.reach, ahead = key0 - diag_max >= a.reach;
+            if (whole && (a.bias == nullptr || behind || ahead)) {
+                const float add = behind ? bias_behind : bias_ahead;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_fmaf(s[b][i], c, add);
+            } else {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = key0 + 32 * b + row_of(i, g);
+                        s[b][i] = j >= lo && j < last ? __builtin_fmaf(s[b][i], c, bias_at(j)) : -INFINITY;
+                    }
+            }
+            float most = s[0][0];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
+            raise_top(fmaxf(most, from_other_half(most)));
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[b][i] = exp2_fast(s[b][i] - base);
+                    sum += s[b][i];
+                }
+            // (weights are rounded to the inputs' 16 bits for the second product, the sum is of the
+            // unrounded ones)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) accumulate<T, DP>(acc, vt, 32 * b, s[b], lane);
+        }
+        tile_arrived();
+        __syncthreads();
+    }
+    sum += from_other_half(sum);
+    if (__any(has_nan(acc))) {   // once more, without what a row does not see
+#pragma unroll
+        for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+        top = -INFINITY;
+        sum = 0.f;
+#pragma unroll 1
+        for (int j = max(key_begin, wave_lo) + wk; j < min(key_end, wave_hi); j += WK) {
+            const float dot = dot_row<T, DP>(q, k_src + (int64_t)j * a.k_row, a.dim, lane);
+            const bool seen = j >= lo && j < last;
+            const float x = seen ? __builtin_fmaf(dot, c, bias_at(j)) : -INFINITY;
+            raise_top(x);
+            if (seen) {
+                const float w = exp2_fast(x - (top == -INFINITY ? 0.f : top));
+                sum += w;
+                accumulate_row<T, DP>(acc, v_src + (int64_t)j * a.v_row, w, a.dim, g);
+            }
+        }
+    }
+
+
+    if (WK > 1) {   // the waves' sums: 2 and 3 to 0 and 1, then 1 to 0
+        float* const ml = reinterpret_cast<float*>(lds);            // [2][64]
+        float* const sums = ml + 2 * 64;                            // [2][NB * 16][64]
+#pragma unroll 1
+        for (int half = 2; half >= 1; half >>= 1) {
+            if (wave >= half && wave < 2 * half) {
+                const int at = wave - half;
+                if (g == 0) ml[at * 64 + col] = top, ml[at * 64 + 32 + col] = sum;
+#pragma unroll
+                for (int db = 0; db < NB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[(at * NB * 16 + db * 16 + i) * 64 + lane] = acc[db][i];
+            }
+            __syncthreads();
+            if (wave < half) {
+                const float other = ml[wave * 64 + col], other_sum = ml[wave * 64 + 32 + col];
+                const float now = fmaxf(top, other), base = now == -INFINITY ? 0.f : now;
+                const float mine = now == top ? 1.f : exp2_fast(top - base);
+                const float theirs = now == other ? 1.f : exp2_fast(other - base);
+                top = now;
+                sum = sum * mine + other_sum * theirs;
+#pragma unroll
+                for (int db = 0; db < NB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        acc[db][i] = acc[db][i] * mine + sums[(wave * NB * 16 + db * 16 + i) * 64 + lane] * theirs;
+            }
+            __syncthreads();
+        }
+        if (wave != 0) return;
+    }
+
+    const int64_t at = (int64_t)token * a.heads + head;
+    if (o.splits > 1) {
+        if (!counts) return;
+        const int64_t part = (int64_t)split * a.n_q * a.heads + at;
+        if (g == 0) o.part_ml[2 * part] = top, o.part_ml[2 * part + 1] = sum;
+        float* const dst = o.part_o + part * a.dim;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * db + row_of(i, g);
+                if (d < a.dim)   // dim is a multiple of 8, d of 4
+                    *reinterpret_cast<f32x4*>(dst + d) = f32x4{acc[db][i], acc[db][i + 1], acc[db][i + 2], acc[db][i + 3]};
+            }
+        return;
+    }
+    if (counts && g == 0) o.lse[at] = sees ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
+    const float scale = sees ? 1.f / sum : 0.f;
+    // through the wave's own part of LDS (nobody reads tiles any more), so that rows go out in whole lines
+    char* const mine = lds + wr * 32 * Tile<DP>::kRowBytes;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = 32 * db + row_of(i, g);
+            const u32x2 w = {pack2<T>(sees ? acc[db][i] * scale : 0.f, sees ? acc[db][i + 1] * scale : 0.f),
+                             pack2<T>(sees ? acc[db][i + 2] * scale : 0.f, sees ? acc[db][i + 3] * scale : 0.f)};
+            *reinterpret_cast<u32x2*>(mine + col * Tile<DP>::kRowBytes + (((d >> 3) ^ Tile<DP>::permuted(col)) * 16) +
+                                      (d & 4) * 2) = w;
+        }
+    wave_sync();
+#pragma unroll
+    for (int n = 0; n < 32 * (DP / 8) / 64; ++n) {
+        const int id = lane + 64 * n, r = id / (DP / 8), ch = id % (DP / 8);
+        const int row_there = 32 * wr + r, token_there = tile.first + row_there / o.pack;
+        if (token_there < tile.last && row_there < tokens * o.pack && ch * 8 < a.dim) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(mine + r * Tile<DP>::kRowBytes + ((ch ^ Tile<DP>::permuted(r)) * 16));
+            char* const dst = static_cast<char*>(o.out) +
+                              (((int64_t)token_there * a.heads + head0 + row_there % o.pack) * a.dim + ch * 8) * 2;
+            *reinterpret_cast<u32x4*>(dst) = w;
+        }
+    }
+}
+
+// One wave a row: the parts of a row whose keys went to several workgroups.
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionOut o, int64_t n_rows, int dim) {
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= n_rows) return;
+    float top = -INFINITY;
+    for (int s = 0; s < o.splits; ++s) top = fmaxf(top, o.part_ml[2 * (s * n_rows + row)]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, x[2] = {0.f, 0.f};
+    for (int s = 0; s < o.splits; ++s) {
+        const int64_t part = s * n_rows + row;
+        const float m = o.part_ml[2 * part], w = m == top ? 1.f : exp2_fast(m - base);
+        if (m == -INFINITY && top != -INFINITY) continue;   // saw nothing
+        sum += w * o.part_ml[2 * part + 1];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (2 * lane + e < dim) x[e] += w * o.part_o[part * dim + 2 * lane + e];
+    }
+    // (a sum of zero: the row sees no key at all)
+    if (lane == 0) o.lse[row] = sum == 0.f ? -INFINITY : (top + log2_fast(sum)) * kLn2;
+    const float scale = sum == 0.f ? 0.f : 1.f / sum;
+    if (2 * lane < dim)
+        static_cast<uint32_t*>(o.out)[row * (dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
+}
+
+struct ForwardPlan {
+    int rows = 128, pack = 1, splits = 1;
+    bool across = false;
+    int64_t tiles = 0;
+};
+
+// How rows are put into tiles, and whether keys are split over workgroups, from the means of the lengths
+// (which are all that the host knows).
+ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
+    ForwardPlan p;
+    const int group = a.heads / a.kv_heads;
+    const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
+    // the bias of every head of a tile lies in LDS: 32 KB of it at most
+    auto fits = [&](int pack) { return a.bias == nullptr || pack == 1 || (int64_t)pack * (2 * a.reach + 1) * 4 <= 32768; };
+    p.across = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q;
+    if (!p.across) {
+        for (int d = 1; d <= group && d <= 32; ++d)
+            if (group % d == 0 && fits(d) && mean_q * d <= 32) p.rows = 32, p.pack = d;
+        if (p.rows == 128)
+            for (int d = group; d >= 1; --d)
+                if (group % d == 0 && d <= 128 && fits(d) && (mean_q * d >= 128 || p.pack == 1 || d > p.pack)) p.pack = d;
+    }
+    const int64_t heads = a.heads / p.pack;
+    p.tiles = tiles_of_rows(a.n_seqs, a.n_q, p.rows / p.pack, p.across);
+    const double full = p.across ? (double)p.tiles : a.n_seqs * ceil(mean_q * p.pack / p.rows);
+    const double blocks = full * heads;
+    if (blocks < 2 * n_cu) {
+        const double most = mean_k / (p.rows == 32 ? 256 : 256);
+        p.splits = (int)fmax(1.0, fmin(fmin(ceil(2.0 * n_cu / blocks), most), 128.0));
+    }
+    return p;
+}
+
+template <class T, int DP, int WR>
+hipError_t launch(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int64_t blocks) {
+    const size_t bytes = ForwardShape<DP, WR>::kLds +
+                         (a.bias != nullptr ? (size_t)o.pack * (2 * a.reach + 1) * sizeof(float) : 0);
+    auto kernel = attention_kernel<T, DP, WR>;
+    if (bytes > 65536) {
+        const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (rc != hipSuccess) return rc;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, a, o);
+    return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t launch_rows(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int rows, int64_t blocks) {
+    return rows == 32 ? launch<T, DP, 1>(stream, a, o, blocks) : launch<T, DP, 4>(stream, a, o, blocks);
+}
+
+template <class T>
+hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, const ForwardPlan& p) {
+    const int64_t blocks = p.tiles * (a.heads / p.pack) * p.splits;
+    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    hipError_t rc = a.dim <= 32   ? launch_rows<T, 32>(stream, a, o, p.rows, blocks)
+                    : a.dim <= 64 ? launch_rows<T, 64>(stream, a, o, p.rows, blocks)
+                    : a.dim <= 96 ? launch_rows<T, 96>(stream, a, o, p.rows, blocks)
+                                  : launch_rows<T, 128>(stream, a, o, p.rows, blocks);
+    if (rc != hipSuccess || p.splits == 1) return rc;
+    const int64_t n_rows = (int64_t)a.n_q * a.heads;
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((n_rows + 3) / 4)), dim3(kThreads), 0, stream, o,
+                       n_rows, a.dim);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attention_scratch_bytes(int n_cu, const AttentionArgs& a) {
+    const ForwardPlan p = forward_plan(a, n_cu);
+    return p.splits == 1 ? 0 : (size_t)p.splits * a.n_q * a.heads * (a.dim + 2) * sizeof(float);
+}
+
+hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, void* out, float* lse,
+                            void* scratch) {
+    const ForwardPlan p = forward_plan(a, n_cu);
+    AttentionOut o;
+    o.out = out;
+    o.lse = lse;
+    o.splits = p.splits;
+    o.pack = p.pack;
+    o.across = p.across;
+    if (p.splits > 1) {
+        o.part_o = static_cast<float*>(scratch);
+        o.part_ml = o.part_o + (int64_t)p.splits * a.n_q * a.heads * a.dim;
+    }
+    return half ? launch_type<Fp16>(stream, a, o, p) : launch_type<Bf16>(stream, a, o, p);
+}
+
+}  // namespace surel

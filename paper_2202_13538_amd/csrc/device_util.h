@@ -18,6 +18,9 @@ constexpr uint32_t kDevCapacity = 0x20u;
 constexpr uint32_t kDevBadTable = 0x40u;
 constexpr uint32_t kDevBadSizes = 0x80u;
 constexpr uint32_t kDevStall = 0x100u;
+constexpr uint32_t kDevBadOffsets = 0x200u;
+constexpr uint32_t kDevBadBucket = 0x400u;
+constexpr uint32_t kDevBadLabel = 0x800u;
 
 __device__ __forceinline__ int lane_id() {
     return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));

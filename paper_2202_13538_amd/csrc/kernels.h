@@ -203,4 +203,11 @@ hipError_t launch_exclusive_scan(hipStream_t stream, int n_cu, const int32_t* co
                                  int64_t* off, int64_t* partials, void* small_scan,
                                  uint32_t spin_limit);
 
+// attention.hip.  scratch: attention_scratch_bytes of device memory (0 where no keys are split).  half: fp16
+// instead of bf16.  Needs a.n_q >= 1 and a.n_seqs >= 1.
+struct AttentionArgs;
+size_t attention_scratch_bytes(int n_cu, const AttentionArgs& a);
+hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, void* out, float* lse,
+                            void* scratch);
+
 }  // namespace surel
