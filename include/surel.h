@@ -17,8 +17,8 @@
  * surel_join_query_ids (the union join over those RPE-IDs), and
  * surel_query_incidence + surel_bfs_batches (Sec. 3.6 "Mini-batching for Training";
  * Algorithm 2: mini-batches of queries that share nodes, by breadth-first search).
- * Behind them, for a model that reads walks or joined sets: surel_attention (rows packed with the
- * offsets that the join and the RPE table are laid out by).
+ * Behind them, for a model that reads walks or joined sets: surel_attention and
+ * surel_attention_grad (rows packed with the offsets that the join and the RPE table are laid out by).
  *
  * Conventions
  *   - Plain C ABI.  Pointers named d_* are DEVICE memory owned by the caller, on the
@@ -138,7 +138,8 @@ extern "C" {
 #define SUREL_K_PRUNE       9   /* surel_prune_rpe (all its launches)                 */
 #define SUREL_K_BATCH       10  /* surel_query_incidence and surel_bfs_batches        */
 #define SUREL_K_ATTENTION   11  /* surel_attention                                    */
-#define SUREL_K_COUNT       12
+#define SUREL_K_ATTENTION_GRAD 12 /* surel_attention_grad (all its launches)           */
+#define SUREL_K_COUNT       13
 
 /* 16-bit element types of a model's tensors */
 #define SUREL_BF16          0
@@ -467,6 +468,21 @@ typedef struct surel_attention_args {
  * by 4 (dim + 2) bytes a row, head and part (128 parts at most).  Results are the same every time.
  * Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
 int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_out, float* d_lse);
+
+/* The gradients of surel_attention for one gradient of its d_out (d_lse is taken to have none).
+ *   d_dout           [n_q][heads][dim] of `type`, dense (device, read-only).
+ *   d_out, d_lse     what surel_attention wrote for these arguments (device, read-only).
+ *   d_dq             [n_q][heads][dim], d_dk and d_dv [n_k][kv_heads][dim], of `type`, dense
+ *                    (device, written): sums over all that read a row, heads of a group among them.
+ *   d_dbias          [n_buckets][heads] of `type` (device, written) if there is a bias, else NULL.
+ * d_dout, d_out, d_dq, d_dk and d_dv start on 16-byte boundaries.  All sums are 32-bit; weights and score
+ * gradients are rounded to `type` for their products (fp16: score gradients scaled by a power of two that
+ * brings the largest |d_dout| below 1), results once more.  A query row that sees no key, and a
+ * key that no row sees, get zeros.  The context's workspace grows by 8 bytes a row and head, and with a bias by
+ * 4 (2 reach + 1) bytes a head and tile of 128 rows (as many tiles more as there are sequences).  Results are
+ * the same every time.  Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
+int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
+                         const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias);
 
 /* Every wait inside the fused kernel of surel_sample_walks_rpe and surel_sample_walks_rpe_ids (a
  * wave waiting for an offset, the offset scan waiting for a row count) and inside the pruning (a

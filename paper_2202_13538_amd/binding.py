@@ -28,12 +28,13 @@ NOALLOC_MAX_QUERIES = 1 << 20
 BF16, FP16 = 0, 1
 
 (K_WALK, K_RPE_COUNT, K_RPE_FILL, K_JOIN_COUNT, K_JOIN_FILL, K_SCAN, K_WALK_RPE,
- K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_ATTENTION, K_COUNT) = range(13)
+ K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_ATTENTION,
+ K_ATTENTION_GRAD, K_COUNT) = range(14)
 KERNEL_NAMES = {K_WALK: "walk", K_RPE_COUNT: "rpe_count", K_RPE_FILL: "rpe_fill",
                 K_JOIN_COUNT: "join_count", K_JOIN_FILL: "join_fill", K_SCAN: "scan",
                 K_WALK_RPE: "walk_rpe", K_EDGE_RECORDS: "edge_records",
                 K_QUERY_IDS: "query_ids", K_PRUNE: "prune", K_BATCH: "batch",
-                K_ATTENTION: "attention"}
+                K_ATTENTION: "attention", K_ATTENTION_GRAD: "attention_grad"}
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
@@ -87,6 +88,7 @@ SIGNATURES = {
     "surel_bfs_batches": (ctypes.c_int, [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _i64, _i32,
                                          _i32, _i32, _vp, _vp, _vp, _vp]),
     "surel_attention": (ctypes.c_int, [_vp, ctypes.POINTER(AttentionArgs), _vp, _vp]),
+    "surel_attention_grad": (ctypes.c_int, [_vp, ctypes.POINTER(AttentionArgs)] + 7 * [_vp]),
     "surel_set_spin_limit": (ctypes.c_int, [_vp, ctypes.c_uint32]),
     "surel_check": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "surel_profile_enable": (ctypes.c_int, [_vp, ctypes.c_int]),
@@ -633,6 +635,29 @@ def attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     if rc != OK:
         raise SurelError(rc, "surel_attention")
     return out, lse
+
+
+def attention_grad(ctx: Context, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   out: torch.Tensor, lse: torch.Tensor, q_off: torch.Tensor,
+                   k_off: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
+                   bias: torch.Tensor | None = None, bucket: torch.Tensor | None = None):
+    """(dq, dk, dv, dbias or None) on the GPU for the gradient dout of attention's out; out and lse are what
+    attention returned, everything else what it was given.  Gradients have the shapes and the type of what
+    they belong to, and are dense."""
+    args = _attention_args(q, k, v, q_off, k_off, causal, scale, bias, bucket)
+    if dout.shape != q.shape or out.shape != q.shape or lse.shape != q.shape[:2]:
+        raise ValueError("dout and out must have q's shape, lse its first two dimensions")
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    dbias = None if bias is None else torch.empty(bias.shape, dtype=q.dtype, device=q.device)
+    rc = load().surel_attention_grad(
+        ctx.handle, ctypes.byref(args), _ptr(dout, q.dtype, "dout"), _ptr(out, q.dtype, "out"),
+        _ptr(lse, torch.float32, "lse"), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        None if dbias is None else dbias.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_attention_grad")
+    return dq, dk, dv, dbias
 
 
 def distance_buckets(reach: int, buckets: int, causal: bool = False) -> list[int]:

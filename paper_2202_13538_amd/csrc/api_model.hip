@@ -79,4 +79,30 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
     return SUREL_OK;
 }
 
+int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
+                         const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias) {
+    surel::AttentionArgs a;
+    if (int rc = attention_args(ctx, args, &a)) return rc;
+    if (a.n_q > 0 && (!d_dout || !d_out || !d_lse || !d_dq)) return SUREL_E_NULL;
+    if (a.n_k > 0 && (!d_dk || !d_dv)) return SUREL_E_NULL;
+    if ((a.bias == nullptr) != (d_dbias == nullptr)) return SUREL_E_NULL;
+    if (misaligned16(d_dout) || misaligned16(d_out) || misaligned16(d_dq) || misaligned16(d_dk) || misaligned16(d_dv))
+        return SUREL_E_RANGE;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SUREL_E_HIP;
+    if (a.n_q == 0 || a.n_k == 0) {   // nothing meets anything
+        hipError_t rc = surel::launch_zero(ctx->stream, d_dq, (int64_t)a.n_q * a.heads * a.dim);
+        if (rc == hipSuccess) rc = surel::launch_zero(ctx->stream, d_dk, (int64_t)a.n_k * a.kv_heads * a.dim);
+        if (rc == hipSuccess) rc = surel::launch_zero(ctx->stream, d_dv, (int64_t)a.n_k * a.kv_heads * a.dim);
+        if (rc == hipSuccess) rc = surel::launch_zero(ctx->stream, d_dbias, (int64_t)a.n_buckets * a.heads);
+        return rc == hipSuccess ? SUREL_OK : SUREL_E_HIP;
+    }
+    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::attention_grad_scratch_bytes(a))) return rc;
+    KernelSpan span(ctx, SUREL_K_ATTENTION_GRAD);
+    if (surel::launch_attention_grad(ctx->stream, a, args->type == SUREL_FP16, d_dout, d_out, d_lse, d_dq, d_dk, d_dv,
+                                     d_dbias, ctx->d_model) != hipSuccess)
+        return SUREL_E_HIP;
+    return SUREL_OK;
+}
+
 }  // extern "C"

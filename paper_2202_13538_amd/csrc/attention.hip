@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionArgs a,
     const bool sees = counts && hi > lo;
     const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
     const int all_lo = wave_max(lo), all_hi = wave_min(hi);   // every row sees what lies between
-    const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x7FFFFFFF);
+    const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x3FFFFFFF);
     int tile_lo = wave_lo, tile_hi = wave_hi;
     if (WR > 1) {
         if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
@@ -262,30 +262,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionArgs a,
     }
     if (counts && g == 0) o.lse[at] = sees ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
     const float scale = sees ? 1.f / sum : 0.f;
-    // through the wave's own part of LDS (nobody reads tiles any more), so that rows go out in whole lines
-    char* const mine = lds + wr * 32 * Tile<DP>::kRowBytes;
-#pragma unroll
-    for (int db = 0; db < NB; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int d = 32 * db + row_of(i, g);
-            const u32x2 w = {pack2<T>(sees ? acc[db][i] * scale : 0.f, sees ? acc[db][i + 1] * scale : 0.f),
-                             pack2<T>(sees ? acc[db][i + 2] * scale : 0.f, sees ? acc[db][i + 3] * scale : 0.f)};
-            *reinterpret_cast<u32x2*>(mine + col * Tile<DP>::kRowBytes + (((d >> 3) ^ Tile<DP>::permuted(col)) * 16) +
-                                      (d & 4) * 2) = w;
-        }
-    wave_sync();
-#pragma unroll
-    for (int n = 0; n < 32 * (DP / 8) / 64; ++n) {
-        const int id = lane + 64 * n, r = id / (DP / 8), ch = id % (DP / 8);
+    store_rows<T, DP>(acc, scale, !sees, lds + wr * 32 * Tile<DP>::kRowBytes, a.dim, lane, [&](int r) -> char* {
         const int row_there = 32 * wr + r, token_there = tile.first + row_there / o.pack;
-        if (token_there < tile.last && row_there < tokens * o.pack && ch * 8 < a.dim) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(mine + r * Tile<DP>::kRowBytes + ((ch ^ Tile<DP>::permuted(r)) * 16));
-            char* const dst = static_cast<char*>(o.out) +
-                              (((int64_t)token_there * a.heads + head0 + row_there % o.pack) * a.dim + ch * 8) * 2;
-            *reinterpret_cast<u32x4*>(dst) = w;
-        }
-    }
+        if (token_there >= tile.last || row_there >= tokens * o.pack) return nullptr;
+        return static_cast<char*>(o.out) + ((int64_t)token_there * a.heads + head0 + row_there % o.pack) * a.dim * 2;
+    });
 }
 
 // One wave a row: the parts of a row whose keys went to several workgroups.

@@ -1,0 +1,575 @@
+// The gradients of attention (surel_attention_grad).
+//
+// With the weights p_ij = exp(s_ij - lse_i) of the forward pass, dp_ij = do_i . v_j and delta_i = do_i . o_i:
+//   dv_j = sum_i p_ij do_i        ds_ij = p_ij (dp_ij - delta_i)
+//   dq_i = scale sum_j ds_ij k_j  dk_j = scale sum_i ds_ij q_i   dbias_b = sum of ds_ij with distance in bucket b
+// Scores are made again from q and k.  Two kernels: one goes over the keys of a tile of query rows (dq), one
+// over the query rows of a tile of keys (dk, dv, dbias).  Each sum then lives in one workgroup's registers and is
+// the same every time; that costs the scores and dp a second time (7 products instead of 5), where one
+// kernel would add dq up in memory with atomics in whatever order its workgroups run.
+#include "attention.h"
+#include "kernels.h"
+
+namespace surel {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTileRows = 64;      // streamed rows of a tile
+constexpr int kChunksOfBias = 32;  // parts that the sums by distance are added up in
+
+struct GradArgs {
+    const char *dout = nullptr, *out = nullptr;  // [n_q][heads][dim]
+    const float* lse = nullptr;                  // [n_q][heads]
+    char *dq = nullptr, *dk = nullptr, *dv = nullptr;
+    void* dbias = nullptr;
+    float *lse2 = nullptr, *delta = nullptr;  // [heads][n_q]: lse in units of log 2
+    uint32_t* largest = nullptr;              // of |dout|, as a float's bits (fp16 only)
+    float* by_distance = nullptr;             // [heads][tiles][2 reach + 1]: ds of a tile of keys
+    float* by_part = nullptr;                 // [heads][kChunksOfBias][2 reach + 1]
+    int q_tiles = 0, k_tiles = 0;
+    int across_q = 0, across_k = 0;
+    int twice = 0;                            // delta from the weights themselves, see attention_dq_kernel
+};
+
+__global__ void clear_word_kernel(uint32_t* word) { *word = 0; }
+
+__global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* dst, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) dst[i] = 0;
+}
+
+// delta and lse by head, so that a tile's 64 rows lie behind one another.  16 lanes a row and head.
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(AttentionArgs a, GradArgs w) {
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    const int c = threadIdx.x & 15;
+    const bool counts = row < (int64_t)a.n_q * a.heads;
+    float sum = 0.f, most = 0.f;
+    if (counts && c * 8 < a.dim) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(w.dout + (row * a.dim + c * 8) * 2);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(w.out + (row * a.dim + c * 8) * 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x2 p = unpack2<T>(x[e]), q = unpack2<T>(y[e]);
+            sum = __builtin_fmaf(p[0], q[0], __builtin_fmaf(p[1], q[1], sum));
+            most = fmaxf(most, fmaxf(fabsf(p[0]), fabsf(p[1])));
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m);
+    if (counts && c == 0) {
+        const int64_t t = row / a.heads, at = (row % a.heads) * a.n_q + t;
+        w.delta[at] = sum;
+        w.lse2[at] = w.lse[row] * kLog2e;
+    }
+    if (T::kNarrow) {
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+        if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(w.largest, __float_as_uint(most));
+    }
+}
+
+// What ds is multiplied by before it is rounded to fp16, a power of two: the largest |dout| becomes
+// 1/2 .. 1, so that a loss's small gradients do not fall below what fp16 can hold.  bf16 has the range
+// of 32-bit floats.
+template <class T>
+__device__ __forceinline__ int lift_of(const GradArgs& w) {
+    if (!T::kNarrow) return 0;
+    const float most = __uint_as_float(*w.largest);
+    if (!(most > 0.f) || !(most < INFINITY)) return 0;
+    return min(max(-1 - ilogbf(most), -60), 60);
+}
+
+// dq of 128 query rows of one head, 32 a wave.
+//
+// delta_i = do_i . o_i comes from an o whose weights and results were rounded to 16 bits.  The sum of ds_ij over j
+// is what it is off by, since it should be zero; the row's delta in memory is corrected by that for dk and dbias.  dq
+// itself would need the keys' weighted sum as a fourth product.  With few keys a row the error is as
+// large as that of rounding ds, and the keys are there again at once: their ds are summed up in a round of
+// its own first (`twice`; walks of 16 steps, 262,144 rows of 8 heads of 64 elements: dq 0.0029 -> 0.0024 off).
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(AttentionArgs a, GradArgs w) {
+    constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int range[2][4];
+    char* const k_tile = lds;
+    char* const v_tile = lds + 2 * kTileBytes;
+    float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+
+    const int head = blockIdx.x % a.heads;
+    const int block = blockIdx.x / a.heads, tile_no = a.causal ? w.q_tiles - 1 - block : block;
+    if (blockIdx.x == 0 && tid == 0) check_ends(a);
+    const TileOfRows tile = tile_of_rows(a.q_off, a.n_seqs, a.n_q, 128, w.across_q, tile_no);
+    if (tile.first >= tile.last) return;
+    const int token = tile.first + 32 * wave + col;
+    const bool counts = token < tile.last;
+    int lo = 0, hi = 0x7FFFFFFF, diag = 0;
+    if (counts) {
+        const int s = tile.seq >= 0 ? tile.seq : segment_of(a.q_off, a.n_seqs, a.n_q, token);
+        const Sequence seq = sequence_at(a, s);
+        diag = seq.k1 - (seq.q1 - token);
+        lo = seq.k0;
+        hi = a.causal ? min(seq.k1, diag + 1) : seq.k1;
+        if (hi <= lo || token < seq.q0 || token >= seq.q1) lo = hi = 0;
+    }
+    const bool sees = counts && hi > lo;
+    const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
+    const int all_lo = wave_max(lo), all_hi = wave_min(hi);
+    const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x3FFFFFFF);
+    if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
+    if (a.bias != nullptr) fill_bias<T>(bias, a, head, tid, kThreads);
+    __syncthreads();
+    int key_begin = 0x7FFFFFFF, key_end = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key_begin = min(key_begin, range[0][i]), key_end = max(key_end, range[1][i]);
+
+    Stationary<DP> q, dout;
+    q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
+    dout.load(w.dout + ((int64_t)token * a.heads + head) * a.dim * 2, counts, a.dim, lane);
+    const float lse2 = counts ? w.lse2[(int64_t)head * a.n_q + token] : 0.f;
+    float delta = counts ? w.delta[(int64_t)head * a.n_q + token] : 0.f;
+    const int lift = lift_of<T>(w);
+    const float c = a.scale * kLog2e, base = lse2 - (float)lift;   // ds comes out lifted
+    float bias_behind = 0.f, bias_ahead = 0.f;
+    if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
+
+    const int kv_head = head / (a.heads / a.kv_heads);
+    const char* const k_src = a.k + (int64_t)kv_head * a.k_head;
+    const char* const v_src = a.v + (int64_t)kv_head * a.v_head;
+    auto fetch = [&](int key, int buffer) {
+        const int rows = key_end - key;
+        copy_tile<DP, kTileRows, kThreads>(k_tile + buffer * kTileBytes, k_src + (int64_t)key * a.k_row, a.k_row, rows, a.dim, tid);
+        copy_tile<DP, kTileRows, kThreads>(v_tile + buffer * kTileBytes, v_src + (int64_t)key * a.v_row, a.v_row, rows, a.dim, tid);
+    };
+    auto bias_at = [&](int key) { return a.bias == nullptr ? 0.f : bias[min(max(key - diag, -a.reach), a.reach) + a.reach]; };
+
+    f32x16 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+    float sum = 0.f;   // of ds
+#pragma unroll 1
+    for (int round = w.twice ? 0 : 1; round < 2; ++round) {
+        if (key_begin < key_end) fetch(key_begin, 0);
+        tile_arrived();
+        __syncthreads();
+        int buffer = 0;
+#pragma unroll 1
+        for (int key = key_begin; key < key_end; key += kTileRows, buffer ^= 1) {
+            if (key + kTileRows < key_end) fetch(key + kTileRows, buffer ^ 1);
+            const char* const kt = k_tile + buffer * kTileBytes;
+            const char* const vt = v_tile + buffer * kTileBytes;
+#pragma unroll
+            for (int b = 0; b < kTileRows; b += 32) {
+                const int key0 = key + b;
+                if (key0 >= wave_hi || key0 + 32 <= wave_lo) continue;
+                f32x16 s = scores<T, DP>(kt, b, q, lane);
+                const f32x16 dp = scores<T, DP>(vt, b, dout, lane);
+                const bool whole = key0 >= all_lo && key0 + 32 <= all_hi;
+                const bool behind = key0 + 31 - diag_min <= -a.reach, ahead = key0 - diag_max >= a.reach;
+                if (whole && (a.bias == nullptr || behind || ahead)) {
+                    const float add = (behind ? bias_behind : bias_ahead) - base;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], c, add)) * (dp[i] - delta);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = key0 + row_of(i, g);
+                        const float p = exp2_fast(__builtin_fmaf(s[i], c, bias_at(j) - base));
+                        s[i] = j >= lo && j < hi ? p * (dp[i] - delta) : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += s[i];
+                if (round == 1) accumulate<T, DP>(acc, kt, b, s, lane);   // (ds rounded to the inputs' 16 bits)
+            }
+            tile_arrived();
+            __syncthreads();
+        }
+        delta += ldexpf(sum + from_other_half(sum), -lift);
+        sum = 0.f;
+    }
+    if (sees && g == 0) w.delta[(int64_t)head * a.n_q + token] = delta;
+    if (__any(has_nan(acc))) {   // once more, without what a row does not see
+#pragma unroll
+        for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+#pragma unroll 1
+        for (int j = wave_lo; j < wave_hi; ++j) {
+            const float dot = dot_row<T, DP>(q, k_src + (int64_t)j * a.k_row, a.dim, lane);
+            const float dp = dot_row<T, DP>(dout, v_src + (int64_t)j * a.v_row, a.dim, lane);
+            if (j >= lo && j < hi)
+                accumulate_row<T, DP>(acc, k_src + (int64_t)j * a.k_row,
+                                      exp2_fast(__builtin_fmaf(dot, c, bias_at(j) - base)) * (dp - delta), a.dim, g);
+        }
+    }
+    store_rows<T, DP>(acc, ldexpf(a.scale, -lift), !sees, lds + wave * 32 * Tile<DP>::kRowBytes, a.dim, lane,
+                      [&](int r) -> char* {
+                          const int there = tile.first + 32 * wave + r;
+                          return there < tile.last ? w.dq + ((int64_t)there * a.heads + head) * a.dim * 2 : nullptr;
+                      });
+}
+
+// dk and dv of 128 keys of one key head, 32 a wave, over the query rows of all heads of its group, and the sums of
+// ds by distance.
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kernel(AttentionArgs a, GradArgs w) {
+    constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int range[2][4];
+    __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][lse, delta][row]
+    char* const q_tile = lds;
+    char* const o_tile = lds + 2 * kTileBytes;
+    const int width = 2 * a.reach + 1;
+    float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);   // [width], then the waves' sums [4][width]
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+
+    const int kv_head = blockIdx.x % a.kv_heads, tile_no = blockIdx.x / a.kv_heads;
+    const TileOfRows tile = tile_of_rows(a.k_off, a.n_seqs, a.n_k, 128, w.across_k, tile_no);
+    float* const sums = bias + (1 + wave) * width;
+    auto by_distance = [&](int head) { return w.by_distance + ((int64_t)head * w.k_tiles + tile_no) * width; };
+    const int group = a.heads / a.kv_heads;
+    if (tile.first >= tile.last) {
+        if (a.bias != nullptr)
+            for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
+                for (int d = tid; d < width; d += kThreads) by_distance(h)[d] = 0.f;
+        return;
+    }
+    // the lane's key, the query rows that see it (lo <= t < hi), and `place`: a row t is place - t away
+    const int key = tile.first + 32 * wave + col;
+    const bool counts = key < tile.last;
+    int lo = 0, hi = 0, place = 0;
+    if (counts) {
+        const int s = tile.seq >= 0 ? tile.seq : segment_of(a.k_off, a.n_seqs, a.n_k, key);
+        const Sequence seq = sequence_at(a, s);
+        place = key - seq.k1 + seq.q1;
+        hi = seq.q1;
+        lo = a.causal ? max(seq.q0, place) : seq.q0;
+        if (hi <= lo || key < seq.k0 || key >= seq.k1) lo = hi = 0;
+    }
+    const bool sees = counts && hi > lo;
+    const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
+    const int all_lo = wave_max(counts ? lo : 0), all_hi = wave_min(counts ? hi : 0x7FFFFFFF);
+    const int place_min = wave_min(counts ? place : 0x7FFFFFFF), place_max = wave_max(counts ? place : -0x3FFFFFFF);
+    if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
+    __syncthreads();
+    int row_begin = 0x7FFFFFFF, row_end = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row_begin = min(row_begin, range[0][i]), row_end = max(row_end, range[1][i]);
+
+    Stationary<DP> k, v;
+    k.load(a.k + (int64_t)key * a.k_row + (int64_t)kv_head * a.k_head, counts, a.dim, lane);
+    v.load(a.v + (int64_t)key * a.v_row + (int64_t)kv_head * a.v_head, counts, a.dim, lane);
+    const int lift = lift_of<T>(w);
+    const float c = a.scale * kLog2e, up = ldexpf(1.f, lift);
+
+    f32x16 dk[NB], dv[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) dk[db] = dv[db] = f32x16{};
+    if (row_begin < row_end) {
+#pragma unroll 1
+        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h) {
+            const char* const q_src = a.q + (int64_t)h * a.q_head;
+            const char* const o_src = w.dout + (int64_t)h * a.dim * 2;
+            const uint32_t o_row = (uint32_t)a.heads * a.dim * 2;
+            const float* const stat_src = (tid < kTileRows ? w.lse2 : w.delta) + (int64_t)h * a.n_q;
+            float stat = 0.f;
+            auto fetch = [&](int row, int buffer) {
+                const int rows = row_end - row;
+                copy_tile<DP, kTileRows, kThreads>(q_tile + buffer * kTileBytes, q_src + (int64_t)row * a.q_row, a.q_row, rows, a.dim, tid);
+                copy_tile<DP, kTileRows, kThreads>(o_tile + buffer * kTileBytes, o_src + (int64_t)row * o_row, o_row, rows, a.dim, tid);
+                if (tid < 2 * kTileRows) stat = stat_src[min(row + (tid & (kTileRows - 1)), row_end - 1)];
+            };
+            auto keep = [&](int buffer) {
+                if (tid < 2 * kTileRows) stats[buffer][tid / kTileRows][tid & (kTileRows - 1)] = stat;
+            };
+            fetch(row_begin, 0);
+            if (a.bias != nullptr) {
+                fill_bias<T>(bias, a, h, tid, kThreads);
+                for (int d = tid; d < 4 * width; d += kThreads) bias[width + d] = 0.f;
+            }
+            float sum_behind = 0.f, sum_ahead = 0.f;   // of ds, distances of reach and more
+            keep(0);
+            tile_arrived();
+            __syncthreads();
+            float bias_behind = 0.f, bias_ahead = 0.f;
+            if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
+            int buffer = 0;
+#pragma unroll 1
+            for (int row = row_begin; row < row_end; row += kTileRows, buffer ^= 1) {
+                const bool more = row + kTileRows < row_end;
+                if (more) fetch(row + kTileRows, buffer ^ 1);
+                const char* const qt = q_tile + buffer * kTileBytes;
+                const char* const ot = o_tile + buffer * kTileBytes;
+#pragma unroll
+                for (int b = 0; b < kTileRows; b += 32) {
+                    const int row0 = row + b;
+                    if (row0 >= wave_hi || row0 + 32 <= wave_lo) continue;
+                    f32x16 p = scores<T, DP>(qt, b, k, lane);
+                    f32x16 ds = scores<T, DP>(ot, b, v, lane);
+                    f32x4 lse2[4], delta[4];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        lse2[n] = *reinterpret_cast<const f32x4*>(&stats[buffer][0][b + 8 * n + 4 * g]);
+                        delta[n] = *reinterpret_cast<const f32x4*>(&stats[buffer][1][b + 8 * n + 4 * g]);
+                    }
+                    const bool whole = row0 >= all_lo && row0 + 32 <= all_hi;
+                    const bool behind = place_max - row0 <= -a.reach, ahead = place_min - (row0 + 31) >= a.reach;
+                    if (whole && (a.bias == nullptr || behind || ahead)) {
+                        const float add = behind ? bias_behind : bias_ahead;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            p[i] = exp2_fast(__builtin_fmaf(p[i], c, add - lse2[i >> 2][i & 3]));
+                            ds[i] = p[i] * (ds[i] - delta[i >> 2][i & 3]);
+                        }
+                        if (a.bias != nullptr) {
+                            float sum = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum += ds[i];
+                            if (behind) sum_behind += sum;
+                            else sum_ahead += sum;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int t = row0 + row_of(i, g);
+                            float add = 0.f;
+                            if (a.bias != nullptr) add = bias[min(max(place - t, -a.reach), a.reach) + a.reach];
+                            const bool seen = t >= lo && t < hi;
+                            p[i] = seen ? exp2_fast(__builtin_fmaf(p[i], c, add - lse2[i >> 2][i & 3])) : 0.f;
+                            ds[i] = seen ? p[i] * (ds[i] - delta[i >> 2][i & 3]) : 0.f;
+                        }
+                        if (a.bias != nullptr) {
+                            // a distance is met by one key of a half: a tile's keys lie at different places.  The
+                            // halves take turns, so no two lanes add to one place at a time, and the order is
+                            // fixed.
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                if (g == half && counts) {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) {
+                                        const int d = place - (row0 + row_of(i, g));
+                                        if (d <= -a.reach) sum_behind += ds[i];
+                                        else if (d >= a.reach) sum_ahead += ds[i];
+                                        else __hip_atomic_fetch_add(&sums[d + a.reach], ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                                    }
+                                }
+                                wave_sync();
+                            }
+                        }
+                    }
+                    if (T::kNarrow) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) ds[i] *= up;
+                    }
+                    accumulate<T, DP>(dv, ot, b, p, lane);    // (p and ds rounded to the inputs' 16 bits)
+                    accumulate<T, DP>(dk, qt, b, ds, lane);
+                }
+                if (more) keep(buffer ^ 1);
+                tile_arrived();
+                __syncthreads();
+            }
+            if (a.bias != nullptr) {
+                if (!counts) sum_behind = sum_ahead = 0.f;
+#pragma unroll
+                for (int m = 1; m < 64; m <<= 1) sum_behind += __shfl_xor(sum_behind, m), sum_ahead += __shfl_xor(sum_ahead, m);
+                if (lane == 0) {
+                    if (a.reach == 0) sums[0] = sum_behind + sum_ahead;
+                    else sums[0] = sum_behind, sums[2 * a.reach] = sum_ahead;
+                }
+                __syncthreads();
+                for (int d = tid; d < width; d += kThreads)
+                    by_distance(h)[d] = (bias[width + d] + bias[2 * width + d]) + (bias[3 * width + d] + bias[4 * width + d]);
+                __syncthreads();
+            }
+        }
+    } else if (a.bias != nullptr) {
+        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
+            for (int d = tid; d < width; d += kThreads) by_distance(h)[d] = 0.f;
+    }
+    if (__any(has_nan(dk) || has_nan(dv))) {   // once more, without rows that do not see the key
+#pragma unroll
+        for (int db = 0; db < NB; ++db) dk[db] = dv[db] = f32x16{};
+#pragma unroll 1
+        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
+#pragma unroll 1
+            for (int t = wave_lo; t < wave_hi; ++t) {
+                const char* const q_row = a.q + (int64_t)t * a.q_row + (int64_t)h * a.q_head;
+                const char* const o_row = w.dout + ((int64_t)t * a.heads + h) * a.dim * 2;
+                const float dot = dot_row<T, DP>(k, q_row, a.dim, lane), dp = dot_row<T, DP>(v, o_row, a.dim, lane);
+                if (t >= lo && t < hi) {
+                    float add = 0.f;
+                    if (a.bias != nullptr) {
+                        const int d = a.bucket[min(max(place - t, -a.reach), a.reach) + a.reach];
+                        const int b = d < 0 || d >= a.n_buckets ? 0 : d;
+                        add = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + h] * kLog2e;
+                    }
+                    const int64_t at = (int64_t)h * a.n_q + t;
+                    const float p = exp2_fast(__builtin_fmaf(dot, c, add - w.lse2[at]));
+                    accumulate_row<T, DP>(dv, o_row, p, a.dim, g);
+                    accumulate_row<T, DP>(dk, q_row, p * (dp - w.delta[at]) * up, a.dim, g);
+                }
+            }
+    }
+    auto row_of_key = [&](char* rows) {
+        return [=](int r) -> char* {
+            const int there = tile.first + 32 * wave + r;
+            return there < tile.last ? rows + ((int64_t)there * a.kv_heads + kv_head) * a.dim * 2 : nullptr;
+        };
+    };
+    char* const mine = lds + wave * 32 * Tile<DP>::kRowBytes;
+    store_rows<T, DP>(dk, ldexpf(a.scale, -lift), !sees, mine, a.dim, lane, row_of_key(w.dk));
+    store_rows<T, DP>(dv, 1.f, !sees, mine, a.dim, lane, row_of_key(w.dv));
+}
+
+// Sums by distance of a part of a head's tiles.
+__global__ __launch_bounds__(kThreads) void attention_dbias_parts_kernel(GradArgs w, int width) {
+    const int head = blockIdx.x / kChunksOfBias, part = blockIdx.x % kChunksOfBias;
+    const int each = (w.k_tiles + kChunksOfBias - 1) / kChunksOfBias;
+    const int first = min(part * each, w.k_tiles), last = min(first + each, w.k_tiles);
+    for (int d = threadIdx.x; d < width; d += kThreads) {
+        float sum = 0.f;
+        for (int t = first; t < last; ++t) sum += w.by_distance[((int64_t)head * w.k_tiles + t) * width + d];
+        w.by_part[((int64_t)head * kChunksOfBias + part) * width + d] = sum;
+    }
+}
+
+// A head's buckets: the parts of every distance, then the distances of every bucket, in order.
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_dbias_kernel(AttentionArgs a, GradArgs w) {
+    __shared__ float sums[2 * 1024 + 1];
+    __shared__ int bucket[2 * 1024 + 1];
+    const int width = 2 * a.reach + 1, head = blockIdx.x;
+    for (int d = threadIdx.x; d < width; d += kThreads) {
+        float sum = 0.f;
+        for (int p = 0; p < kChunksOfBias; ++p) sum += w.by_part[((int64_t)head * kChunksOfBias + p) * width + d];
+        sums[d] = sum;
+        const int b = a.bucket[d];
+        bucket[d] = b < 0 || b >= a.n_buckets ? 0 : b;
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < a.n_buckets; b += kThreads) {
+        float sum = 0.f;
+        for (int d = 0; d < width; ++d) sum += bucket[d] == b ? sums[d] : 0.f;
+        static_cast<typename T::elem*>(w.dbias)[(int64_t)b * a.heads + head] = (typename T::elem)sum;
+    }
+}
+
+struct GradPlan {
+    bool across_q, across_k, twice;
+    int64_t q_tiles, k_tiles;
+};
+GradPlan grad_plan(const AttentionArgs& a) {
+    GradPlan p;
+    const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
+    // Tiles across sequences where these are short and alike.  With a bias the keys of a tile have to lie at
+    // different places, which those of several sequences do only where queries and keys lie alike.
+    p.across_q = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q;
+    p.across_k = mean_k < 128 && mean_q <= 256 && mean_q <= 2 * mean_k && (a.bias == nullptr || a.q_off == a.k_off);
+    p.twice = mean_k <= 256;
+    p.q_tiles = tiles_of_rows(a.n_seqs, a.n_q, 128, p.across_q);
+    p.k_tiles = tiles_of_rows(a.n_seqs, a.n_k, 128, p.across_k);
+    return p;
+}
+
+size_t aligned(size_t x) { return (x + 255) / 256 * 256; }
+
+template <class T, int DP>
+hipError_t launch_width(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
+    const size_t tiles = 4 * (size_t)kTileRows * Tile<DP>::kRowBytes;
+    const size_t width = a.bias != nullptr ? 2 * (size_t)a.reach + 1 : 0;
+    auto allow = [](const void* kernel, size_t bytes) {
+        return bytes <= 65536 ? hipSuccess
+                              : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    };
+    {
+        const size_t bytes = tiles + width * sizeof(float);
+        hipError_t rc = allow(reinterpret_cast<const void*>(attention_dq_kernel<T, DP>), bytes);
+        if (rc != hipSuccess) return rc;
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP>), dim3((unsigned)(p.q_tiles * a.heads)), dim3(kThreads), bytes,
+                           stream, a, w);
+        if ((rc = hipGetLastError()) != hipSuccess) return rc;
+    }
+    {
+        const size_t bytes = tiles + 5 * width * sizeof(float);
+        hipError_t rc = allow(reinterpret_cast<const void*>(attention_dkv_kernel<T, DP>), bytes);
+        if (rc != hipSuccess) return rc;
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DP>), dim3((unsigned)(p.k_tiles * a.kv_heads)), dim3(kThreads), bytes,
+                           stream, a, w);
+        if ((rc = hipGetLastError()) != hipSuccess) return rc;
+    }
+    return hipSuccess;
+}
+
+template <class T>
+hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
+    if (p.q_tiles * a.heads > 0x7FFFFFFF || p.k_tiles * a.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const int64_t rows = (int64_t)a.n_q * a.heads;
+    if (T::kNarrow) hipLaunchKernelGGL(clear_word_kernel, dim3(1), dim3(1), 0, stream, w.largest);
+    hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)((rows + kThreads / 16 - 1) / (kThreads / 16))),
+                       dim3(kThreads), 0, stream, a, w);
+    hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    rc = a.dim <= 32   ? launch_width<T, 32>(stream, a, w, p)
+         : a.dim <= 64 ? launch_width<T, 64>(stream, a, w, p)
+         : a.dim <= 96 ? launch_width<T, 96>(stream, a, w, p)
+                       : launch_width<T, 128>(stream, a, w, p);
+    if (rc != hipSuccess || a.bias == nullptr) return rc;
+    hipLaunchKernelGGL(attention_dbias_parts_kernel, dim3((unsigned)(a.heads * kChunksOfBias)), dim3(kThreads), 0, stream, w,
+                       2 * a.reach + 1);
+    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)a.heads), dim3(kThreads), 0, stream, a, w);
+    return hipGetLastError();
+}
+
+// Where the parts of the scratch lie; returns its size.
+size_t lay_out(const AttentionArgs& a, const GradPlan& p, char* scratch, GradArgs* w) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* const here = scratch + at;
+        at += aligned(bytes);
+        return here;
+    };
+    const size_t rows = (size_t)a.n_q * a.heads * sizeof(float);
+    const size_t width = a.bias != nullptr ? (2 * (size_t)a.reach + 1) * sizeof(float) : 0;
+    w->lse2 = reinterpret_cast<float*>(take(rows));
+    w->delta = reinterpret_cast<float*>(take(rows));
+    w->largest = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+    w->by_distance = reinterpret_cast<float*>(take((size_t)p.k_tiles * a.heads * width));
+    w->by_part = reinterpret_cast<float*>(take((size_t)kChunksOfBias * a.heads * width));
+    return at;
+}
+
+}  // namespace
+
+hipError_t launch_zero(hipStream_t stream, void* dst, int64_t n) {
+    if (n <= 0) return hipSuccess;
+    const int64_t blocks = (n + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(kThreads), 0, stream,
+                       static_cast<uint16_t*>(dst), n);
+    return hipGetLastError();
+}
+
+size_t attention_grad_scratch_bytes(const AttentionArgs& a) {
+    GradArgs w;
+    return lay_out(a, grad_plan(a), nullptr, &w);
+}
+
+hipError_t launch_attention_grad(hipStream_t stream, const AttentionArgs& a, bool half, const void* dout, const void* out,
+                                 const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch) {
+    const GradPlan p = grad_plan(a);
+    GradArgs w;
+    lay_out(a, p, static_cast<char*>(scratch), &w);
+    w.dout = static_cast<const char*>(dout);
+    w.out = static_cast<const char*>(out);
+    w.lse = lse;
+    w.dq = static_cast<char*>(dq);
+    w.dk = static_cast<char*>(dk);
+    w.dv = static_cast<char*>(dv);
+    w.dbias = dbias;
+    w.q_tiles = (int)p.q_tiles;
+    w.k_tiles = (int)p.k_tiles;
+    w.across_q = p.across_q;
+    w.across_k = p.across_k;
+    w.twice = p.twice;
+    return half ? launch_type<Fp16>(stream, a, w, p) : launch_type<Bf16>(stream, a, w, p);
+}
+
+}  // namespace surel

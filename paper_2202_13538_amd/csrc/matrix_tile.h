@@ -220,6 +220,35 @@ __device__ __forceinline__ void accumulate_row(f32x16 (&acc)[DP / 32], const cha
         }
 }
 
+// Sums of 32 stationary rows, times `scale` (a lane's own), rounded and written as rows of 16-bit
+// elements.  They pass through 32 rows of LDS of the wave's own (of a tile that nobody reads any more), so that
+// rows go out 16 bytes a lane in whole lines.  dst_of(row) is where row `row` of the 32 goes, or null.
+template <class T, int DP, class Dst>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], float scale, bool zero, char* lds, int dim, int lane,
+                                           Dst dst_of) {
+    const int g = lane >> 5, col = lane & 31;
+    wave_sync();
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = 32 * db + row_of(i, g);
+            const u32x2 w = {pack2<T>(acc[db][i] * scale, acc[db][i + 1] * scale),
+                             pack2<T>(acc[db][i + 2] * scale, acc[db][i + 3] * scale)};
+            *reinterpret_cast<u32x2*>(lds + col * Tile<DP>::kRowBytes + (((d >> 3) ^ Tile<DP>::permuted(col)) * 16) +
+                                      (d & 4) * 2) = zero ? u32x2{0, 0} : w;
+        }
+    wave_sync();
+#pragma unroll
+    for (int n = 0; n < DP / 16; ++n) {
+        const int id = lane + 64 * n, r = id / Tile<DP>::kChunks, c = id % Tile<DP>::kChunks;
+        char* const dst = dst_of(r);
+        if (dst != nullptr && c * 8 < dim)
+            *reinterpret_cast<u32x4*>(dst + c * 16) =
+                *reinterpret_cast<const u32x4*>(lds + r * Tile<DP>::kRowBytes + ((c ^ Tile<DP>::permuted(r)) * 16));
+    }
+}
+
 template <int NB>
 __device__ __forceinline__ bool has_nan(const f32x16 (&acc)[NB]) {
     bool bad = false;

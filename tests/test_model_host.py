@@ -43,6 +43,29 @@ def test_attention_refuses(status, changes):
     assert lib.surel_attention(None, ctypes.byref(attention_args(**changes)), P, P) == status
 
 
+@pytest.mark.parametrize("status,changes", ATTENTION, ids=lambda x: str(x))
+def test_attention_grad_refuses(status, changes):
+    args = attention_args(**changes)
+    dbias = P if args.d_bias else None
+    assert binding.load().surel_attention_grad(None, ctypes.byref(args), P, P, P, P, P, P, dbias) == status
+
+
+def test_outputs_that_are_missing_or_off_their_boundary():
+    lib, plain = binding.load(), attention_args()
+    biased = attention_args(d_bias=P, d_bucket=P, n_buckets=3, reach=1)
+    fake = ctypes.create_string_buffer(4096)  # a context that is looked at only after these checks passed
+    call = lambda args, *p: lib.surel_attention(fake, ctypes.byref(args), *p)  # noqa: E731
+    assert call(plain, None, P) == call(plain, P, None) == binding.E_NULL
+    assert call(plain, P + 8, P) == binding.E_RANGE
+    call = lambda args, *p: lib.surel_attention_grad(fake, ctypes.byref(args), *p)  # noqa: E731
+    for missing in range(6):
+        assert call(plain, *[None if i == missing else P for i in range(6)], None) == binding.E_NULL
+    for off in (0, 1, 3, 4, 5):
+        assert call(plain, *[P + 8 if i == off else P for i in range(6)], None) == binding.E_RANGE
+    assert call(plain, *[P] * 7) == binding.E_NULL          # a gradient of a bias that is not there
+    assert call(biased, *[P] * 6, None) == binding.E_NULL
+
+
 def test_attention_refuses_no_arguments():
     assert binding.load().surel_attention(None, None, P, P) == binding.E_NULL
 
@@ -76,3 +99,27 @@ def test_distance_buckets_refuse():
     for bad in ((-1, 4, True), (4, 0, True), (4, 1, False)):
         with pytest.raises(ValueError):
             binding.distance_buckets(*bad)
+
+
+def test_reference_gradients_against_differences():
+    """The gradients that the GPU's are held to, against central differences in 64 bits."""
+    from attention_cases import inputs, reference
+    q_lens, k_lens = [3, 1, 2], [4, 0, 7]
+    q, k, v, q_off, k_off, how = inputs(q_lens, k_lens, 4, 2, 8, torch.float64, seed=1, reach=3, buckets=4,
+                                        causal=True, device="cpu")
+    g = torch.Generator().manual_seed(2)
+    dout = torch.randn(q.shape, generator=g, dtype=torch.float64)
+    r = reference(q, k, v, q_off, k_off, True, 0.3, dout=dout, **how)
+    loss = lambda: (reference(q, k, v, q_off, k_off, True, 0.3, **how)["out"] * dout.numpy()).sum()  # noqa: E731
+    h = 1e-5
+    for x, name in ((q, "dq"), (k, "dk"), (v, "dv"), (how["bias"], "dbias")):
+        flat = x.view(-1)
+        for i in torch.randperm(flat.numel(), generator=g)[:40].tolist():
+            old = flat[i].item()
+            flat[i] = old + h
+            above = loss()
+            flat[i] = old - h
+            below = loss()
+            flat[i] = old
+            # the error of a central difference is h^2 / 6 of a third derivative of order one, and 1e-16 / h
+            assert abs((above - below) / (2 * h) - r[name].reshape(-1)[i]) < 1e-8, (name, i)
