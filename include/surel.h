@@ -18,7 +18,8 @@
  * surel_query_incidence + surel_bfs_batches (Sec. 3.6 "Mini-batching for Training";
  * Algorithm 2: mini-batches of queries that share nodes, by breadth-first search).
  * Behind them, for a model that reads walks or joined sets: surel_attention and
- * surel_attention_grad (rows packed with the offsets that the join and the RPE table are laid out by).
+ * surel_attention_grad (rows packed with the offsets that the join and the RPE table are laid out by), and
+ * surel_softmax_loss and surel_softmax_loss_grad (a row's next node among all nodes of the graph).
  *
  * Conventions
  *   - Plain C ABI.  Pointers named d_* are DEVICE memory owned by the caller, on the
@@ -107,6 +108,7 @@ extern "C" {
 #define SUREL_DEV_BAD_OFFSETS   0x200u /* packed offsets are not non-decreasing from 0 to the number
                                           of rows; rows of such a sequence are empty or unwritten */
 #define SUREL_DEV_BAD_BUCKET    0x400u /* a bucket number is not in [0, n_buckets): taken as 0 */
+#define SUREL_DEV_BAD_LABEL     0x800u /* a label is not below n_classes: the row does not count */
 
 /* limits */
 #define SUREL_MAX_NODES   268435455   /* 2^28 - 1: node id and step share one 32-bit sort key */
@@ -120,6 +122,7 @@ extern "C" {
 #define SUREL_MAX_ROWS    1073741824  /* attention: packed rows of queries or keys (2^30)    */
 #define SUREL_MAX_HEAD_DIM 128        /* attention: elements of a head's row                 */
 #define SUREL_MAX_REACH   1024        /* attention: largest distance with a bucket of its own */
+#define SUREL_MAX_CLASS_DIM 256      /* loss: elements of a row                             */
 #define SUREL_MAX_STRIDE  16777208    /* attention: elements between rows or heads (2^24 - 8) */
 #define SUREL_NOALLOC_MAX_QUERIES 1048576  /* surel_join_queries_noalloc: n_queries (2^20)    */
 
@@ -139,7 +142,9 @@ extern "C" {
 #define SUREL_K_BATCH       10  /* surel_query_incidence and surel_bfs_batches        */
 #define SUREL_K_ATTENTION   11  /* surel_attention                                    */
 #define SUREL_K_ATTENTION_GRAD 12 /* surel_attention_grad (all its launches)           */
-#define SUREL_K_COUNT       13
+#define SUREL_K_LOSS        13  /* surel_softmax_loss                                 */
+#define SUREL_K_LOSS_GRAD   14  /* surel_softmax_loss_grad (all its launches)         */
+#define SUREL_K_COUNT       15
 
 /* 16-bit element types of a model's tensors */
 #define SUREL_BF16          0
@@ -483,6 +488,34 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
  * the same every time.  Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
 int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
                          const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias);
+
+/* Softmax cross entropy over a large number of classes (the graph's nodes), without keeping a logit: with
+ * z_nc = h_n . w_c, lse_n = log sum_c exp(z_nc), and loss_n = lse_n - z_n,label(n).
+ *   type       SUREL_BF16 or SUREL_FP16.
+ *   d_h        [n_rows][dim] of `type`, d_w [n_classes][dim] of `type`: dense, on 16-byte boundaries (device,
+ *              read-only).
+ *   d_labels   int32[n_rows] (device, read-only); a negative one: the row does not count, its loss is 0.
+ *   d_loss, d_lse   float[n_rows] (device, written); d_lse also of rows that do not count.
+ * Logits and sums are 32-bit.  Classes stream by in parts, several of them at a time: the context's
+ * workspace grows by 16 bytes a row and part (1,024 parts at most, 4,096 for up to 32 rows).  Results are the
+ * same every time.  Limits: n_rows >= 0 up to SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, dim a multiple of 8
+ * up to SUREL_MAX_CLASS_DIM.  Asynchronous.  Device-detected: BAD_LABEL. */
+int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void* d_w, const int32_t* d_labels,
+                       int64_t n_rows, int32_t n_classes, int32_t dim, float* d_loss, float* d_lse);
+
+/* The gradients of sum_n dloss_n loss_n.
+ *   d_dloss    float[n_rows] (device, read-only; entries of rows that do not count are not used).
+ *   d_lse      what surel_softmax_loss wrote (device, read-only).
+ *   d_dh       [n_rows][dim], d_dw [n_classes][dim] of `type`, dense, on 16-byte boundaries (device,
+ *              written).  Rows that do not count get zeros in d_dh and have no part in d_dw.
+ * Logits are made again; they and all sums are 32-bit, weights are rounded to `type` for their products (fp16: after a
+ * multiplication by a power of two), results once more.  Where d_dh's rows or d_dw's classes are too few to fill the
+ * device, parts of their sums are added up in a second step, in a fixed order: the context's workspace then grows by
+ * 4 dim bytes a row and part (256 at most) or class and part (64 at most), whichever is more.  Results are the
+ * same every time.  Limits and errors as above. */
+int surel_softmax_loss_grad(surel_ctx* ctx, int32_t type, const float* d_dloss, const void* d_h, const void* d_w,
+                            const int32_t* d_labels, const float* d_lse, int64_t n_rows, int32_t n_classes, int32_t dim,
+                            void* d_dh, void* d_dw);
 
 /* Every wait inside the fused kernel of surel_sample_walks_rpe and surel_sample_walks_rpe_ids (a
  * wave waiting for an offset, the offset scan waiting for a row count) and inside the pruning (a

@@ -18,23 +18,25 @@ LIB_PATH = os.path.join(_PKG_DIR, "libsurel.so")
 OK, E_NULL, E_RANGE, E_HIP, E_CAPACITY, E_CTX, E_DEVICE = 0, -1, -2, -3, -4, -5, -6
 DEV_BAD_SEED, DEV_BAD_GRAPH, DEV_BAD_WALK, DEV_BAD_QUERY = 0x01, 0x02, 0x04, 0x08
 DEV_SET_TOO_LARGE, DEV_CAPACITY, DEV_BAD_TABLE, DEV_BAD_SIZES = 0x10, 0x20, 0x40, 0x80
-DEV_STALL, DEV_BAD_OFFSETS, DEV_BAD_BUCKET = 0x100, 0x200, 0x400
+DEV_STALL, DEV_BAD_OFFSETS, DEV_BAD_BUCKET, DEV_BAD_LABEL = 0x100, 0x200, 0x400, 0x800
 MAX_NODES, MAX_STEPS, MAX_WALKS = 268435455, 15, 65535
 MAX_WALK_ENTRIES, MAX_SET, MAX_TUPLE = 2048, 2048, 3
 MAX_DISTINCT = 1 << 24
 MAX_BATCH = 1 << 20
 MAX_ROWS, MAX_HEAD_DIM, MAX_REACH, MAX_STRIDE = 1 << 30, 128, 1024, (1 << 24) - 8
+MAX_CLASS_DIM = 256
 NOALLOC_MAX_QUERIES = 1 << 20
 BF16, FP16 = 0, 1
 
 (K_WALK, K_RPE_COUNT, K_RPE_FILL, K_JOIN_COUNT, K_JOIN_FILL, K_SCAN, K_WALK_RPE,
  K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_ATTENTION,
- K_ATTENTION_GRAD, K_COUNT) = range(14)
+ K_ATTENTION_GRAD, K_LOSS, K_LOSS_GRAD, K_COUNT) = range(16)
 KERNEL_NAMES = {K_WALK: "walk", K_RPE_COUNT: "rpe_count", K_RPE_FILL: "rpe_fill",
                 K_JOIN_COUNT: "join_count", K_JOIN_FILL: "join_fill", K_SCAN: "scan",
                 K_WALK_RPE: "walk_rpe", K_EDGE_RECORDS: "edge_records",
                 K_QUERY_IDS: "query_ids", K_PRUNE: "prune", K_BATCH: "batch",
-                K_ATTENTION: "attention", K_ATTENTION_GRAD: "attention_grad"}
+                K_ATTENTION: "attention", K_ATTENTION_GRAD: "attention_grad",
+                K_LOSS: "loss", K_LOSS_GRAD: "loss_grad"}
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
@@ -89,6 +91,9 @@ SIGNATURES = {
                                          _i32, _i32, _vp, _vp, _vp, _vp]),
     "surel_attention": (ctypes.c_int, [_vp, ctypes.POINTER(AttentionArgs), _vp, _vp]),
     "surel_attention_grad": (ctypes.c_int, [_vp, ctypes.POINTER(AttentionArgs)] + 7 * [_vp]),
+    "surel_softmax_loss": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp]),
+    "surel_softmax_loss_grad": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp,
+                                               _vp]),
     "surel_set_spin_limit": (ctypes.c_int, [_vp, ctypes.c_uint32]),
     "surel_check": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "surel_profile_enable": (ctypes.c_int, [_vp, ctypes.c_int]),
@@ -680,3 +685,46 @@ def distance_buckets(reach: int, buckets: int, causal: bool = False) -> list[int
             b = min(b, half - 1)
         out.append(b if d <= 0 or causal else half + b)
     return out
+
+
+def _loss_shape(h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor) -> tuple[int, int, int, int]:
+    """(type, rows, classes, dim), checked."""
+    if h.dtype not in _TYPES:
+        raise TypeError(f"h must be torch.bfloat16 or torch.float16, got {h.dtype}")
+    if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[1]:
+        raise ValueError("h must be [rows][dim], w [classes][dim]")
+    if labels.shape != h.shape[:1]:
+        raise ValueError("labels must have one entry a row")
+    return _TYPES[h.dtype], h.shape[0], w.shape[0], h.shape[1]
+
+
+def softmax_loss(ctx: Context, h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor):
+    """(loss float32[rows], lse float32[rows]) on the GPU: softmax cross entropy of rows h [rows][dim] against all
+    classes w [classes][dim] (bfloat16 or float16, dense), of which labels int32[rows] names each row's; a
+    negative label: the row does not count, its loss is 0.  Logits are not kept."""
+    kind, n, classes, dim = _loss_shape(h, w, labels)
+    loss = torch.empty(n, dtype=torch.float32, device=h.device)
+    lse = torch.empty(n, dtype=torch.float32, device=h.device)
+    rc = load().surel_softmax_loss(ctx.handle, kind, _ptr(h, h.dtype, "h"), _ptr(w, h.dtype, "w"),
+                                   _ptr(labels, torch.int32, "labels"), n, classes, dim, loss.data_ptr(),
+                                   lse.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_softmax_loss")
+    return loss, lse
+
+
+def softmax_loss_grad(ctx: Context, dloss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor,
+                      lse: torch.Tensor):
+    """(dh, dw) on the GPU, of the shapes and type of h and w, for the gradient dloss float32[rows] of
+    softmax_loss's loss; lse is what it returned, everything else what it was given."""
+    kind, n, classes, dim = _loss_shape(h, w, labels)
+    if dloss.shape != labels.shape or lse.shape != labels.shape:
+        raise ValueError("dloss and lse must have one entry a row")
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    rc = load().surel_softmax_loss_grad(
+        ctx.handle, kind, _ptr(dloss, torch.float32, "dloss"), _ptr(h, h.dtype, "h"), _ptr(w, h.dtype, "w"),
+        _ptr(labels, torch.int32, "labels"), _ptr(lse, torch.float32, "lse"), n, classes, dim, dh.data_ptr(),
+        dw.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_softmax_loss_grad")
+    return dh, dw

@@ -9,6 +9,7 @@
 #include "attention.h"
 #include "context.h"
 #include "kernels.h"
+#include "loss.h"
 
 namespace {
 
@@ -58,6 +59,24 @@ int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::A
     return SUREL_OK;
 }
 
+int loss_args(const surel_ctx* ctx, int32_t type, const void* d_h, const void* d_w, const int32_t* d_labels,
+              int64_t n_rows, int32_t n_classes, int32_t dim, surel::LossArgs* a) {
+    if (type != SUREL_BF16 && type != SUREL_FP16) return SUREL_E_RANGE;
+    if (n_rows < 0 || n_rows > SUREL_MAX_ROWS || n_classes < 1 || n_classes > SUREL_MAX_NODES) return SUREL_E_RANGE;
+    if (dim < 8 || dim > SUREL_MAX_CLASS_DIM || dim % 8 != 0) return SUREL_E_RANGE;
+    if (!d_w || (n_rows > 0 && (!d_h || !d_labels))) return SUREL_E_NULL;
+    if (misaligned16(d_h) || misaligned16(d_w)) return SUREL_E_RANGE;
+    if (!ctx) return SUREL_E_CTX;
+    a->h = static_cast<const char*>(d_h);
+    a->w = static_cast<const char*>(d_w);
+    a->labels = d_labels;
+    a->n_rows = (int32_t)n_rows;
+    a->n_classes = n_classes;
+    a->dim = dim;
+    a->err = ctx->d_err;
+    return SUREL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -101,6 +120,40 @@ int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const
     KernelSpan span(ctx, SUREL_K_ATTENTION_GRAD);
     if (surel::launch_attention_grad(ctx->stream, a, args->type == SUREL_FP16, d_dout, d_out, d_lse, d_dq, d_dk, d_dv,
                                      d_dbias, ctx->d_model) != hipSuccess)
+        return SUREL_E_HIP;
+    return SUREL_OK;
+}
+
+int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void* d_w, const int32_t* d_labels,
+                       int64_t n_rows, int32_t n_classes, int32_t dim, float* d_loss, float* d_lse) {
+    surel::LossArgs a;
+    if (int rc = loss_args(ctx, type, d_h, d_w, d_labels, n_rows, n_classes, dim, &a)) return rc;
+    if (n_rows > 0 && (!d_loss || !d_lse)) return SUREL_E_NULL;
+    if (n_rows == 0) return SUREL_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SUREL_E_HIP;
+    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::loss_scratch_bytes(ctx->n_cu, a))) return rc;
+    KernelSpan span(ctx, SUREL_K_LOSS);
+    if (surel::launch_loss(ctx->stream, ctx->n_cu, a, type == SUREL_FP16, d_loss, d_lse, ctx->d_model) != hipSuccess)
+        return SUREL_E_HIP;
+    return SUREL_OK;
+}
+
+int surel_softmax_loss_grad(surel_ctx* ctx, int32_t type, const float* d_dloss, const void* d_h, const void* d_w,
+                            const int32_t* d_labels, const float* d_lse, int64_t n_rows, int32_t n_classes, int32_t dim,
+                            void* d_dh, void* d_dw) {
+    surel::LossArgs a;
+    if (int rc = loss_args(ctx, type, d_h, d_w, d_labels, n_rows, n_classes, dim, &a)) return rc;
+    if (!d_dw || (n_rows > 0 && (!d_dloss || !d_lse || !d_dh))) return SUREL_E_NULL;
+    if (misaligned16(d_dh) || misaligned16(d_dw)) return SUREL_E_RANGE;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SUREL_E_HIP;
+    if (n_rows == 0)
+        return surel::launch_zero(ctx->stream, d_dw, (int64_t)n_classes * dim) == hipSuccess ? SUREL_OK : SUREL_E_HIP;
+    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::loss_grad_scratch_bytes(ctx->n_cu, a))) return rc;
+    KernelSpan span(ctx, SUREL_K_LOSS_GRAD);
+    if (surel::launch_loss_grad(ctx->stream, ctx->n_cu, a, type == SUREL_FP16, d_dloss, d_lse, d_dh, d_dw, ctx->d_model) !=
+        hipSuccess)
         return SUREL_E_HIP;
     return SUREL_OK;
 }

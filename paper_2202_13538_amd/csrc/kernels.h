@@ -218,4 +218,12 @@ size_t attention_grad_scratch_bytes(const AttentionArgs& a);
 hipError_t launch_attention_grad(hipStream_t stream, const AttentionArgs& a, bool half, const void* dout, const void* out,
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch);
 
+// loss.hip, loss_grad.hip.  scratch: that many bytes of device memory.  Need a.n_rows, a.n_classes >= 1.
+struct LossArgs;
+size_t loss_scratch_bytes(int n_cu, const LossArgs& a);
+hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch);
+size_t loss_grad_scratch_bytes(int n_cu, const LossArgs& a);
+hipError_t launch_loss_grad(hipStream_t stream, int n_cu, const LossArgs& a, bool half, const float* dloss, const float* lse,
+                            void* dh, void* dw, void* scratch);
+
 }  // namespace surel

@@ -1,0 +1,209 @@
+// Softmax cross entropy of rows against a large table of classes (surel_softmax_loss).
+#include <math.h>
+
+#include "kernels.h"
+#include "loss.h"
+
+namespace surel {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct LossOut {
+    f32x4* part = nullptr;  // [n_rows][parts of rows]: maximum and sum (base 2), the label's score
+    float *loss = nullptr, *lse = nullptr;
+    int splits = 1;
+    int row_parts = 1;      // splits times the waves that share a row
+};
+
+template <int DP, int WR>
+struct LossShape {
+    static constexpr int WK = 4 / WR;
+    static constexpr int RB = WR == 1 ? 1 : 2;               // blocks of 32 rows a wave holds
+    static constexpr int kRows = 32 * RB * WR;
+    static constexpr int kKeys = WK == 1 ? 64 : 32;          // classes a wave takes at a time
+    static constexpr int kTileKeys = kKeys * WK;
+    static constexpr int kTileBytes = kTileKeys * Tile<DP>::kRowBytes;
+};
+
+// One workgroup: kRows rows against a part of the classes, which stream through LDS.  Waves hold their rows
+// in registers and compute scores^T = W h^T: a row's scores lie in one lane and its partner, each of
+// which keeps a running maximum and sum of its own until the end.  No logit leaves the registers.
+//   WR = 4: 256 rows, every wave 64 of them and all classes of a tile;
+//   WR = 1: 32 rows, the waves take different classes of a tile.
+template <class T, int DP, int WR>
+__global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o) {
+    using Shape = LossShape<DP, WR>;
+    constexpr int RB = Shape::RB;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int split = blockIdx.x % o.splits, row_tile = blockIdx.x / o.splits;
+    const int first = row_tile * Shape::kRows + (WR == 1 ? 0 : wave * 32 * RB), wk = WR == 1 ? wave : 0;
+
+    Stationary<DP> h[RB];
+    int label[RB];
+    float top[RB], sum[RB], hit[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int row = first + 32 * r + col;
+        const bool counts = row < a.n_rows;
+        h[r].load(a.h + (int64_t)row * a.dim * 2, counts, a.dim, lane);
+        label[r] = counts ? label_of(a, row) : -1;
+        top[r] = -INFINITY, sum[r] = 0.f, hit[r] = 0.f;
+    }
+    const int steps = (a.n_classes + Shape::kTileKeys - 1) / Shape::kTileKeys, each = (steps + o.splits - 1) / o.splits;
+    const int begin = min(split * each, steps), end = min(begin + each, steps);
+    const uint32_t row_bytes = (uint32_t)a.dim * 2;
+    auto fetch = [&](int step, int buffer) {
+        const int c0 = step * Shape::kTileKeys;
+        copy_tile<DP, Shape::kTileKeys, kThreads>(lds + buffer * Shape::kTileBytes, a.w + (int64_t)c0 * row_bytes, row_bytes,
+                                                  a.n_classes - c0, a.dim, tid);
+    };
+    if (begin < end) fetch(begin, 0);
+    tile_arrived();
+    __syncthreads();
+    const bool works = first < a.n_rows;
+    int buffer = 0;
+#pragma unroll 1
+    for (int step = begin; step < end; ++step, buffer ^= 1) {
+        if (step + 1 < end) fetch(step + 1, buffer ^ 1);
+        if (works) {
+#pragma unroll
+            for (int b = 0; b < Shape::kKeys; b += 32) {
+                const int c0 = step * Shape::kTileKeys + wk * Shape::kKeys + b;
+                const char* const tile = lds + buffer * Shape::kTileBytes;
+                f32x16 s[RB] = {};
+#pragma unroll
+                for (int ks = 0; ks < DP / 16; ++ks) {
+                    const u32x4 x = Tile<DP>::rows(tile, wk * Shape::kKeys + b, ks, lane);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) s[r] = T::mma(x, h[r].k[ks], s[r]);
+                }
+                if (c0 + 32 > a.n_classes) {
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[r][i] = c0 + row_of(i, g) < a.n_classes ? s[r][i] : -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    if (__any((uint32_t)(label[r] - c0) < 32u)) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) hit[r] = label[r] - c0 == row_of(i, g) ? s[r][i] : hit[r];
+                    }
+                    float most = s[r][0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[r][i]);
+                    const float now = fmaxf(top[r], most * kLog2e), base = now == -INFINITY ? 0.f : now;
+                    float part = sum[r] * exp2_fast(top[r] - base);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part += exp2_fast(__builtin_fmaf(s[r][i], kLog2e, -base));
+                    sum[r] = part;
+                    top[r] = now;
+                }
+            }
+        }
+        tile_arrived();
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const float other = from_other_half(top[r]), other_sum = from_other_half(sum[r]), other_hit = from_other_half(hit[r]);
+        const float now = fmaxf(top[r], other), base = now == -INFINITY ? 0.f : now;
+        const float total = sum[r] * exp2_fast(top[r] - base) + other_sum * exp2_fast(other - base);
+        const int row = first + 32 * r + col;
+        if (g == 0 && row < a.n_rows)
+            o.part[(int64_t)row * o.row_parts + split * Shape::WK + wk] = f32x4{now, total, hit[r] + other_hit, 0.f};
+    }
+}
+
+// One wave a row: the parts of its classes.
+__global__ __launch_bounds__(kThreads) void loss_join_kernel(LossArgs a, LossOut o) {
+    const int row = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= a.n_rows) return;
+    float top = -INFINITY, sum = 0.f, hit = 0.f;
+    for (int p = lane; p < o.row_parts; p += 64) {
+        const f32x4 x = o.part[(int64_t)row * o.row_parts + p];
+        const float now = fmaxf(top, x[0]), base = now == -INFINITY ? 0.f : now;
+        sum = sum * exp2_fast(top - base) + x[1] * exp2_fast(x[0] - base);
+        top = now;
+        hit += x[2];
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const float other = __shfl_xor(top, m), other_sum = __shfl_xor(sum, m);
+        const float now = fmaxf(top, other), base = now == -INFINITY ? 0.f : now;
+        sum = sum * exp2_fast(top - base) + other_sum * exp2_fast(other - base);
+        top = now;
+        hit += __shfl_xor(hit, m);
+    }
+    if (lane == 0) {
+        const float lse = (top + log2_fast(sum)) * kLn2;
+        const int label = a.labels[row];
+        o.lse[row] = lse;
+        o.loss[row] = label < 0 || label >= a.n_classes ? 0.f : lse - hit;
+    }
+}
+
+struct LossPlan {
+    bool few;
+    int splits, row_parts;
+    int64_t tiles;
+};
+LossPlan loss_plan(const LossArgs& a, int n_cu) {
+    LossPlan p;
+    p.few = a.n_rows <= 32;
+    const int rows = p.few ? 32 : 256, keys = p.few ? 128 : 64;
+    p.tiles = (a.n_rows + rows - 1) / rows;
+    p.splits = parts_for(p.tiles, (a.n_classes + keys - 1) / keys, 2 * n_cu, 1024);
+    p.row_parts = p.splits * (p.few ? 4 : 1);
+    return p;
+}
+
+template <class T, int DP, int WR>
+hipError_t launch(hipStream_t stream, const LossArgs& a, const LossOut& o, const LossPlan& p) {
+    const size_t bytes = 2 * LossShape<DP, WR>::kTileBytes;
+    auto kernel = loss_kernel<T, DP, WR>;
+    if (bytes > 65536) {
+        const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (rc != hipSuccess) return rc;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.splits)), dim3(kThreads), bytes, stream, a, o);
+    return hipGetLastError();
+}
+template <class T, int DP>
+hipError_t launch_rows(hipStream_t stream, const LossArgs& a, const LossOut& o, const LossPlan& p) {
+    return p.few ? launch<T, DP, 1>(stream, a, o, p) : launch<T, DP, 4>(stream, a, o, p);
+}
+template <class T>
+hipError_t launch_type(hipStream_t stream, const LossArgs& a, const LossOut& o, const LossPlan& p) {
+    return a.dim <= 32    ? launch_rows<T, 32>(stream, a, o, p)
+           : a.dim <= 64  ? launch_rows<T, 64>(stream, a, o, p)
+           : a.dim <= 96  ? launch_rows<T, 96>(stream, a, o, p)
+           : a.dim <= 128 ? launch_rows<T, 128>(stream, a, o, p)
+           : a.dim <= 192 ? launch_rows<T, 192>(stream, a, o, p)
+                          : launch_rows<T, 256>(stream, a, o, p);
+}
+
+}  // namespace
+
+size_t loss_scratch_bytes(int n_cu, const LossArgs& a) {
+    return (size_t)a.n_rows * loss_plan(a, n_cu).row_parts * sizeof(f32x4);
+}
+
+hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch) {
+    const LossPlan p = loss_plan(a, n_cu);
+    LossOut o;
+    o.part = static_cast<f32x4*>(scratch);
+    o.loss = loss;
+    o.lse = lse;
+    o.splits = p.splits;
+    o.row_parts = p.row_parts;
+    const hipError_t rc = half ? launch_type<Fp16>(stream, a, o, p) : launch_type<Bf16>(stream, a, o, p);
+    if (rc != hipSuccess) return rc;
+    hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(kThreads), 0, stream, a, o);
+    return hipGetLastError();
+}
+
+}  // namespace surel

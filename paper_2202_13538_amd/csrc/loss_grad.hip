@@ -1,0 +1,334 @@
+// The gradients of the softmax loss (surel_softmax_loss_grad).
+//
+// With z = h w^T and g_nc = dloss_n (exp(z_nc - lse_n) - [c = label_n]):  dh = g w,  dw = g^T h.
+// Logits are made again where they are needed, in the registers of the workgroup that needs them: once for
+// dh (rows stay, classes stream by) and once for dw (classes stay, rows stream by).  For rows of up to 256
+// elements that is less than to write g, 16 bits a row and class, and read it twice: 4 dim operations against
+// 6 bytes, 0.4 against 1.2 ps at 128 elements and the rates of a large product and a large copy.
+#include <math.h>
+
+#include "kernels.h"
+#include "loss.h"
+
+namespace surel {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kStep = 64;  // streamed rows or classes of a tile
+// fp16 only: weights (of at most 1) are multiplied by 2^12 before they are rounded, so that a class's share
+// of 1.5e-8 still has all its bits.
+constexpr int kLift = 12;
+
+struct LossGradArgs {
+    const float *dloss = nullptr, *lse = nullptr;
+    void *dh = nullptr, *dw = nullptr;
+    float *part_h = nullptr, *part_w = nullptr;  // [split][rows][dim], where there are several
+    uint32_t* largest = nullptr;                 // of |dloss|, as a float's bits (fp16 only)
+    int splits_h = 1, splits_w = 1;
+};
+
+__global__ void clear_largest_kernel(uint32_t* word) { *word = 0; }
+
+__global__ __launch_bounds__(kThreads) void largest_kernel(LossArgs a, LossGradArgs w) {
+    float most = 0.f;
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_rows; i += gridDim.x * kThreads)
+        if (a.labels[i] >= 0) most = fmaxf(most, fabsf(w.dloss[i]));
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(w.largest, __float_as_uint(most));
+}
+
+// The power of two that dloss is multiplied by before weights are rounded to fp16: the largest becomes 2^11 .. 2^12.
+template <class T>
+__device__ __forceinline__ int lift_of(const LossGradArgs& w) {
+    if (!T::kNarrow) return 0;
+    const float most = __uint_as_float(*w.largest);
+    if (!(most > 0.f) || !(most < INFINITY)) return 0;
+    return min(max(kLift - 1 - ilogbf(most), -100), 100);
+}
+
+// dh of 128 rows, 32 a wave, from a part of the classes.
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(LossArgs a, LossGradArgs w) {
+    constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int split = blockIdx.x % w.splits_h, first = blockIdx.x / w.splits_h * 128 + wave * 32, row = first + col;
+    const bool in = row < a.n_rows, works = first < a.n_rows;
+    Stationary<DP> h;
+    h.load(a.h + (int64_t)row * a.dim * 2, in, a.dim, lane);
+    const int label = in ? label_of(a, row) : -1;
+    const float lift = T::kNarrow ? (float)kLift : 0.f, one = T::kNarrow ? (float)(1 << kLift) : 1.f;
+    const float base = (in ? w.lse[row] * kLog2e : 0.f) - lift;
+    const float scale = label >= 0 ? w.dloss[row] / one : 0.f;
+
+    f32x16 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+    const int steps = (a.n_classes + kStep - 1) / kStep, each = (steps + w.splits_h - 1) / w.splits_h;
+    const int begin = min(split * each, steps), end = min(begin + each, steps);
+    const uint32_t row_bytes = (uint32_t)a.dim * 2;
+    auto fetch = [&](int step, int buffer) {
+        const int c0 = step * kStep;
+        copy_tile<DP, kStep, kThreads>(lds + buffer * kTileBytes, a.w + (int64_t)c0 * row_bytes, row_bytes,
+                                       a.n_classes - c0, a.dim, tid);
+    };
+    if (begin < end) fetch(begin, 0);
+    tile_arrived();
+    __syncthreads();
+    int buffer = 0;
+#pragma unroll 1
+    for (int step = begin; step < end; ++step, buffer ^= 1) {
+        if (step + 1 < end) fetch(step + 1, buffer ^ 1);
+        const char* const tile = lds + buffer * kTileBytes;
+        if (works) {
+#pragma unroll
+            for (int b = 0; b < kStep; b += 32) {
+                const int c0 = step * kStep + b;
+                f32x16 s = scores<T, DP>(tile, b, h, lane);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], kLog2e, -base));
+                if (__any((uint32_t)(label - c0) < 32u)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] -= label - c0 == row_of(i, g) ? one : 0.f;
+                }
+                if (c0 + 32 > a.n_classes) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = c0 + row_of(i, g) < a.n_classes ? s[i] : 0.f;
+                }
+                accumulate<T, DP>(acc, tile, b, s, lane);   // (weights rounded to the inputs' 16 bits)
+            }
+        }
+        tile_arrived();
+        __syncthreads();
+    }
+    if (w.splits_h > 1) {
+        if (!in) return;
+        float* const dst = w.part_h + ((int64_t)split * a.n_rows + row) * a.dim;
+        const bool zero = scale == 0.f;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * db + row_of(i, g);
+                const f32x4 x = {acc[db][i] * scale, acc[db][i + 1] * scale, acc[db][i + 2] * scale, acc[db][i + 3] * scale};
+                if (d < a.dim) *reinterpret_cast<f32x4*>(dst + d) = zero ? f32x4{0.f, 0.f, 0.f, 0.f} : x;
+            }
+        return;
+    }
+    store_rows<T, DP>(acc, scale, scale == 0.f, lds + wave * 32 * Tile<DP>::kRowBytes, a.dim, lane, [&](int r) -> char* {
+        return first + r < a.n_rows ? static_cast<char*>(w.dh) + (int64_t)(first + r) * a.dim * 2 : nullptr;
+    });
+}
+
+// dw of 128 classes, 32 a wave, from a part of the rows.
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(LossArgs a, LossGradArgs w) {
+    constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ __align__(16) float stats[2][2][kStep];   // [buffer][lse, dloss][row]
+    __shared__ __align__(16) int labels[2][kStep];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int split = blockIdx.x % w.splits_w, first = blockIdx.x / w.splits_w * 128 + wave * 32, cls = first + col;
+    const bool in = cls < a.n_classes, works = first < a.n_classes;
+    Stationary<DP> c;
+    c.load(a.w + (int64_t)cls * a.dim * 2, in, a.dim, lane);
+    const int lift = lift_of<T>(w);
+    const float up = ldexpf(1.f, lift);
+
+    f32x16 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+    const int steps = (a.n_rows + kStep - 1) / kStep, each = (steps + w.splits_w - 1) / w.splits_w;
+    const int begin = min(split * each, steps), end = min(begin + each, steps);
+    const uint32_t row_bytes = (uint32_t)a.dim * 2;
+    float stat = 0.f;
+    int label = -1;
+    auto fetch = [&](int step, int buffer) {
+        const int r0 = step * kStep, n = r0 + (tid & (kStep - 1));
+        copy_tile<DP, kStep, kThreads>(lds + buffer * kTileBytes, a.h + (int64_t)r0 * row_bytes, row_bytes, a.n_rows - r0,
+                                       a.dim, tid);
+        if (tid < 2 * kStep) {
+            label = n < a.n_rows ? a.labels[n] : -1;
+            if (label >= a.n_classes) label = -1;
+            // (a row that does not count: weights of zero)
+            if (tid < kStep) stat = label < 0 ? INFINITY : w.lse[n] * kLog2e;
+            else stat = label < 0 ? 0.f : w.dloss[n] * up;
+        }
+    };
+    auto keep = [&](int buffer) {
+        if (tid < 2 * kStep) stats[buffer][tid / kStep][tid & (kStep - 1)] = stat;
+        if (tid < kStep) labels[buffer][tid] = label;
+    };
+    if (begin < end) {
+        fetch(begin, 0);
+        keep(0);
+    }
+    tile_arrived();
+    __syncthreads();
+    int buffer = 0;
+#pragma unroll 1
+    for (int step = begin; step < end; ++step, buffer ^= 1) {
+        const bool more = step + 1 < end;
+        if (more) fetch(step + 1, buffer ^ 1);
+        const char* const tile = lds + buffer * kTileBytes;
+        if (works) {
+#pragma unroll
+            for (int b = 0; b < kStep; b += 32) {
+                f32x16 s = scores<T, DP>(tile, b, c, lane);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&stats[buffer][0][b + 8 * n + 4 * g]);
+                    const f32x4 dl = *reinterpret_cast<const f32x4*>(&stats[buffer][1][b + 8 * n + 4 * g]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[4 * n + i] = exp2_fast(__builtin_fmaf(s[4 * n + i], kLog2e, -lse2[i])) * dl[i];
+                }
+                if (__any((uint32_t)(labels[buffer][b + col] - first) < 32u)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int n = b + row_of(i, g);
+                        s[i] -= labels[buffer][n] == cls ? stats[buffer][1][n] : 0.f;
+                    }
+                }
+                accumulate<T, DP>(acc, tile, b, s, lane);   // (weights rounded to the inputs' 16 bits)
+            }
+        }
+        if (more) keep(buffer ^ 1);
+        tile_arrived();
+        __syncthreads();
+    }
+    if (__any(has_nan(acc))) {   // once more, without the rows that do not count
+#pragma unroll
+        for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
+#pragma unroll 1
+        for (int n = begin * kStep; n < min(end * kStep, a.n_rows); ++n) {
+            const int label_n = a.labels[n];
+            if (label_n < 0 || label_n >= a.n_classes) continue;
+            const char* const row = a.h + (int64_t)n * row_bytes;
+            const float z = dot_row<T, DP>(c, row, a.dim, lane);
+            const float p = exp2_fast(__builtin_fmaf(z, kLog2e, -w.lse[n] * kLog2e)) - (label_n == cls ? 1.f : 0.f);
+            accumulate_row<T, DP>(acc, row, p * w.dloss[n] * up, a.dim, g);
+        }
+    }
+    const float down = ldexpf(1.f, -lift);
+    if (w.splits_w > 1) {
+        if (!in) return;
+        float* const dst = w.part_w + ((int64_t)split * a.n_classes + cls) * a.dim;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * db + row_of(i, g);
+                if (d < a.dim)
+                    *reinterpret_cast<f32x4*>(dst + d) = f32x4{acc[db][i] * down, acc[db][i + 1] * down,
+                                                               acc[db][i + 2] * down, acc[db][i + 3] * down};
+            }
+        return;
+    }
+    store_rows<T, DP>(acc, down, false, lds + wave * 32 * Tile<DP>::kRowBytes, a.dim, lane, [&](int r) -> char* {
+        return first + r < a.n_classes ? static_cast<char*>(w.dw) + (int64_t)(first + r) * a.dim * 2 : nullptr;
+    });
+}
+
+// The parts of every element, in order, four elements a thread.
+template <class T>
+__global__ __launch_bounds__(kThreads) void add_parts_kernel(const float* part, int splits, int64_t n4, void* out) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= n4) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) sum += reinterpret_cast<const f32x4*>(part)[s * n4 + i];
+    static_cast<u32x2*>(out)[i] = u32x2{pack2<T>(sum[0], sum[1]), pack2<T>(sum[2], sum[3])};
+}
+
+struct LossGradPlan {
+    int64_t tiles_h, tiles_w;
+    int splits_h, splits_w;
+};
+LossGradPlan loss_grad_plan(const LossArgs& a, int n_cu) {
+    LossGradPlan p;
+    p.tiles_h = (a.n_rows + 127) / 128;
+    p.tiles_w = ((int64_t)a.n_classes + 127) / 128;
+    const int slots = a.dim > 192 ? n_cu : 2 * n_cu;
+    p.splits_h = parts_for(p.tiles_h, (a.n_classes + kStep - 1) / kStep, slots, 256);
+    p.splits_w = parts_for(p.tiles_w, (a.n_rows + kStep - 1) / kStep, slots, 64);
+    return p;
+}
+
+size_t lay_out(const LossArgs& a, const LossGradPlan& p, char* scratch, LossGradArgs* w) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* const here = scratch + at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    w->largest = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+    // one after the other in one place: dh's parts are added up before dw's are written
+    const size_t h = p.splits_h > 1 ? (size_t)p.splits_h * a.n_rows * a.dim * sizeof(float) : 0;
+    const size_t c = p.splits_w > 1 ? (size_t)p.splits_w * a.n_classes * a.dim * sizeof(float) : 0;
+    w->part_h = w->part_w = reinterpret_cast<float*>(take(h > c ? h : c));
+    return at;
+}
+
+template <class T>
+hipError_t add_parts(hipStream_t stream, const float* part, int splits, int64_t elements, void* out) {
+    const int64_t n4 = elements / 4;
+    hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)((n4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, part,
+                       splits, n4, out);
+    return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t launch_width(hipStream_t stream, const LossArgs& a, const LossGradArgs& w, const LossGradPlan& p) {
+    const size_t bytes = 2 * (size_t)kStep * Tile<DP>::kRowBytes;   // 64 KB at most
+    hipLaunchKernelGGL((loss_dh_kernel<T, DP>), dim3((unsigned)(p.tiles_h * p.splits_h)), dim3(kThreads), bytes, stream, a, w);
+    hipError_t rc = hipGetLastError();
+    if (rc == hipSuccess && p.splits_h > 1)
+        rc = add_parts<T>(stream, w.part_h, p.splits_h, (int64_t)a.n_rows * a.dim, w.dh);
+    if (rc != hipSuccess) return rc;
+    hipLaunchKernelGGL((loss_dw_kernel<T, DP>), dim3((unsigned)(p.tiles_w * p.splits_w)), dim3(kThreads), bytes, stream, a, w);
+    rc = hipGetLastError();
+    if (rc == hipSuccess && p.splits_w > 1)
+        rc = add_parts<T>(stream, w.part_w, p.splits_w, (int64_t)a.n_classes * a.dim, w.dw);
+    return rc;
+}
+
+template <class T>
+hipError_t launch_type(hipStream_t stream, const LossArgs& a, const LossGradArgs& w, const LossGradPlan& p) {
+    if (T::kNarrow) {
+        hipLaunchKernelGGL(clear_largest_kernel, dim3(1), dim3(1), 0, stream, w.largest);
+        const int blocks = (a.n_rows + kThreads - 1) / kThreads;
+        hipLaunchKernelGGL(largest_kernel, dim3((unsigned)(blocks < 256 ? blocks : 256)), dim3(kThreads), 0, stream, a, w);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess) return rc;
+    }
+    return a.dim <= 32    ? launch_width<T, 32>(stream, a, w, p)
+           : a.dim <= 64  ? launch_width<T, 64>(stream, a, w, p)
+           : a.dim <= 96  ? launch_width<T, 96>(stream, a, w, p)
+           : a.dim <= 128 ? launch_width<T, 128>(stream, a, w, p)
+           : a.dim <= 192 ? launch_width<T, 192>(stream, a, w, p)
+                          : launch_width<T, 256>(stream, a, w, p);
+}
+
+}  // namespace
+
+size_t loss_grad_scratch_bytes(int n_cu, const LossArgs& a) {
+    LossGradArgs w;
+    return lay_out(a, loss_grad_plan(a, n_cu), nullptr, &w);
+}
+
+hipError_t launch_loss_grad(hipStream_t stream, int n_cu, const LossArgs& a, bool half, const float* dloss, const float* lse,
+                            void* dh, void* dw, void* scratch) {
+    const LossGradPlan p = loss_grad_plan(a, n_cu);
+    LossGradArgs w;
+    lay_out(a, p, static_cast<char*>(scratch), &w);
+    w.dloss = dloss;
+    w.lse = lse;
+    w.dh = dh;
+    w.dw = dw;
+    w.splits_h = p.splits_h;
+    w.splits_w = p.splits_w;
+    return half ? launch_type<Fp16>(stream, a, w, p) : launch_type<Bf16>(stream, a, w, p);
+}
+
+}  // namespace surel

@@ -1,6 +1,7 @@
 """What the model operators refuse before they touch a device, and the helpers that need none."""
 import ctypes
 import math
+import types
 
 import pytest
 import torch
@@ -70,12 +71,48 @@ def test_attention_refuses_no_arguments():
     assert binding.load().surel_attention(None, None, P, P) == binding.E_NULL
 
 
+LOSS = [  # status, changes of (type, h, w, labels, rows, classes, dim)
+    (binding.E_RANGE, dict(type=2)), (binding.E_RANGE, dict(rows=-1)), (binding.E_RANGE, dict(rows=binding.MAX_ROWS + 1)),
+    (binding.E_RANGE, dict(classes=0)), (binding.E_RANGE, dict(classes=binding.MAX_NODES + 1)),
+    (binding.E_RANGE, dict(dim=0)), (binding.E_RANGE, dict(dim=20)), (binding.E_RANGE, dict(dim=264)),
+    (binding.E_NULL, dict(h=None)), (binding.E_NULL, dict(w=None)), (binding.E_NULL, dict(labels=None)),
+    (binding.E_RANGE, dict(h=P + 8)), (binding.E_RANGE, dict(w=P + 4)), (binding.E_CTX, {}),
+]
+
+
+@pytest.mark.parametrize("status,changes", LOSS, ids=lambda x: str(x))
+def test_loss_refuses(status, changes):
+    lib = binding.load()
+    a = dict(type=binding.FP16, h=P, w=P, labels=P, rows=5, classes=100, dim=64) | changes
+    shape = (a["rows"], a["classes"], a["dim"])
+    assert lib.surel_softmax_loss(None, a["type"], a["h"], a["w"], a["labels"], *shape, P, P) == status
+    assert lib.surel_softmax_loss_grad(None, a["type"], P, a["h"], a["w"], a["labels"], P, *shape, P, P) == status
+
+
+def test_loss_outputs_that_are_missing_or_off_their_boundary():
+    lib = binding.load()
+    fake = ctypes.create_string_buffer(4096)
+    for loss, lse in ((None, P), (P, None)):
+        assert lib.surel_softmax_loss(fake, 0, P, P, P, 5, 100, 64, loss, lse) == binding.E_NULL
+    call = lambda dloss, lse, dh, dw: lib.surel_softmax_loss_grad(fake, 0, dloss, P, P, P, lse, 5, 100, 64, dh, dw)  # noqa: E731
+    for missing in range(4):
+        assert call(*[None if i == missing else P for i in range(4)]) == binding.E_NULL
+    assert call(P, P, P + 8, P) == call(P, P, P, P + 2) == binding.E_RANGE
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     t = torch.zeros(4, 2, 32)
     with pytest.raises(TypeError, match="bfloat16 or torch.float16"):
         binding.attention(None, t, t, t, torch.tensor([0, 4]))
     with pytest.raises(ValueError, match="GPU"):
         binding.attention(None, t.half(), t.half(), t.half(), torch.tensor([0, 4]))
+    h, w, labels = torch.zeros(3, 16).half(), torch.zeros(9, 16).half(), torch.zeros(3, dtype=torch.int32)
+    for bad in ((h.float(), w, labels), (h, w.bfloat16(), labels), (h, w, labels.long())):
+        with pytest.raises((TypeError, ValueError)):
+            binding.softmax_loss(types.SimpleNamespace(handle=None), *bad)
+    for bad in ((h[0], w, labels), (h, w[:, :8], labels), (h, w, labels[:2])):
+        with pytest.raises(ValueError):
+            binding.softmax_loss(types.SimpleNamespace(handle=None), *bad)
 
 
 @pytest.mark.parametrize("reach,buckets,causal", [(0, 1, True), (0, 2, False), (1, 2, True), (15, 16, True),
