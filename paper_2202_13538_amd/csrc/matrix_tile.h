@@ -12,8 +12,10 @@
 // 8 + 4 g .. 8 + 4 g + 3 of 16.  Its A operand, 16 streamed rows of a tile transposed, is read in the
 // same order by two transposing LDS loads of 4 rows each.
 //
-// Rows lie in LDS in chunks of 16 bytes, those of row r permuted by r's lowest bits: the 8 lanes that
-// a 16-byte load serves at a time (8 rows, one chunk) then meet 8 different groups of banks.
+// Rows lie in LDS in chunks of 16 bytes, permuted inside a row by the row's number so that neither
+// kind of load meets a bank twice in a cycle (of 256 bytes, 64 banks): 16 rows' chunks of one column lie in 16
+// places of 256 bytes, and 4 neighbouring rows' groups of 4 chunks in 4 different quarters of them.  (Permuted by
+// the low 3 bits of the row alone, two thirds of the LDS cycles of rows of 128 elements were conflicts.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -91,8 +93,12 @@ template <int DP>
 struct Tile {
     static constexpr int kChunks = DP / 8;
     static constexpr int kRowBytes = 2 * DP;
-    // (rows of an odd number of 64 bytes: two of them lie in 128 bytes)
-    __device__ __forceinline__ static int permuted(int row) { return DP % 64 == 0 ? row & 7 : (row >> 1) & 3; }
+    // What a chunk's number is xor-ed with.  Rows of a multiple of 256 bytes begin in one place of the banks: the
+    // row's low bits choose the quarter.  Of 128 bytes, two rows share the 256; of 64, four lie in all quarters.
+    __device__ __forceinline__ static int permuted(int row) {
+        const int high = DP % 128 == 0 ? (row & 3) << 2 : DP % 64 == 0 ? (row & 2) << 1 : 0;
+        return high | ((row >> 2) & 3);
+    }
 
     // A operand: rows row0 .. row0 + 31, inner values 16 ks .. 16 ks + 15.
     __device__ __forceinline__ static u32x4 rows(const char* tile, int row0, int ks, int lane) {
