@@ -113,15 +113,16 @@ __device__ __forceinline__ void fill_bias(float* table, const AttentionArgs& a, 
     }
 }
 
+// (the same in every lane, and the compiler is told so: branches on it are scalar)
 __device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) x = min(x, __shfl_xor(x, m));
-    return x;
+    return __builtin_amdgcn_readfirstlane(x);
 }
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) x = max(x, __shfl_xor(x, m));
-    return x;
+    return __builtin_amdgcn_readfirstlane(x);
 }
 
 }  // namespace surel

@@ -36,7 +36,7 @@ struct ForwardShape {
 //   WR = 1: 32 rows (single tokens, a pooling row a set); the four waves take different keys of a tile of 128
 //           and join their sums at the end.
 template <class T, int DP, int WR>
-__global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionArgs a, AttentionOut o) {
+__global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_kernel(AttentionArgs a, AttentionOut o) {
     using Shape = ForwardShape<DP, WR>;
     constexpr int WK = Shape::WK, kBlocks = Shape::kKeys / 32, NB = DP / 32;
     extern __shared__ __align__(16) char lds[];
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionArgs a,
     char* const v_tile = lds + Shape::kBuffers * Shape::kTileBytes;
     float* const bias = reinterpret_cast<float*>(lds + Shape::kLds);
 
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int wr = WR == 1 ? 0 : wave, wk = WR == 1 ? wave : 0;
     const int n_head_tiles = a.heads / o.pack;
     int block = blockIdx.x;

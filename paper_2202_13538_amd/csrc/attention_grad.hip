@@ -15,7 +15,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTileRows = 64;      // streamed rows of a tile
-constexpr int kChunksOfBias = 32;  // parts that the sums by distance are added up in
+constexpr int kMaxima = 1024;      // workgroups that look for the largest |dout|, at most
+constexpr int kDiagonals = 48;     // distances between 16 query rows and 32 keys (47), a row of LDS
 
 struct GradArgs {
     const char *dout = nullptr, *out = nullptr;  // [n_q][heads][dim]
@@ -23,58 +24,80 @@ struct GradArgs {
     char *dq = nullptr, *dk = nullptr, *dv = nullptr;
     void* dbias = nullptr;
     float *lse2 = nullptr, *delta = nullptr;  // [heads][n_q]: lse in units of log 2
-    uint32_t* largest = nullptr;              // of |dout|, as a float's bits (fp16 only)
+    float* maxima = nullptr;                  // [n_maxima], of parts of |dout| (fp16 only)
     float* by_distance = nullptr;             // [heads][tiles][2 reach + 1]: ds of a tile of keys
-    float* by_part = nullptr;                 // [heads][kChunksOfBias][2 reach + 1]
+    int n_maxima = 0;
     int q_tiles = 0, k_tiles = 0;
     int across_q = 0, across_k = 0;
     int twice = 0;                            // delta from the weights themselves, see attention_dq_kernel
 };
 
-__global__ void clear_word_kernel(uint32_t* word) { *word = 0; }
-
 __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* dst, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) dst[i] = 0;
 }
 
-// delta and lse by head, so that a tile's 64 rows lie behind one another.  16 lanes a row and head.
+// delta and lse by head, so that a tile's 64 rows lie behind one another (unless `twice`), and the largest |dout|.
+// 16 lanes a row and head, four of these at a time.
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(AttentionArgs a, GradArgs w) {
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    constexpr int kEach = 4, kRows = kThreads / 16;
+    __shared__ float most_of[kThreads / 64];
+    const int64_t n_rows = (int64_t)a.n_q * a.heads;
     const int c = threadIdx.x & 15;
-    const bool counts = row < (int64_t)a.n_q * a.heads;
-    float sum = 0.f, most = 0.f;
-    if (counts && c * 8 < a.dim) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(w.dout + (row * a.dim + c * 8) * 2);
-        const u32x4 y = *reinterpret_cast<const u32x4*>(w.out + (row * a.dim + c * 8) * 2);
+    float most = 0.f;
+    for (int64_t first = (int64_t)blockIdx.x * kRows * kEach; first < n_rows; first += (int64_t)gridDim.x * kRows * kEach) {
+        u32x4 x[kEach], y[kEach];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const f32x2 p = unpack2<T>(x[e]), q = unpack2<T>(y[e]);
-            sum = __builtin_fmaf(p[0], q[0], __builtin_fmaf(p[1], q[1], sum));
-            most = fmaxf(most, fmaxf(fabsf(p[0]), fabsf(p[1])));
+        for (int n = 0; n < kEach; ++n) {
+            const int64_t row = first + n * kRows + (threadIdx.x >> 4);
+            x[n] = y[n] = u32x4{0, 0, 0, 0};
+            if (row < n_rows && c * 8 < a.dim) {
+                x[n] = *reinterpret_cast<const u32x4*>(w.dout + (row * a.dim + c * 8) * 2);
+                if (!w.twice) y[n] = *reinterpret_cast<const u32x4*>(w.out + (row * a.dim + c * 8) * 2);
+            }
         }
-    }
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m);
-    if (counts && c == 0) {
-        const int64_t t = row / a.heads, at = (row % a.heads) * a.n_q + t;
-        w.delta[at] = sum;
-        w.lse2[at] = w.lse[row] * kLog2e;
+        for (int n = 0; n < kEach; ++n) {
+            const int64_t row = first + n * kRows + (threadIdx.x >> 4);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x2 p = unpack2<T>(x[n][e]), q = unpack2<T>(y[n][e]);
+                sum = __builtin_fmaf(p[0], q[0], __builtin_fmaf(p[1], q[1], sum));
+                most = fmaxf(most, fmaxf(fabsf(p[0]), fabsf(p[1])));
+            }
+            if (w.twice) continue;
+#pragma unroll
+            for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m);
+            if (row < n_rows && c == 0) {
+                const int64_t at = (row % a.heads) * a.n_q + row / a.heads;
+                w.delta[at] = sum;
+                w.lse2[at] = w.lse[row] * kLog2e;
+            }
+        }
     }
     if (T::kNarrow) {
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-        if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(w.largest, __float_as_uint(most));
+        if ((threadIdx.x & 63) == 0) most_of[threadIdx.x >> 6] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) w.maxima[blockIdx.x] = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
     }
 }
 
 // What ds is multiplied by before it is rounded to fp16, a power of two: the largest |dout| becomes
 // 1/2 .. 1, so that a loss's small gradients do not fall below what fp16 can hold.  bf16 has the range
-// of 32-bit floats.
+// of 32-bit floats.  For all threads of a workgroup; `scratch` holds 4 words of LDS.
 template <class T>
-__device__ __forceinline__ int lift_of(const GradArgs& w) {
+__device__ __forceinline__ int lift_of(const GradArgs& w, float* scratch, int tid) {
     if (!T::kNarrow) return 0;
-    const float most = __uint_as_float(*w.largest);
+    float most = 0.f;
+    for (int i = tid; i < w.n_maxima; i += kThreads) most = fmaxf(most, w.maxima[i]);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+    if ((tid & 63) == 0) scratch[tid >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3]));
     if (!(most > 0.f) || !(most < INFINITY)) return 0;
     return min(max(-1 - ilogbf(most), -60), 60);
 }
@@ -87,14 +110,15 @@ __device__ __forceinline__ int lift_of(const GradArgs& w) {
 // large as that of rounding ds, and the keys are there again at once: their ds are summed up in a round of
 // its own first (`twice`; walks of 16 steps, 262,144 rows of 8 heads of 64 elements: dq 0.0029 -> 0.0024 off).
 template <class T, int DP>
-__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(AttentionArgs a, GradArgs w) {
+__global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_dq_kernel(AttentionArgs a, GradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes;
     extern __shared__ __align__(16) char lds[];
     __shared__ int range[2][4];
+    __shared__ float maxima[4];
     char* const k_tile = lds;
     char* const v_tile = lds + 2 * kTileBytes;
     float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
 
     const int head = blockIdx.x % a.heads;
     const int block = blockIdx.x / a.heads, tile_no = a.causal ? w.q_tiles - 1 - block : block;
@@ -126,9 +150,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(AttentionArgs
     Stationary<DP> q, dout;
     q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
     dout.load(w.dout + ((int64_t)token * a.heads + head) * a.dim * 2, counts, a.dim, lane);
-    const float lse2 = counts ? w.lse2[(int64_t)head * a.n_q + token] : 0.f;
-    float delta = counts ? w.delta[(int64_t)head * a.n_q + token] : 0.f;
-    const int lift = lift_of<T>(w);
+    const int64_t by_head = (int64_t)head * a.n_q + token;
+    float lse2 = 0.f, delta = 0.f;
+    if (counts) {
+        if (w.twice) lse2 = w.lse[(int64_t)token * a.heads + head] * kLog2e;
+        else lse2 = w.lse2[by_head], delta = w.delta[by_head];
+    }
+    const int lift = lift_of<T>(w, maxima, tid);
     const float c = a.scale * kLog2e, base = lse2 - (float)lift;   // ds comes out lifted
     float bias_behind = 0.f, bias_ahead = 0.f;
     if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
@@ -188,7 +216,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(AttentionArgs
         delta += ldexpf(sum + from_other_half(sum), -lift);
         sum = 0.f;
     }
-    if (sees && g == 0) w.delta[(int64_t)head * a.n_q + token] = delta;
+    if (counts && g == 0) {
+        w.delta[by_head] = delta;
+        if (w.twice) w.lse2[by_head] = lse2;
+    }
     if (__any(has_nan(acc))) {   // once more, without what a row does not see
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
@@ -208,23 +239,29 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(AttentionArgs
                       });
 }
 
-// dk and dv of 128 keys of one key head, 32 a wave, over the query rows of all heads of its group, and the sums of
+// dk and dv of 32 WR keys of one key head, 32 a wave, over the query rows of all heads of its group, and the sums of
 // ds by distance.
-template <class T, int DP>
+//   WR = 4: 128 keys, every wave takes all rows of a tile;
+//   WR = 2: 64 keys for twice as many workgroups: two waves share keys, take every other 32 rows, and add their
+//           sums up at the end.
+template <class T, int DP, int WR>
 __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kernel(AttentionArgs a, GradArgs w) {
-    constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes;
+    constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes, WK = 4 / WR;
     extern __shared__ __align__(16) char lds[];
     __shared__ int range[2][4];
-    __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][lse, delta][row]
+    __shared__ float maxima[4];
+    __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][-lse / scale, -delta][row]
     char* const q_tile = lds;
     char* const o_tile = lds + 2 * kTileBytes;
     const int width = 2 * a.reach + 1;
-    float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);   // [width], then the waves' sums [4][width]
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);   // [width], the waves' sums [4][width], then
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int wr = wave % WR, wk = wave / WR;
+    float* const sums = bias + (1 + wave) * width;
+    float* const diagonals = bias + 5 * width + wave * 16 * kDiagonals;   // [4][16][kDiagonals]
 
     const int kv_head = blockIdx.x % a.kv_heads, tile_no = blockIdx.x / a.kv_heads;
-    const TileOfRows tile = tile_of_rows(a.k_off, a.n_seqs, a.n_k, 128, w.across_k, tile_no);
-    float* const sums = bias + (1 + wave) * width;
+    const TileOfRows tile = tile_of_rows(a.k_off, a.n_seqs, a.n_k, 32 * WR, w.across_k, tile_no);
     auto by_distance = [&](int head) { return w.by_distance + ((int64_t)head * w.k_tiles + tile_no) * width; };
     const int group = a.heads / a.kv_heads;
     if (tile.first >= tile.last) {
@@ -234,7 +271,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         return;
     }
     // the lane's key, the query rows that see it (lo <= t < hi), and `place`: a row t is place - t away
-    const int key = tile.first + 32 * wave + col;
+    const int key0 = tile.first + 32 * wr, key = key0 + col;
     const bool counts = key < tile.last;
     int lo = 0, hi = 0, place = 0;
     if (counts) {
@@ -249,7 +286,10 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
     const int all_lo = wave_max(counts ? lo : 0), all_hi = wave_min(counts ? hi : 0x7FFFFFFF);
     const int place_min = wave_min(counts ? place : 0x7FFFFFFF), place_max = wave_max(counts ? place : -0x3FFFFFFF);
+    const int place0 = place_min;   // of the wave's first key: the others' lie behind it one by one
     if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
+    if (a.bias != nullptr)
+        for (int i = tid; i < 4 * 16 * kDiagonals; i += kThreads) bias[5 * width + i] = 0.f;
     __syncthreads();
     int row_begin = 0x7FFFFFFF, row_end = 0;
 #pragma unroll
@@ -258,132 +298,136 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     Stationary<DP> k, v;
     k.load(a.k + (int64_t)key * a.k_row + (int64_t)kv_head * a.k_head, counts, a.dim, lane);
     v.load(a.v + (int64_t)key * a.v_row + (int64_t)kv_head * a.v_head, counts, a.dim, lane);
-    const int lift = lift_of<T>(w);
+    const int lift = lift_of<T>(w, maxima, tid);
     const float c = a.scale * kLog2e, up = ldexpf(1.f, lift);
 
     f32x16 dk[NB], dv[NB];
 #pragma unroll
     for (int db = 0; db < NB; ++db) dk[db] = dv[db] = f32x16{};
-    if (row_begin < row_end) {
 #pragma unroll 1
-        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h) {
-            const char* const q_src = a.q + (int64_t)h * a.q_head;
-            const char* const o_src = w.dout + (int64_t)h * a.dim * 2;
-            const uint32_t o_row = (uint32_t)a.heads * a.dim * 2;
-            const float* const stat_src = (tid < kTileRows ? w.lse2 : w.delta) + (int64_t)h * a.n_q;
-            float stat = 0.f;
-            auto fetch = [&](int row, int buffer) {
-                const int rows = row_end - row;
-                copy_tile<DP, kTileRows, kThreads>(q_tile + buffer * kTileBytes, q_src + (int64_t)row * a.q_row, a.q_row, rows, a.dim, tid);
-                copy_tile<DP, kTileRows, kThreads>(o_tile + buffer * kTileBytes, o_src + (int64_t)row * o_row, o_row, rows, a.dim, tid);
-                if (tid < 2 * kTileRows) stat = stat_src[min(row + (tid & (kTileRows - 1)), row_end - 1)];
-            };
-            auto keep = [&](int buffer) {
-                if (tid < 2 * kTileRows) stats[buffer][tid / kTileRows][tid & (kTileRows - 1)] = stat;
-            };
+    for (int h = kv_head * group; h < (kv_head + 1) * group; ++h) {
+        const char* const q_src = a.q + (int64_t)h * a.q_head;
+        const char* const o_src = w.dout + (int64_t)h * a.dim * 2;
+        const uint32_t o_row = (uint32_t)a.heads * a.dim * 2;
+        const float* const stat_src = (tid < kTileRows ? w.lse2 : w.delta) + (int64_t)h * a.n_q;
+        const float stat_times = tid < kTileRows ? -1.f / c : -1.f;
+        float stat = 0.f;
+        auto fetch = [&](int row, int buffer) {
+            const int rows = row_end - row;
+            copy_tile<DP, kTileRows, kThreads>(q_tile + buffer * kTileBytes, q_src + (int64_t)row * a.q_row, a.q_row, rows, a.dim, tid);
+            copy_tile<DP, kTileRows, kThreads>(o_tile + buffer * kTileBytes, o_src + (int64_t)row * o_row, o_row, rows, a.dim, tid);
+            if (tid < 2 * kTileRows) stat = stat_src[min(row + (tid & (kTileRows - 1)), row_end - 1)];
+        };
+        auto keep = [&](int buffer) {
+            if (tid < 2 * kTileRows) stats[buffer][tid / kTileRows][tid & (kTileRows - 1)] = stat * stat_times;
+        };
+        if (row_begin < row_end) {
             fetch(row_begin, 0);
-            if (a.bias != nullptr) {
-                fill_bias<T>(bias, a, h, tid, kThreads);
-                for (int d = tid; d < 4 * width; d += kThreads) bias[width + d] = 0.f;
-            }
-            float sum_behind = 0.f, sum_ahead = 0.f;   // of ds, distances of reach and more
             keep(0);
+        }
+        if (a.bias != nullptr) {
+            fill_bias<T>(bias, a, h, tid, kThreads);
+            for (int d = tid; d < 4 * width; d += kThreads) bias[width + d] = 0.f;
+        }
+        float sum_behind = 0.f, sum_ahead = 0.f;   // of ds, distances of reach and more
+        tile_arrived();
+        __syncthreads();
+        float bias_behind = 0.f, bias_ahead = 0.f;
+        if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
+        int buffer = 0;
+#pragma unroll 1
+        for (int row = row_begin; row < row_end; row += kTileRows, buffer ^= 1) {
+            const bool more = row + kTileRows < row_end;
+            if (more) fetch(row + kTileRows, buffer ^ 1);
+#pragma unroll 1
+            for (int b = 32 * wk; b < kTileRows; b += 32 * WK) {
+                const int row0 = row + b;
+                if (row0 >= wave_hi || row0 + 32 <= wave_lo) continue;
+                const char* const qt = q_tile + buffer * kTileBytes + b * Tile<DP>::kRowBytes;
+                const char* const ot = o_tile + buffer * kTileBytes + b * Tile<DP>::kRowBytes;
+                // (products start from -lse / scale and -delta, so that these need neither registers nor additions)
+                f32x16 p = scores<T, DP>(qt, 0, k, lane, by_row(&stats[buffer][0][b], g));
+                f32x16 ds = scores<T, DP>(ot, 0, v, lane, by_row(&stats[buffer][1][b], g));
+                const bool whole = row0 >= all_lo && row0 + 32 <= all_hi;
+                const bool behind = place_max - row0 <= -a.reach, ahead = place_min - (row0 + 31) >= a.reach;
+                const bool plain = whole && (a.bias == nullptr || behind || ahead);
+                if (plain) {
+                    const float add = behind ? bias_behind : bias_ahead;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(p[i], c, add);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int t = row0 + row_of(i, g);
+                        float add = 0.f;
+                        if (a.bias != nullptr) add = bias[min(max(place - t, -a.reach), a.reach) + a.reach];
+                        const bool seen = t >= lo && t < hi;
+                        p[i] = seen ? __builtin_fmaf(p[i], c, add) : -INFINITY;
+                        ds[i] = seen ? ds[i] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[i] = exp2_fast(p[i]);
+                    ds[i] *= p[i];
+                }
+                if (a.bias != nullptr) {
+                    if (plain) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum += ds[i];
+                        sum = counts ? sum : 0.f;
+                        if (behind) sum_behind += sum;
+                        else sum_ahead += sum;
+                    } else {
+                        // Neighbouring keys lie at neighbouring places, so 16 rows' ds, each row moved one place
+                        // against the one before, have a distance a column: every lane adds one up.  (Adding every
+                        // element to its distance's sum with LDS atomics takes 30 cycles for 32 lanes.)  The
+                        // corners that no ds falls on stay zero.
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int t = row_of(e, g);
+                                diagonals[t * kDiagonals + col - t + 15] = ds[8 * half + e];
+                            }
+                            wave_sync();
+                            if (lane < kDiagonals - 1) {
+                                float sum = 0.f;
+#pragma unroll
+                                for (int t = 0; t < 16; ++t) sum += diagonals[t * kDiagonals + lane];
+                                const int d = place0 + lane - 15 - (row0 + 16 * half);
+                                if (d <= -a.reach) sum_behind += sum;
+                                else if (d >= a.reach) sum_ahead += sum;
+                                else sums[d + a.reach] += sum;
+                            }
+                            wave_sync();
+                        }
+                    }
+                }
+                if (T::kNarrow) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ds[i] *= up;
+                }
+                accumulate<T, DP>(dv, ot, 0, p, lane);    // (p and ds rounded to the inputs' 16 bits)
+                accumulate<T, DP>(dk, qt, 0, ds, lane);
+            }
+            if (more) keep(buffer ^ 1);
             tile_arrived();
             __syncthreads();
-            float bias_behind = 0.f, bias_ahead = 0.f;
-            if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
-            int buffer = 0;
-#pragma unroll 1
-            for (int row = row_begin; row < row_end; row += kTileRows, buffer ^= 1) {
-                const bool more = row + kTileRows < row_end;
-                if (more) fetch(row + kTileRows, buffer ^ 1);
-                const char* const qt = q_tile + buffer * kTileBytes;
-                const char* const ot = o_tile + buffer * kTileBytes;
-#pragma unroll
-                for (int b = 0; b < kTileRows; b += 32) {
-                    const int row0 = row + b;
-                    if (row0 >= wave_hi || row0 + 32 <= wave_lo) continue;
-                    f32x16 p = scores<T, DP>(qt, b, k, lane);
-                    f32x16 ds = scores<T, DP>(ot, b, v, lane);
-                    f32x4 lse2[4], delta[4];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        lse2[n] = *reinterpret_cast<const f32x4*>(&stats[buffer][0][b + 8 * n + 4 * g]);
-                        delta[n] = *reinterpret_cast<const f32x4*>(&stats[buffer][1][b + 8 * n + 4 * g]);
-                    }
-                    const bool whole = row0 >= all_lo && row0 + 32 <= all_hi;
-                    const bool behind = place_max - row0 <= -a.reach, ahead = place_min - (row0 + 31) >= a.reach;
-                    if (whole && (a.bias == nullptr || behind || ahead)) {
-                        const float add = behind ? bias_behind : bias_ahead;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            p[i] = exp2_fast(__builtin_fmaf(p[i], c, add - lse2[i >> 2][i & 3]));
-                            ds[i] = p[i] * (ds[i] - delta[i >> 2][i & 3]);
-                        }
-                        if (a.bias != nullptr) {
-                            float sum = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) sum += ds[i];
-                            if (behind) sum_behind += sum;
-                            else sum_ahead += sum;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int t = row0 + row_of(i, g);
-                            float add = 0.f;
-                            if (a.bias != nullptr) add = bias[min(max(place - t, -a.reach), a.reach) + a.reach];
-                            const bool seen = t >= lo && t < hi;
-                            p[i] = seen ? exp2_fast(__builtin_fmaf(p[i], c, add - lse2[i >> 2][i & 3])) : 0.f;
-                            ds[i] = seen ? p[i] * (ds[i] - delta[i >> 2][i & 3]) : 0.f;
-                        }
-                        if (a.bias != nullptr) {
-                            // a distance is met by one key of a half: a tile's keys lie at different places.  The
-                            // halves take turns, so no two lanes add to one place at a time, and the order is
-                            // fixed.
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                if (g == half && counts) {
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        const int d = place - (row0 + row_of(i, g));
-                                        if (d <= -a.reach) sum_behind += ds[i];
-                                        else if (d >= a.reach) sum_ahead += ds[i];
-                                        else __hip_atomic_fetch_add(&sums[d + a.reach], ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                                    }
-                                }
-                                wave_sync();
-                            }
-                        }
-                    }
-                    if (T::kNarrow) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) ds[i] *= up;
-                    }
-                    accumulate<T, DP>(dv, ot, b, p, lane);    // (p and ds rounded to the inputs' 16 bits)
-                    accumulate<T, DP>(dk, qt, b, ds, lane);
-                }
-                if (more) keep(buffer ^ 1);
-                tile_arrived();
-                __syncthreads();
-            }
-            if (a.bias != nullptr) {
-                if (!counts) sum_behind = sum_ahead = 0.f;
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1) sum_behind += __shfl_xor(sum_behind, m), sum_ahead += __shfl_xor(sum_ahead, m);
-                if (lane == 0) {
-                    if (a.reach == 0) sums[0] = sum_behind + sum_ahead;
-                    else sums[0] = sum_behind, sums[2 * a.reach] = sum_ahead;
-                }
-                __syncthreads();
-                for (int d = tid; d < width; d += kThreads)
-                    by_distance(h)[d] = (bias[width + d] + bias[2 * width + d]) + (bias[3 * width + d] + bias[4 * width + d]);
-                __syncthreads();
-            }
         }
-    } else if (a.bias != nullptr) {
-        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
-            for (int d = tid; d < width; d += kThreads) by_distance(h)[d] = 0.f;
+        if (a.bias != nullptr) {
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) sum_behind += __shfl_xor(sum_behind, m), sum_ahead += __shfl_xor(sum_ahead, m);
+            if (lane == 0) {
+                if (a.reach == 0) sums[0] = sum_behind + sum_ahead;
+                else sums[0] = sum_behind, sums[2 * a.reach] = sum_ahead;
+            }
+            __syncthreads();
+            for (int d = tid; d < width; d += kThreads)
+                by_distance(h)[d] = (bias[width + d] + bias[2 * width + d]) + (bias[3 * width + d] + bias[4 * width + d]);
+            __syncthreads();
+        }
     }
     if (__any(has_nan(dk) || has_nan(dv))) {   // once more, without rows that do not see the key
 #pragma unroll
@@ -392,6 +436,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
 #pragma unroll 1
             for (int t = wave_lo; t < wave_hi; ++t) {
+                if (WK > 1 && ((t - row_begin) >> 5) % WK != wk) continue;
                 const char* const q_row = a.q + (int64_t)t * a.q_row + (int64_t)h * a.q_head;
                 const char* const o_row = w.dout + ((int64_t)t * a.heads + h) * a.dim * 2;
                 const float dot = dot_row<T, DP>(k, q_row, a.dim, lane), dp = dot_row<T, DP>(v, o_row, a.dim, lane);
@@ -409,55 +454,86 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                 }
             }
     }
+    if (WK > 1) {   // the second wave of a pair to the first
+        float* const there = reinterpret_cast<float*>(lds) + wr * 2 * NB * 16 * 64 + lane;   // [WR][2 NB 16][64]
+        __syncthreads();
+        if (wk == 1) {
+#pragma unroll
+            for (int db = 0; db < NB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    there[(db * 16 + i) * 64] = dk[db][i];
+                    there[((NB + db) * 16 + i) * 64] = dv[db][i];
+                }
+        }
+        __syncthreads();
+        if (wk == 0) {
+#pragma unroll
+            for (int db = 0; db < NB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    dk[db][i] += there[(db * 16 + i) * 64];
+                    dv[db][i] += there[((NB + db) * 16 + i) * 64];
+                }
+        }
+        __syncthreads();
+        if (wk == 1) return;
+    }
     auto row_of_key = [&](char* rows) {
         return [=](int r) -> char* {
-            const int there = tile.first + 32 * wave + r;
+            const int there = key0 + r;
             return there < tile.last ? rows + ((int64_t)there * a.kv_heads + kv_head) * a.dim * 2 : nullptr;
         };
     };
-    char* const mine = lds + wave * 32 * Tile<DP>::kRowBytes;
+    char* const mine = lds + wr * 32 * Tile<DP>::kRowBytes;
     store_rows<T, DP>(dk, ldexpf(a.scale, -lift), !sees, mine, a.dim, lane, row_of_key(w.dk));
     store_rows<T, DP>(dv, 1.f, !sees, mine, a.dim, lane, row_of_key(w.dv));
 }
 
-// Sums by distance of a part of a head's tiles.
-__global__ __launch_bounds__(kThreads) void attention_dbias_parts_kernel(GradArgs w, int width) {
-    const int head = blockIdx.x / kChunksOfBias, part = blockIdx.x % kChunksOfBias;
-    const int each = (w.k_tiles + kChunksOfBias - 1) / kChunksOfBias;
-    const int first = min(part * each, w.k_tiles), last = min(first + each, w.k_tiles);
-    for (int d = threadIdx.x; d < width; d += kThreads) {
-        float sum = 0.f;
-        for (int t = first; t < last; ++t) sum += w.by_distance[((int64_t)head * w.k_tiles + t) * width + d];
-        w.by_part[((int64_t)head * kChunksOfBias + part) * width + d] = sum;
-    }
-}
-
-// A head's buckets: the parts of every distance, then the distances of every bucket, in order.
+// A head's buckets: the tiles' sums of every distance, then the distances of every bucket, in a fixed order.
+constexpr int kBiasThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kThreads) void attention_dbias_kernel(AttentionArgs a, GradArgs w) {
+__global__ __launch_bounds__(kBiasThreads) void attention_dbias_kernel(AttentionArgs a, GradArgs w) {
+    __shared__ float part[kBiasThreads];
     __shared__ float sums[2 * 1024 + 1];
     __shared__ int bucket[2 * 1024 + 1];
-    const int width = 2 * a.reach + 1, head = blockIdx.x;
-    for (int d = threadIdx.x; d < width; d += kThreads) {
+    const int width = 2 * a.reach + 1, head = blockIdx.x, tid = threadIdx.x;
+    // threads: as many distances as there are, up to 256 at a time, times slices of the tiles
+    int across = 16;
+    while (across < 256 && across < width) across *= 2;
+    const int slices = kBiasThreads / across, slice = tid / across;
+    for (int d0 = 0; d0 < width; d0 += across) {
+        const int d = d0 + tid % across;
         float sum = 0.f;
-        for (int p = 0; p < kChunksOfBias; ++p) sum += w.by_part[((int64_t)head * kChunksOfBias + p) * width + d];
-        sums[d] = sum;
-        const int b = a.bucket[d];
-        bucket[d] = b < 0 || b >= a.n_buckets ? 0 : b;
+        if (d < width) {
+#pragma unroll 8
+            for (int t = slice; t < w.k_tiles; t += slices) sum += w.by_distance[((int64_t)head * w.k_tiles + t) * width + d];
+        }
+        part[tid] = sum;
+        __syncthreads();
+        if (slice == 0 && d < width) {
+            for (int s = 1; s < slices; ++s) sum += part[s * across + tid];
+            sums[d] = sum;
+            const int b = a.bucket[d];
+            bucket[d] = b < 0 || b >= a.n_buckets ? 0 : b;
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int b = threadIdx.x; b < a.n_buckets; b += kThreads) {
+    for (int b = tid >> 6; b < a.n_buckets; b += kBiasThreads / 64) {
         float sum = 0.f;
-        for (int d = 0; d < width; ++d) sum += bucket[d] == b ? sums[d] : 0.f;
-        static_cast<typename T::elem*>(w.dbias)[(int64_t)b * a.heads + head] = (typename T::elem)sum;
+        for (int d = tid & 63; d < width; d += 64) sum += bucket[d] == b ? sums[d] : 0.f;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+        if ((tid & 63) == 0) static_cast<typename T::elem*>(w.dbias)[(int64_t)b * a.heads + head] = (typename T::elem)sum;
     }
 }
 
 struct GradPlan {
     bool across_q, across_k, twice;
+    int keys;   // of a tile
     int64_t q_tiles, k_tiles;
 };
-GradPlan grad_plan(const AttentionArgs& a) {
+GradPlan grad_plan(const AttentionArgs& a, int n_cu) {
     GradPlan p;
     const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
     // Tiles across sequences where these are short and alike.  With a bias the keys of a tile have to lie at
@@ -466,56 +542,56 @@ GradPlan grad_plan(const AttentionArgs& a) {
     p.across_k = mean_k < 128 && mean_q <= 256 && mean_q <= 2 * mean_k && (a.bias == nullptr || a.q_off == a.k_off);
     p.twice = mean_k <= 256;
     p.q_tiles = tiles_of_rows(a.n_seqs, a.n_q, 128, p.across_q);
-    p.k_tiles = tiles_of_rows(a.n_seqs, a.n_k, 128, p.across_k);
+    p.keys = 128;
+    if (a.kv_heads * ((double)a.n_k / 128 + (p.across_k ? 0 : 0.5 * a.n_seqs)) < 8 * n_cu) p.keys = 64;
+    p.k_tiles = tiles_of_rows(a.n_seqs, a.n_k, p.keys, p.across_k);
     return p;
 }
 
 size_t aligned(size_t x) { return (x + 255) / 256 * 256; }
 
+hipError_t allow_lds(const void* kernel, size_t bytes) {
+    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <class T, int DP, int WR>
+hipError_t launch_dkv(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p, size_t bytes) {
+    auto kernel = attention_dkv_kernel<T, DP, WR>;
+    const hipError_t rc = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
+    if (rc != hipSuccess) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.k_tiles * a.kv_heads)), dim3(kThreads), bytes, stream, a, w);
+    return hipGetLastError();
+}
+
 template <class T, int DP>
 hipError_t launch_width(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
     const size_t tiles = 4 * (size_t)kTileRows * Tile<DP>::kRowBytes;
     const size_t width = a.bias != nullptr ? 2 * (size_t)a.reach + 1 : 0;
-    auto allow = [](const void* kernel, size_t bytes) {
-        return bytes <= 65536 ? hipSuccess
-                              : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    };
-    {
-        const size_t bytes = tiles + width * sizeof(float);
-        hipError_t rc = allow(reinterpret_cast<const void*>(attention_dq_kernel<T, DP>), bytes);
-        if (rc != hipSuccess) return rc;
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP>), dim3((unsigned)(p.q_tiles * a.heads)), dim3(kThreads), bytes,
-                           stream, a, w);
-        if ((rc = hipGetLastError()) != hipSuccess) return rc;
-    }
-    {
-        const size_t bytes = tiles + 5 * width * sizeof(float);
-        hipError_t rc = allow(reinterpret_cast<const void*>(attention_dkv_kernel<T, DP>), bytes);
-        if (rc != hipSuccess) return rc;
-        hipLaunchKernelGGL((attention_dkv_kernel<T, DP>), dim3((unsigned)(p.k_tiles * a.kv_heads)), dim3(kThreads), bytes,
-                           stream, a, w);
-        if ((rc = hipGetLastError()) != hipSuccess) return rc;
-    }
-    return hipSuccess;
+    auto kernel = attention_dq_kernel<T, DP>;
+    const size_t bytes = tiles + width * sizeof(float);
+    hipError_t rc = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
+    if (rc != hipSuccess) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.q_tiles * a.heads)), dim3(kThreads), bytes, stream, a, w);
+    if ((rc = hipGetLastError()) != hipSuccess) return rc;
+    const size_t sums = width == 0 ? 0 : (5 * width + 4 * 16 * kDiagonals) * sizeof(float);
+    return p.keys == 64 ? launch_dkv<T, DP, 2>(stream, a, w, p, tiles + sums) : launch_dkv<T, DP, 4>(stream, a, w, p, tiles + sums);
 }
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
     if (p.q_tiles * a.heads > 0x7FFFFFFF || p.k_tiles * a.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
-    const int64_t rows = (int64_t)a.n_q * a.heads;
-    if (T::kNarrow) hipLaunchKernelGGL(clear_word_kernel, dim3(1), dim3(1), 0, stream, w.largest);
-    hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)((rows + kThreads / 16 - 1) / (kThreads / 16))),
-                       dim3(kThreads), 0, stream, a, w);
-    hipError_t rc = hipGetLastError();
+    hipError_t rc = hipSuccess;
+    if (T::kNarrow || !p.twice) {
+        hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)w.n_maxima), dim3(kThreads), 0, stream, a, w);
+        rc = hipGetLastError();
+    }
     if (rc != hipSuccess) return rc;
     rc = a.dim <= 32   ? launch_width<T, 32>(stream, a, w, p)
          : a.dim <= 64 ? launch_width<T, 64>(stream, a, w, p)
          : a.dim <= 96 ? launch_width<T, 96>(stream, a, w, p)
                        : launch_width<T, 128>(stream, a, w, p);
     if (rc != hipSuccess || a.bias == nullptr) return rc;
-    hipLaunchKernelGGL(attention_dbias_parts_kernel, dim3((unsigned)(a.heads * kChunksOfBias)), dim3(kThreads), 0, stream, w,
-                       2 * a.reach + 1);
-    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)a.heads), dim3(kThreads), 0, stream, a, w);
+    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)a.heads), dim3(kBiasThreads), 0, stream, a, w);
     return hipGetLastError();
 }
 
@@ -531,9 +607,8 @@ size_t lay_out(const AttentionArgs& a, const GradPlan& p, char* scratch, GradArg
     const size_t width = a.bias != nullptr ? (2 * (size_t)a.reach + 1) * sizeof(float) : 0;
     w->lse2 = reinterpret_cast<float*>(take(rows));
     w->delta = reinterpret_cast<float*>(take(rows));
-    w->largest = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+    w->maxima = reinterpret_cast<float*>(take(kMaxima * sizeof(float)));
     w->by_distance = reinterpret_cast<float*>(take((size_t)p.k_tiles * a.heads * width));
-    w->by_part = reinterpret_cast<float*>(take((size_t)kChunksOfBias * a.heads * width));
     return at;
 }
 
@@ -547,14 +622,14 @@ hipError_t launch_zero(hipStream_t stream, void* dst, int64_t n) {
     return hipGetLastError();
 }
 
-size_t attention_grad_scratch_bytes(const AttentionArgs& a) {
+size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a) {
     GradArgs w;
-    return lay_out(a, grad_plan(a), nullptr, &w);
+    return lay_out(a, grad_plan(a, n_cu), nullptr, &w);
 }
 
-hipError_t launch_attention_grad(hipStream_t stream, const AttentionArgs& a, bool half, const void* dout, const void* out,
+hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, const void* dout, const void* out,
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch) {
-    const GradPlan p = grad_plan(a);
+    const GradPlan p = grad_plan(a, n_cu);
     GradArgs w;
     lay_out(a, p, static_cast<char*>(scratch), &w);
     w.dout = static_cast<const char*>(dout);
@@ -569,6 +644,8 @@ hipError_t launch_attention_grad(hipStream_t stream, const AttentionArgs& a, boo
     w.across_q = p.across_q;
     w.across_k = p.across_k;
     w.twice = p.twice;
+    const int64_t blocks = ((int64_t)a.n_q * a.heads + 63) / 64;   // of the kernel that goes over the rows
+    w.n_maxima = (int)(blocks < kMaxima ? blocks : kMaxima);
     return half ? launch_type<Fp16>(stream, a, w, p) : launch_type<Bf16>(stream, a, w, p);
 }
 

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
     using Shape = LossShape<DP, WR>;
     constexpr int RB = Shape::RB;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int split = blockIdx.x % o.splits, row_tile = blockIdx.x / o.splits;
     const int first = row_tile * Shape::kRows + (WR == 1 ? 0 : wave * 32 * RB), wk = WR == 1 ? wave : 0;
 

@@ -52,7 +52,7 @@ template <class T, int DP>
 __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(LossArgs a, LossGradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int split = blockIdx.x % w.splits_h, first = blockIdx.x / w.splits_h * 128 + wave * 32, row = first + col;
     const bool in = row < a.n_rows, works = first < a.n_rows;
     Stationary<DP> h;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(Los
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) float stats[2][2][kStep];   // [buffer][lse, dloss][row]
     __shared__ __align__(16) int labels[2][kStep];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, col = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int split = blockIdx.x % w.splits_w, first = blockIdx.x / w.splits_w * 128 + wave * 32, cls = first + col;
     const bool in = cls < a.n_classes, works = first < a.n_classes;
     Stationary<DP> c;

@@ -54,6 +54,12 @@ struct Fp16 {
     }
 };
 
+// The thread's wave, and what is the same in all of its lanes, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x)));
+}
+
 // Two 32-bit values rounded to nearest, in one word.
 template <class T>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -139,12 +145,13 @@ __device__ __forceinline__ void copy_tile(char* tile, const char* src, uint32_t 
     static_assert(kEach * THREADS == ROWS * kChunks, "the tile is not a multiple of the threads");
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef const __attribute__((address_space(1))) void* global_ptr;
+    char* const mine = tile + uniform(tid & ~63) * 16;
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
         const int id = tid + n * THREADS, row = id / kChunks;
         const int c = (id % kChunks) ^ Tile<DP>::permuted(row);
         const uint32_t at = (uint32_t)min(row, rows - 1) * row_bytes + (c * 8 < dim ? c * 16 : 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)(src + at), (lds_ptr)(tile + (id & ~63) * 16), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(src + at), (lds_ptr)(mine + n * THREADS * 16), 16, 0, 0);
     }
 }
 __device__ __forceinline__ void tile_arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt(0)
@@ -164,12 +171,23 @@ struct Stationary {
     }
 };
 
-// C[32 streamed rows from row0][32 stationary rows] of a tile.
+// C[32 streamed rows from row0][32 stationary rows] of a tile, on top of c.
 template <class T, int DP>
-__device__ __forceinline__ f32x16 scores(const char* tile, int row0, const Stationary<DP>& b, int lane) {
-    f32x16 c = {};
+__device__ __forceinline__ f32x16 scores(const char* tile, int row0, const Stationary<DP>& b, int lane, f32x16 c = {}) {
 #pragma unroll
     for (int ks = 0; ks < DP / 16; ++ks) c = T::mma(Tile<DP>::rows(tile, row0, ks, lane), b.k[ks], c);
+    return c;
+}
+
+// What is one value a streamed row, 32 of them from LDS, as the start of a product.
+__device__ __forceinline__ f32x16 by_row(const float* values, int g) {
+    f32x16 c;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(values + 8 * n + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[4 * n + e] = x[e];
+    }
     return c;
 }
 
