@@ -141,17 +141,16 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     tile_arrived();
     __syncthreads();
     const int last = min(hi, key_end);
-    int buffer = 0;
-#pragma unroll 1
-    for (int key = key_begin; key < key_end; key += Shape::kTileKeys, buffer ^= 1) {
+    alternate(key_begin, key_end, Shape::kTileKeys, [&](int key, auto of) __attribute__((always_inline)) {
+        constexpr int buffer = decltype(of)::value;
         if (key + Shape::kTileKeys < key_end) fetch(key + Shape::kTileKeys, buffer ^ 1);
         const int key0 = key + wk * Shape::kKeys;
         if (key0 < min(wave_hi, key_end) && key0 + Shape::kKeys > wave_lo) {
-            const char* const kt = k_tile + buffer * Shape::kTileBytes + wk * Shape::kKeys * Tile<DP>::kRowBytes;
-            const char* const vt = v_tile + buffer * Shape::kTileBytes + wk * Shape::kKeys * Tile<DP>::kRowBytes;
+            const uint32_t kt = buffer * Shape::kTileBytes + wk * Shape::kKeys * Tile<DP>::kRowBytes;
+            const uint32_t vt = kt + Shape::kBuffers * Shape::kTileBytes;
             f32x16 s[kBlocks];
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) s[b] = scores<T, DP>(kt, 32 * b, q, lane);
+            for (int b = 0; b < kBlocks; ++b) s[b] = scores<T, DP>(lds, kt + 32 * b * Tile<DP>::kRowBytes, q, lane);
             const bool whole = key0 >= all_lo && key0 + Shape::kKeys <= min(all_hi, key_end);
             const bool behind = key0 + Shape::kKeys - 1 - diag_min <= -a.reach, ahead = key0 - diag_max >= a.reach;
             if (whole && (a.bias == nullptr || behind || ahead)) {
@@ -186,11 +185,11 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
             // (weights are rounded to the inputs' 16 bits for the second product, the sum is of the
             // unrounded ones)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) accumulate<T, DP>(acc, vt, 32 * b, s[b], lane);
+            for (int b = 0; b < kBlocks; ++b) accumulate<T, DP>(acc, lds, vt + 32 * b * Tile<DP>::kRowBytes, s[b], lane);
         }
         tile_arrived();
         __syncthreads();
-    }
+    });
     sum += from_other_half(sum);
     if (__any(has_nan(acc))) {   // once more, without what a row does not see
 #pragma unroll

@@ -184,14 +184,13 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 #pragma unroll 1
         for (int key = key_begin; key < key_end; key += kTileRows, buffer ^= 1) {
             if (key + kTileRows < key_end) fetch(key + kTileRows, buffer ^ 1);
-            const char* const kt = k_tile + buffer * kTileBytes;
-            const char* const vt = v_tile + buffer * kTileBytes;
 #pragma unroll
             for (int b = 0; b < kTileRows; b += 32) {
                 const int key0 = key + b;
                 if (key0 >= wave_hi || key0 + 32 <= wave_lo) continue;
-                f32x16 s = scores<T, DP>(kt, b, q, lane);
-                const f32x16 dp = scores<T, DP>(vt, b, dout, lane);
+                const uint32_t kt = buffer * kTileBytes + b * Tile<DP>::kRowBytes, vt = kt + 2 * kTileBytes;
+                f32x16 s = scores<T, DP>(lds, kt, q, lane);
+                const f32x16 dp = scores<T, DP>(lds, vt, dout, lane);
                 const bool whole = key0 >= all_lo && key0 + 32 <= all_hi;
                 const bool behind = key0 + 31 - diag_min <= -a.reach, ahead = key0 - diag_max >= a.reach;
                 if (whole && (a.bias == nullptr || behind || ahead)) {
@@ -208,7 +207,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum += s[i];
-                if (round == 1) accumulate<T, DP>(acc, kt, b, s, lane);   // (ds rounded to the inputs' 16 bits)
+                if (round == 1) accumulate<T, DP>(acc, lds, kt, s, lane);   // (ds rounded to the inputs' 16 bits)
             }
             tile_arrived();
             __syncthreads();
@@ -309,17 +308,17 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         const char* const q_src = a.q + (int64_t)h * a.q_head;
         const char* const o_src = w.dout + (int64_t)h * a.dim * 2;
         const uint32_t o_row = (uint32_t)a.heads * a.dim * 2;
-        const float* const stat_src = (tid < kTileRows ? w.lse2 : w.delta) + (int64_t)h * a.n_q;
-        const float stat_times = tid < kTileRows ? -1.f / c : -1.f;
         float stat = 0.f;
         auto fetch = [&](int row, int buffer) {
-            const int rows = row_end - row;
-            copy_tile<DP, kTileRows, kThreads>(q_tile + buffer * kTileBytes, q_src + (int64_t)row * a.q_row, a.q_row, rows, a.dim, tid);
-            copy_tile<DP, kTileRows, kThreads>(o_tile + buffer * kTileBytes, o_src + (int64_t)row * o_row, o_row, rows, a.dim, tid);
-            if (tid < 2 * kTileRows) stat = stat_src[min(row + (tid & (kTileRows - 1)), row_end - 1)];
+            const int rows = row_end - row, t = tid;
+            copy_tile<DP, kTileRows, kThreads>(q_tile + buffer * kTileBytes, q_src + (int64_t)row * a.q_row, a.q_row, rows, a.dim, t);
+            copy_tile<DP, kTileRows, kThreads>(o_tile + buffer * kTileBytes, o_src + (int64_t)row * o_row, o_row, rows, a.dim, t);
+            if (t < 2 * kTileRows)
+                stat = (t < kTileRows ? w.lse2 : w.delta)[(int64_t)h * a.n_q + min(row + (t & (kTileRows - 1)), row_end - 1)];
         };
         auto keep = [&](int buffer) {
-            if (tid < 2 * kTileRows) stats[buffer][tid / kTileRows][tid & (kTileRows - 1)] = stat * stat_times;
+            const int t = tid;
+            if (t < 2 * kTileRows) stats[buffer][t / kTileRows][t & (kTileRows - 1)] = stat * (t < kTileRows ? -1.f / c : -1.f);
         };
         if (row_begin < row_end) {
             fetch(row_begin, 0);
@@ -343,11 +342,10 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
             for (int b = 32 * wk; b < kTileRows; b += 32 * WK) {
                 const int row0 = row + b;
                 if (row0 >= wave_hi || row0 + 32 <= wave_lo) continue;
-                const char* const qt = q_tile + buffer * kTileBytes + b * Tile<DP>::kRowBytes;
-                const char* const ot = o_tile + buffer * kTileBytes + b * Tile<DP>::kRowBytes;
+                const uint32_t qt = buffer * kTileBytes + b * Tile<DP>::kRowBytes, ot = qt + 2 * kTileBytes;
                 // (products start from -lse / scale and -delta, so that these need neither registers nor additions)
-                f32x16 p = scores<T, DP>(qt, 0, k, lane, by_row(&stats[buffer][0][b], g));
-                f32x16 ds = scores<T, DP>(ot, 0, v, lane, by_row(&stats[buffer][1][b], g));
+                f32x16 p = scores<T, DP>(lds, qt, k, lane, by_row(&stats[buffer][0][b], g));
+                f32x16 ds = scores<T, DP>(lds, ot, v, lane, by_row(&stats[buffer][1][b], g));
                 const bool whole = row0 >= all_lo && row0 + 32 <= all_hi;
                 const bool behind = place_max - row0 <= -a.reach, ahead = place_min - (row0 + 31) >= a.reach;
                 const bool plain = whole && (a.bias == nullptr || behind || ahead);
@@ -409,8 +407,8 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[i] *= up;
                 }
-                accumulate<T, DP>(dv, ot, 0, p, lane);    // (p and ds rounded to the inputs' 16 bits)
-                accumulate<T, DP>(dk, qt, 0, ds, lane);
+                accumulate<T, DP>(dv, lds, ot, p, lane);    // (p and ds rounded to the inputs' 16 bits)
+                accumulate<T, DP>(dk, lds, qt, ds, lane);
             }
             if (more) keep(buffer ^ 1);
             tile_arrived();

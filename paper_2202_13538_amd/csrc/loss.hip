@@ -63,19 +63,18 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
     tile_arrived();
     __syncthreads();
     const bool works = first < a.n_rows;
-    int buffer = 0;
-#pragma unroll 1
-    for (int step = begin; step < end; ++step, buffer ^= 1) {
+    alternate(begin, end, 1, [&](int step, auto of) __attribute__((always_inline)) {
+        constexpr int buffer = decltype(of)::value;
         if (step + 1 < end) fetch(step + 1, buffer ^ 1);
         if (works) {
 #pragma unroll
             for (int b = 0; b < Shape::kKeys; b += 32) {
                 const int c0 = step * Shape::kTileKeys + wk * Shape::kKeys + b;
-                const char* const tile = lds + buffer * Shape::kTileBytes;
+                const uint32_t at = buffer * Shape::kTileBytes + (wk * Shape::kKeys + b) * Tile<DP>::kRowBytes;
                 f32x16 s[RB] = {};
 #pragma unroll
                 for (int ks = 0; ks < DP / 16; ++ks) {
-                    const u32x4 x = Tile<DP>::rows(tile, wk * Shape::kKeys + b, ks, lane);
+                    const u32x4 x = Tile<DP>::rows(lds, at, Tile<DP>::lane_rows(lane), ks);
 #pragma unroll
                     for (int r = 0; r < RB; ++r) s[r] = T::mma(x, h[r].k[ks], s[r]);
                 }
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
         }
         tile_arrived();
         __syncthreads();
-    }
+    });
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const float other = from_other_half(top[r]), other_sum = from_other_half(sum[r]), other_hit = from_other_half(hit[r]);

@@ -76,16 +76,15 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(Los
     if (begin < end) fetch(begin, 0);
     tile_arrived();
     __syncthreads();
-    int buffer = 0;
-#pragma unroll 1
-    for (int step = begin; step < end; ++step, buffer ^= 1) {
+    alternate(begin, end, 1, [&](int step, auto of) __attribute__((always_inline)) {
+        constexpr int buffer = decltype(of)::value;
         if (step + 1 < end) fetch(step + 1, buffer ^ 1);
-        const char* const tile = lds + buffer * kTileBytes;
+        constexpr uint32_t tile = buffer * kTileBytes;
         if (works) {
 #pragma unroll
             for (int b = 0; b < kStep; b += 32) {
                 const int c0 = step * kStep + b;
-                f32x16 s = scores<T, DP>(tile, b, h, lane);
+                f32x16 s = scores<T, DP>(lds, tile + b * Tile<DP>::kRowBytes, h, lane);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], kLog2e, -base));
                 if (__any((uint32_t)(label - c0) < 32u)) {
@@ -96,12 +95,12 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(Los
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = c0 + row_of(i, g) < a.n_classes ? s[i] : 0.f;
                 }
-                accumulate<T, DP>(acc, tile, b, s, lane);   // (weights rounded to the inputs' 16 bits)
+                accumulate<T, DP>(acc, lds, tile + b * Tile<DP>::kRowBytes, s, lane);   // (weights rounded to the inputs' 16 bits)
             }
         }
         tile_arrived();
         __syncthreads();
-    }
+    });
     if (w.splits_h > 1) {
         if (!in) return;
         float* const dst = w.part_h + ((int64_t)split * a.n_rows + row) * a.dim;
@@ -166,16 +165,15 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(Los
     }
     tile_arrived();
     __syncthreads();
-    int buffer = 0;
-#pragma unroll 1
-    for (int step = begin; step < end; ++step, buffer ^= 1) {
+    alternate(begin, end, 1, [&](int step, auto of) __attribute__((always_inline)) {
+        constexpr int buffer = decltype(of)::value;
         const bool more = step + 1 < end;
         if (more) fetch(step + 1, buffer ^ 1);
-        const char* const tile = lds + buffer * kTileBytes;
+        constexpr uint32_t tile = buffer * kTileBytes;
         if (works) {
 #pragma unroll
             for (int b = 0; b < kStep; b += 32) {
-                f32x16 s = scores<T, DP>(tile, b, c, lane);
+                f32x16 s = scores<T, DP>(lds, tile + b * Tile<DP>::kRowBytes, c, lane);
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
                     const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&stats[buffer][0][b + 8 * n + 4 * g]);
@@ -191,13 +189,13 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(Los
                         s[i] -= labels[buffer][n] == cls ? stats[buffer][1][n] : 0.f;
                     }
                 }
-                accumulate<T, DP>(acc, tile, b, s, lane);   // (weights rounded to the inputs' 16 bits)
+                accumulate<T, DP>(acc, lds, tile + b * Tile<DP>::kRowBytes, s, lane);   // (weights rounded to the inputs' 16 bits)
             }
         }
         if (more) keep(buffer ^ 1);
         tile_arrived();
         __syncthreads();
-    }
+    });
     if (__any(has_nan(acc))) {   // once more, without the rows that do not count
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};

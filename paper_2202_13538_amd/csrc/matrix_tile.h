@@ -54,6 +54,21 @@ struct Fp16 {
     }
 };
 
+// Runs turn(step, buffer) for step = begin, begin + by, ... < end, with buffers 0 and 1 in turn as constants: the places of
+// tiles are then parts of the instructions that read them.
+template <int N>
+struct Constant {
+    static constexpr int value = N;
+};
+template <class Turn>
+__device__ __forceinline__ void alternate(int begin, int end, int by, Turn turn) {
+#pragma unroll 1
+    for (int step = begin; step < end; step += 2 * by) {
+        turn(step, Constant<0>());
+        if (step + by < end) turn(step + by, Constant<1>());
+    }
+}
+
 // The thread's wave, and what is the same in all of its lanes, in scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float uniform(float x) {
@@ -94,39 +109,48 @@ __device__ __forceinline__ float from_other_half(float x) {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
-// Rows of DP elements (a multiple of 32) in LDS.
+// Rows of DP elements (a multiple of 32) in LDS, at byte offsets `at` from the start of dynamic LDS that are
+// multiples of 256 (tiles, and 16 rows of them).
 template <int DP>
 struct Tile {
     static constexpr int kChunks = DP / 8;
     static constexpr int kRowBytes = 2 * DP;
     // What a chunk's number is xor-ed with.  Rows of a multiple of 256 bytes begin in one place of the banks: the
     // row's low bits choose the quarter.  Of 128 bytes, two rows share the 256; of 64, four lie in all quarters.
+    static constexpr uint32_t kMixed = DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3;   // the bits that change
     __device__ __forceinline__ static int permuted(int row) {
         const int high = DP % 128 == 0 ? (row & 3) << 2 : DP % 64 == 0 ? (row & 2) << 1 : 0;
         return high | ((row >> 2) & 3);
     }
 
-    // A operand: rows row0 .. row0 + 31, inner values 16 ks .. 16 ks + 15.
-    __device__ __forceinline__ static u32x4 rows(const char* tile, int row0, int ks, int lane) {
-        const int r = row0 + (lane & 31);
-        const int c = (2 * ks + (lane >> 5)) ^ permuted(r);
-        return *reinterpret_cast<const u32x4*>(tile + r * kRowBytes + c * 16);
+    // A operand: the 32 rows at `at`, inner values 16 ks .. 16 ks + 15; lane_rows is the lane's place in rows
+    // for ks = 0.  (For other ks it differs by an xor of constant bits; `at` is a constant where loops are unrolled
+    // over buffers, and part of the instruction.)
+    __device__ __forceinline__ static uint32_t lane_rows(int lane) {
+        const int r = lane & 31;
+        return r * kRowBytes + (((lane >> 5) ^ permuted(r)) * 16);
+    }
+    __device__ __forceinline__ static u32x4 rows(const char* lds, uint32_t at, uint32_t lane_rows, int ks) {
+        const uint32_t c = 2 * ks;
+        return *reinterpret_cast<const u32x4*>(lds + (lane_rows ^ ((c & kMixed) * 16)) + (at + (c & ~kMixed) * 16));
     }
 
-    // A operand: columns 32 db .. 32 db + 31 as rows, the tile's rows row0 .. row0 + 15 (row0 a
-    // multiple of 16) as inner values, in the order that as_operand gives its own.
-    __device__ __forceinline__ static u32x4 columns(const char* tile, int row0, int db, int lane) {
+    // A operand: columns 32 db .. 32 db + 31 as rows, the 16 rows at `at` as inner values, in the order that
+    // as_operand gives its own; lane_columns as lane_rows above.
+    __device__ __forceinline__ static uint32_t lane_columns(int lane) {
+        const int i = lane & 15, r = 4 * (lane >> 5) + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        return r * kRowBytes + ((c ^ permuted(r)) * 16) + (i & 1) * 8;
+    }
+    __device__ __forceinline__ static u32x4 columns(const char* lds, uint32_t at, uint32_t lane_columns, int db) {
         typedef short v4i16 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) v4i16* lds_ptr;
-        const int i = lane & 15;
-        const int r = 4 * (lane >> 5) + (i >> 2);
-        const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        const uint32_t c = 4 * db;
         u32x4 out;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int row = row0 + 8 * half + r;
-            const char* at = tile + row * kRowBytes + ((chunk ^ permuted(row)) * 16) + (i & 1) * 8;
-            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
+        for (int half = 0; half < 2; ++half) {   // 8 rows further down the permutation's second bit changes
+            const char* const place = lds + (lane_columns ^ (((c & kMixed) ^ (2 * half)) * 16)) +
+                                      (at + (c & ~kMixed) * 16 + half * 8 * kRowBytes);
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)place));
             out[2 * half] = x[0];
             out[2 * half + 1] = x[1];
         }
@@ -149,7 +173,7 @@ __device__ __forceinline__ void copy_tile(char* tile, const char* src, uint32_t 
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
         const int id = tid + n * THREADS, row = id / kChunks;
-        const int c = (id % kChunks) ^ Tile<DP>::permuted(row);
+        const int c = (id % kChunks) ^ Tile<DP>::permuted(row);   // (below kMixed: stays inside the row)
         const uint32_t at = (uint32_t)min(row, rows - 1) * row_bytes + (c * 8 < dim ? c * 16 : 0);
         __builtin_amdgcn_global_load_lds((global_ptr)(src + at), (lds_ptr)(mine + n * THREADS * 16), 16, 0, 0);
     }
@@ -171,11 +195,12 @@ struct Stationary {
     }
 };
 
-// C[32 streamed rows from row0][32 stationary rows] of a tile, on top of c.
+// C[32 streamed rows][32 stationary rows] of the rows at `at`, on top of c.
 template <class T, int DP>
-__device__ __forceinline__ f32x16 scores(const char* tile, int row0, const Stationary<DP>& b, int lane, f32x16 c = {}) {
+__device__ __forceinline__ f32x16 scores(const char* lds, uint32_t at, const Stationary<DP>& b, int lane, f32x16 c = {}) {
+    const uint32_t mine = Tile<DP>::lane_rows(lane);
 #pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) c = T::mma(Tile<DP>::rows(tile, row0, ks, lane), b.k[ks], c);
+    for (int ks = 0; ks < DP / 16; ++ks) c = T::mma(Tile<DP>::rows(lds, at, mine, ks), b.k[ks], c);
     return c;
 }
 
@@ -191,16 +216,16 @@ __device__ __forceinline__ f32x16 by_row(const float* values, int g) {
     return c;
 }
 
-// acc[d][stationary row] += sum over 32 streamed rows from row0 of tile[row][d] w[row][stationary row].
+// acc[d][stationary row] += sum over the 32 streamed rows at `at` of row[d] w[row][stationary row].
 template <class T, int DP>
-__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const char* tile, int row0, const f32x16& w,
-                                           int lane) {
+__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const char* lds, uint32_t at, const f32x16& w, int lane) {
+    const uint32_t mine = Tile<DP>::lane_columns(lane);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const u32x4 b = as_operand<T>(w, t);
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
-            acc[db] = T::mma(Tile<DP>::columns(tile, row0 + 16 * t, db, lane), b, acc[db]);
+            acc[db] = T::mma(Tile<DP>::columns(lds, at + 16 * t * Tile<DP>::kRowBytes, mine, db), b, acc[db]);
     }
 }
 
