@@ -165,13 +165,15 @@ struct Tile {
 // weights of zero or lands in columns that nobody reads.
 template <int DP, int ROWS, int THREADS>
 __device__ __forceinline__ void copy_tile(char* tile, const char* src, uint32_t row_bytes, int rows, int dim, int tid) {
-    constexpr int kChunks = Tile<DP>::kChunks, kEach = ROWS * kChunks / THREADS;
-    static_assert(kEach * THREADS == ROWS * kChunks, "the tile is not a multiple of the threads");
+    constexpr int kChunks = Tile<DP>::kChunks, kEach = (ROWS * kChunks + THREADS - 1) / THREADS;
+    static_assert(ROWS * kChunks % 64 == 0, "the tile is not a multiple of a wave's chunks");
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef const __attribute__((address_space(1))) void* global_ptr;
-    char* const mine = tile + uniform(tid & ~63) * 16;
+    const int wave = uniform(tid & ~63);
+    char* const mine = tile + wave * 16;
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
+        if (ROWS * kChunks % THREADS != 0 && n * THREADS + wave >= ROWS * kChunks) break;
         const int id = tid + n * THREADS, row = id / kChunks;
         const int c = (id % kChunks) ^ Tile<DP>::permuted(row);   // (below kMixed: stays inside the row)
         const uint32_t at = (uint32_t)min(row, rows - 1) * row_bytes + (c * 8 < dim ? c * 16 : 0);
