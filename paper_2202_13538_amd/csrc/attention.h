@@ -19,14 +19,15 @@ struct AttentionArgs {
     uint32_t* err = nullptr;
 };
 
-// The rows of a sequence's part of `off` that hold row t: the last s with off[s] <= t.  Looks around the
-// place where equally long sequences have it, in steps that double, then halves what is left: one load where
-// they are equally long.
+// The last s with off[s] <= t, of n >= 1 parts.  Looks where equally long ones have it, then around that place in steps
+// that double, then halves what is left: one turn of memory where they are equally long.
 __device__ __forceinline__ int segment_of(const int64_t* __restrict__ off, int n, int64_t total, int64_t t) {
     int lo = total > 0 ? (int)((double)t * (double)n / (double)total) : 0;
     lo = min(max(lo, 0), n - 1);
+    const int64_t here = off[lo], next = off[lo + 1];
+    if (here <= t && t < next) return lo;
     int hi, step = 1;
-    if (off[lo] <= t) {
+    if (here <= t) {
         hi = lo + 1;
         while (hi < n && off[hi] <= t) {
             lo = hi;
@@ -57,7 +58,9 @@ struct Sequence {
     int q0, q1, k0, k1;
 };
 __device__ __forceinline__ Sequence sequence_at(const AttentionArgs& a, int s) {
-    const int64_t q0 = a.q_off[s], q1 = a.q_off[s + 1], k0 = a.k_off[s], k1 = a.k_off[s + 1];
+    const int64_t q0 = a.q_off[s], q1 = a.q_off[s + 1];
+    const bool alike = a.k_off == a.q_off;
+    const int64_t k0 = alike ? q0 : a.k_off[s], k1 = alike ? q1 : a.k_off[s + 1];
     if (q0 < 0 || q1 < q0 || q1 > a.n_q || k0 < 0 || k1 < k0 || k1 > a.n_k) {
         atomicOr(a.err, kDevBadOffsets);
         return Sequence{0, 0, 0, 0};
@@ -81,15 +84,19 @@ struct TileOfRows {
 __device__ __forceinline__ TileOfRows tile_of_rows(const int64_t* __restrict__ off, int n, int total, int rows,
                                                    bool across, int tile) {
     if (across) return TileOfRows{min(tile * rows, total), (int)min((int64_t)(tile + 1) * rows, (int64_t)total), -1};
-    // the last s with off[s] / rows + s <= tile
+    // the last s with off[s] / rows + s <= tile: 64 lanes look at as many places at once, so that 4,096
+    // sequences take two turns of memory
+    const int lane = lane_id();
     int lo = 0, hi = n;
     while (hi - lo > 1) {
-        // (a wave's lanes could look at 64 places at once; with the 13 steps of 8,192 sequences in the caches
-        // this is not what a tile waits for)
-        const int mid = lo + (hi - lo) / 2;
-        if (off[mid] / rows + mid <= tile) lo = mid;
-        else hi = mid;
+        const int step = (hi - lo + 63) / 64;
+        const int64_t at = lo + (int64_t)lane * step;
+        const bool below = at < hi && off[at] / rows + at <= tile;
+        const int count = __popcll(__ballot(below));   // lane 0's place is below or equal by construction
+        lo += (max(count, 1) - 1) * step;
+        hi = min(lo + step, hi);
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);
     int64_t r0 = off[lo], r1 = off[lo + 1];
     if (r0 < 0 || r1 < r0 || r1 > total) return TileOfRows{0, 0, lo};
     const int64_t at = r0 + (tile - (r0 / rows + lo)) * rows;

@@ -6,7 +6,7 @@ namespace surel {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kSlack = 8.f;  // see the running maximum below
+constexpr float kMost = 1024.f;  // a lane's weights of a tile add up to less, see the kernel
 
 struct AttentionOut {
     void* out = nullptr;        // [n_q][heads][dim]
@@ -65,6 +65,8 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     const int row = 32 * wr + col;
     const int token = tile.first + row / o.pack, head = head0 + row % o.pack;
     const bool counts = token < tile.last && row < tokens * o.pack;
+    Stationary<DP> q;
+    q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
     int lo = 0, hi = 0x7FFFFFFF, diag = 0;
     if (counts) {
         const int s = tile.seq >= 0 ? tile.seq : segment_of(a.q_off, a.n_seqs, a.n_q, token);
@@ -93,8 +95,6 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
         key_end = (int)min((int64_t)key_begin + each, (int64_t)tile_hi);
     }
 
-    Stationary<DP> q;
-    q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
     const float c = a.scale * kLog2e;   // scores in units of log 2
     const int width = 2 * a.reach + 1;
     if (a.bias != nullptr)
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     f32x16 acc[NB];
 #pragma unroll
     for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
-    float top = -INFINITY, sum = 0.f;
+    float top = sees ? -INFINITY : 0.f, sum = 0.f;   // what weights are taken relative to (base 2), and their sum
 
     auto fetch = [&](int key, int buffer) {
         const int rows = key_end - key;
@@ -119,19 +119,15 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
         copy_tile<DP, Shape::kTileKeys, kThreads>(v_tile + buffer * Shape::kTileBytes, v_src + (int64_t)key * a.v_row,
                                                   a.v_row, rows, a.dim, tid);
     };
-    // The maximum that weights are taken relative to may lag by 2^8: 32-bit sums and 16-bit floats (of at
-    // most 256 here) are as exact at that size, and most tiles need no rescaling.
-    auto raise_top = [&](float most) {
-        if (__any(most > top + kSlack)) {
-            const float now = fmaxf(top, most);
-            const float shrink = now == top ? 1.f : exp2_fast(top - now);
-            top = now;
-            sum *= shrink;
+    auto raise_top = [&](float most, bool mine) {
+        const float now = mine ? fmaxf(top, most) : top;
+        const float shrink = now == top ? 1.f : exp2_fast(top - now);
+        top = now;
+        sum *= shrink;
 #pragma unroll
-            for (int db = 0; db < NB; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[db][i] *= shrink;
-        }
+            for (int i = 0; i < 16; ++i) acc[db][i] *= shrink;
     };
     auto bias_at = [&](int key) {
         return a.bias == nullptr ? 0.f : my_bias[min(max(key - diag, -a.reach), a.reach) + a.reach];
@@ -153,13 +149,9 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
             for (int b = 0; b < kBlocks; ++b) s[b] = scores<T, DP>(lds, kt + 32 * b * Tile<DP>::kRowBytes, q, lane);
             const bool whole = key0 >= all_lo && key0 + Shape::kKeys <= min(all_hi, key_end);
             const bool behind = key0 + Shape::kKeys - 1 - diag_min <= -a.reach, ahead = key0 - diag_max >= a.reach;
-            if (whole && (a.bias == nullptr || behind || ahead)) {
-                const float add = behind ? bias_behind : bias_ahead;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_fmaf(s[b][i], c, add);
-            } else {
+            const bool plain = whole && (a.bias == nullptr || behind || ahead);
+            const float far = behind ? bias_behind : bias_ahead;
+            if (!plain) {   // scores, in units of log 2, of what the row sees
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -168,24 +160,41 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
                         s[b][i] = j >= lo && j < last ? __builtin_fmaf(s[b][i], c, bias_at(j)) : -INFINITY;
                     }
             }
-            float most = s[0][0];
+            // Weights relative to a maximum of earlier keys: 32-bit sums and 16-bit floats are as exact
+            // for weights of some hundreds as for those below one, so the maximum of these keys need not be known as
+            // long as they stay below kMost.  It is looked for only where they do not, or where a row meets
+            // its first key.  (Saves two of seven instructions a score.)
+            const float times = plain ? c : 1.f, plus = plain ? far : 0.f;
+            f32x16 p[kBlocks];
+            float part;
+            bool again = top == -INFINITY;   // the row's own affair: no other row's result depends on it
+            for (int turn = 0;; ++turn) {
+                if (__any(again)) {
+                    float most = s[0][0];
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
+                    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
-            raise_top(fmaxf(most, from_other_half(most)));
-            const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[b][i] = exp2_fast(s[b][i] - base);
-                    sum += s[b][i];
+                        for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
+                    most = __builtin_fmaf(most, times, plus);
+                    raise_top(fmaxf(most, from_other_half(most)), again);
                 }
+                const float less = plus - (top == -INFINITY ? 0.f : top);
+                part = 0.f;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        p[b][i] = exp2_fast(__builtin_fmaf(s[b][i], times, less));
+                        part += p[b][i];
+                    }
+                again = !(fmaxf(part, from_other_half(part)) < kMost) && !again;
+                if (turn > 0 || !__any(again)) break;
+            }
+            sum += part;
             // (weights are rounded to the inputs' 16 bits for the second product, the sum is of the
             // unrounded ones)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) accumulate<T, DP>(acc, lds, vt + 32 * b * Tile<DP>::kRowBytes, s[b], lane);
+            for (int b = 0; b < kBlocks; ++b) accumulate<T, DP>(acc, lds, vt + 32 * b * Tile<DP>::kRowBytes, p[b], lane);
         }
         tile_arrived();
         __syncthreads();
@@ -194,14 +203,14 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     if (__any(has_nan(acc))) {   // once more, without what a row does not see
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
-        top = -INFINITY;
+        top = sees ? -INFINITY : 0.f;
         sum = 0.f;
 #pragma unroll 1
         for (int j = max(key_begin, wave_lo) + wk; j < min(key_end, wave_hi); j += WK) {
             const float dot = dot_row<T, DP>(q, k_src + (int64_t)j * a.k_row, a.dim, lane);
             const bool seen = j >= lo && j < last;
             const float x = seen ? __builtin_fmaf(dot, c, bias_at(j)) : -INFINITY;
-            raise_top(x);
+            raise_top(x, true);
             if (seen) {
                 const float w = exp2_fast(x - (top == -INFINITY ? 0.f : top));
                 sum += w;
@@ -268,30 +277,42 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     });
 }
 
-// One wave a row: the parts of a row whose keys went to several workgroups.
+// One wave a row: the parts of a row whose keys went to several workgroups (128 at most, two a lane).
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionOut o, int64_t n_rows, int dim) {
     const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (row >= n_rows) return;
-    float top = -INFINITY;
-    for (int s = 0; s < o.splits; ++s) top = fmaxf(top, o.part_ml[2 * (s * n_rows + row)]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, x[2] = {0.f, 0.f};
-    for (int s = 0; s < o.splits; ++s) {
-        const int64_t part = s * n_rows + row;
-        const float m = o.part_ml[2 * part], w = m == top ? 1.f : exp2_fast(m - base);
-        if (m == -INFINITY && top != -INFINITY) continue;   // saw nothing
-        sum += w * o.part_ml[2 * part + 1];
+    float m[2], l[2], top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (2 * lane + e < dim) x[e] += w * o.part_o[part * dim + 2 * lane + e];
+    for (int e = 0; e < 2; ++e) {
+        const int s = lane + 64 * e;
+        const float2 x = s < o.splits ? reinterpret_cast<const float2*>(o.part_ml)[s * n_rows + row] : float2{-INFINITY, 0.f};
+        m[e] = x.x, l[e] = x.y;
+        if (l[e] != 0.f) top = fmaxf(top, m[e]);   // (a part that saw nothing has no say)
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        m[e] = l[e] == 0.f ? 0.f : m[e] == top ? 1.f : exp2_fast(m[e] - base);   // the part's weight
+        sum += m[e] * l[e];
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+    f32x2 x = {0.f, 0.f};
+    const bool mine = 2 * lane < dim;
+#pragma unroll 8
+    for (int s = 0; s < o.splits; ++s) {
+        const float w = __shfl(s < 64 ? m[0] : m[1], s & 63);
+        const f32x2 y = mine ? *reinterpret_cast<const f32x2*>(&o.part_o[(s * n_rows + row) * dim + 2 * lane]) : f32x2{0.f, 0.f};
+        if (w != 0.f) x[0] = __builtin_fmaf(w, y[0], x[0]), x[1] = __builtin_fmaf(w, y[1], x[1]);
     }
     // (a sum of zero: the row sees no key at all)
     if (lane == 0) o.lse[row] = sum == 0.f ? -INFINITY : (top + log2_fast(sum)) * kLn2;
     const float scale = sum == 0.f ? 0.f : 1.f / sum;
-    if (2 * lane < dim)
-        static_cast<uint32_t*>(o.out)[row * (dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
+    if (mine) static_cast<uint32_t*>(o.out)[row * (dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
 }
 
 struct ForwardPlan {

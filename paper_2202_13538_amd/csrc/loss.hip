@@ -8,6 +8,14 @@ namespace surel {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr float kMost = 1e12f;
+
+__device__ __forceinline__ float sum_of(const f32x16& s, float base) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += exp2_fast(__builtin_fmaf(s[i], kLog2e, -base));
+    return sum;
+}
 
 struct LossOut {
     f32x4* part = nullptr;  // [n_rows][parts of rows]: maximum and sum (base 2), the label's score
@@ -90,15 +98,20 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
 #pragma unroll
                         for (int i = 0; i < 16; ++i) hit[r] = label[r] - c0 == row_of(i, g) ? s[r][i] : hit[r];
                     }
-                    float most = s[r][0];
+                    // Relative to a maximum of earlier classes: as long as these add up to less than kMost,
+                    // their own need not be known.
+                    float part = sum_of(s[r], top[r] == -INFINITY ? 0.f : top[r]);
+                    const bool again = top[r] == -INFINITY || !(part < kMost);   // (the row's own affair: no other row's
+                    if (__any(again)) {                                          // result depends on it)
+                        float most = s[r][0];
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[r][i]);
-                    const float now = fmaxf(top[r], most * kLog2e), base = now == -INFINITY ? 0.f : now;
-                    float part = sum[r] * exp2_fast(top[r] - base);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) part += exp2_fast(__builtin_fmaf(s[r][i], kLog2e, -base));
-                    sum[r] = part;
-                    top[r] = now;
+                        for (int i = 1; i < 16; ++i) most = fmaxf(most, s[r][i]);
+                        const float now = again ? fmaxf(top[r], most * kLog2e) : top[r], base = now == -INFINITY ? 0.f : now;
+                        sum[r] *= exp2_fast(top[r] - base);
+                        top[r] = now;
+                        part = sum_of(s[r], base);
+                    }
+                    sum[r] += part;
                 }
             }
         }
@@ -116,27 +129,38 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
     }
 }
 
-// One wave a row: the parts of its classes.
+// The parts of a row's classes: a wave a row, or a workgroup where there are more than 64 parts.
+template <int WAVES>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(LossArgs a, LossOut o) {
-    const int row = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    __shared__ float of_wave[3][kThreads / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int row = WAVES == 1 ? blockIdx.x * (kThreads / 64) + wave : blockIdx.x;
     if (row >= a.n_rows) return;
     float top = -INFINITY, sum = 0.f, hit = 0.f;
-    for (int p = lane; p < o.row_parts; p += 64) {
+#pragma unroll 4
+    for (int p = WAVES == 1 ? lane : threadIdx.x; p < o.row_parts; p += 64 * WAVES) {
         const f32x4 x = o.part[(int64_t)row * o.row_parts + p];
         const float now = fmaxf(top, x[0]), base = now == -INFINITY ? 0.f : now;
         sum = sum * exp2_fast(top - base) + x[1] * exp2_fast(x[0] - base);
         top = now;
         hit += x[2];
     }
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const float other = __shfl_xor(top, m), other_sum = __shfl_xor(sum, m);
+    auto add = [&](float other, float other_sum, float other_hit) {
         const float now = fmaxf(top, other), base = now == -INFINITY ? 0.f : now;
         sum = sum * exp2_fast(top - base) + other_sum * exp2_fast(other - base);
         top = now;
-        hit += __shfl_xor(hit, m);
+        hit += other_hit;
+    };
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) add(__shfl_xor(top, m), __shfl_xor(sum, m), __shfl_xor(hit, m));
+    if (WAVES > 1) {
+        if (lane == 0) of_wave[0][wave] = top, of_wave[1][wave] = sum, of_wave[2][wave] = hit;
+        __syncthreads();
+        top = of_wave[0][0], sum = of_wave[1][0], hit = of_wave[2][0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) add(of_wave[0][w], of_wave[1][w], of_wave[2][w]);
     }
-    if (lane == 0) {
+    if (lane == 0 && (WAVES == 1 || wave == 0)) {
         const float lse = (top + log2_fast(sum)) * kLn2;
         const int label = a.labels[row];
         o.lse[row] = lse;
@@ -181,7 +205,9 @@ hipError_t launch_type(hipStream_t stream, const LossArgs& a, const LossOut& o, 
            : a.dim <= 64  ? launch_rows<T, 64>(stream, a, o, p)
            : a.dim <= 96  ? launch_rows<T, 96>(stream, a, o, p)
            : a.dim <= 128 ? launch_rows<T, 128>(stream, a, o, p)
+           : a.dim <= 160 ? launch_rows<T, 160>(stream, a, o, p)
            : a.dim <= 192 ? launch_rows<T, 192>(stream, a, o, p)
+           : a.dim <= 224 ? launch_rows<T, 224>(stream, a, o, p)
                           : launch_rows<T, 256>(stream, a, o, p);
 }
 
@@ -201,7 +227,8 @@ hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool hal
     o.row_parts = p.row_parts;
     const hipError_t rc = half ? launch_type<Fp16>(stream, a, o, p) : launch_type<Bf16>(stream, a, o, p);
     if (rc != hipSuccess) return rc;
-    hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(kThreads), 0, stream, a, o);
+    if (p.row_parts > 64) hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)a.n_rows), dim3(kThreads), 0, stream, a, o);
+    else hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(kThreads), 0, stream, a, o);
     return hipGetLastError();
 }
 

@@ -18,31 +18,37 @@ constexpr int kStep = 64;  // streamed rows or classes of a tile
 // fp16 only: weights (of at most 1) are multiplied by 2^12 before they are rounded, so that a class's share
 // of 1.5e-8 still has all its bits.
 constexpr int kLift = 12;
+constexpr int kMaxima = 256;  // workgroups that look for the largest |dloss|, at most
 
 struct LossGradArgs {
     const float *dloss = nullptr, *lse = nullptr;
     void *dh = nullptr, *dw = nullptr;
     float *part_h = nullptr, *part_w = nullptr;  // [split][rows][dim], where there are several
-    uint32_t* largest = nullptr;                 // of |dloss|, as a float's bits (fp16 only)
+    float* maxima = nullptr;                     // [n_maxima], of parts of |dloss| (fp16 only)
+    int n_maxima = 0;
     int splits_h = 1, splits_w = 1;
 };
 
-__global__ void clear_largest_kernel(uint32_t* word) { *word = 0; }
-
 __global__ __launch_bounds__(kThreads) void largest_kernel(LossArgs a, LossGradArgs w) {
+    __shared__ float most_of[kThreads / 64];
     float most = 0.f;
-    for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_rows; i += gridDim.x * kThreads)
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.n_rows; i += (int64_t)gridDim.x * kThreads)
         if (a.labels[i] >= 0) most = fmaxf(most, fabsf(w.dloss[i]));
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(w.largest, __float_as_uint(most));
+    if ((threadIdx.x & 63) == 0) most_of[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) w.maxima[blockIdx.x] = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
 }
 
 // The power of two that dloss is multiplied by before weights are rounded to fp16: the largest becomes 2^11 .. 2^12.
 template <class T>
-__device__ __forceinline__ int lift_of(const LossGradArgs& w) {
+__device__ __forceinline__ int lift_of(const LossGradArgs& w, int lane) {
     if (!T::kNarrow) return 0;
-    const float most = __uint_as_float(*w.largest);
+    float most = 0.f;
+    for (int i = lane; i < w.n_maxima; i += 64) most = fmaxf(most, w.maxima[i]);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
     if (!(most > 0.f) || !(most < INFINITY)) return 0;
     return min(max(kLift - 1 - ilogbf(most), -100), 100);
 }
@@ -125,14 +131,16 @@ template <class T, int DP>
 __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(LossArgs a, LossGradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
     extern __shared__ __align__(16) char lds[];
-    __shared__ __align__(16) float stats[2][2][kStep];   // [buffer][lse, dloss][row]
+    __shared__ __align__(16) float start[2][kStep];   // [buffer][row]: log |dloss| - lse
+    __shared__ __align__(16) float dloss[2][kStep];
     __shared__ __align__(16) int labels[2][kStep];
+    __shared__ int negative[2];                       // [buffer]: some dloss of the tile is
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int split = blockIdx.x % w.splits_w, first = blockIdx.x / w.splits_w * 128 + wave * 32, cls = first + col;
     const bool in = cls < a.n_classes, works = first < a.n_classes;
     Stationary<DP> c;
     c.load(a.w + (int64_t)cls * a.dim * 2, in, a.dim, lane);
-    const int lift = lift_of<T>(w);
+    const int lift = lift_of<T>(w, lane);
     const float up = ldexpf(1.f, lift);
 
     f32x16 acc[NB];
@@ -141,23 +149,29 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(Los
     const int steps = (a.n_rows + kStep - 1) / kStep, each = (steps + w.splits_w - 1) / w.splits_w;
     const int begin = min(split * each, steps), end = min(begin + each, steps);
     const uint32_t row_bytes = (uint32_t)a.dim * 2;
-    float stat = 0.f;
+    // Products start from log |dloss| - lse of their rows: the exponential of that is a weight with dloss in it, and only
+    // a tile with negative ones has to be multiplied by signs.  A row that does not count starts from minus infinity.
+    float dl = 0.f, lse = 0.f;
     int label = -1;
     auto fetch = [&](int step, int buffer) {
-        const int r0 = step * kStep, n = r0 + (tid & (kStep - 1));
+        const int r0 = step * kStep, n = r0 + tid;
         copy_tile<DP, kStep, kThreads>(lds + buffer * kTileBytes, a.h + (int64_t)r0 * row_bytes, row_bytes, a.n_rows - r0,
                                        a.dim, tid);
-        if (tid < 2 * kStep) {
+        if (tid < kStep) {
             label = n < a.n_rows ? a.labels[n] : -1;
             if (label >= a.n_classes) label = -1;
-            // (a row that does not count: weights of zero)
-            if (tid < kStep) stat = label < 0 ? INFINITY : w.lse[n] * kLog2e;
-            else stat = label < 0 ? 0.f : w.dloss[n] * up;
+            dl = label < 0 ? 0.f : w.dloss[n] * up;
+            lse = label < 0 ? 0.f : w.lse[n];
         }
     };
     auto keep = [&](int buffer) {
-        if (tid < 2 * kStep) stats[buffer][tid / kStep][tid & (kStep - 1)] = stat;
-        if (tid < kStep) labels[buffer][tid] = label;
+        if (tid < kStep) {
+            start[buffer][tid] = dl == 0.f ? -INFINITY : log2_fast(fabsf(dl)) * kLn2 - lse;
+            dloss[buffer][tid] = dl;
+            labels[buffer][tid] = label;
+            const bool any = __any(dl < 0.f);
+            if (tid == 0) negative[buffer] = any;
+        }
     };
     if (begin < end) {
         fetch(begin, 0);
@@ -173,20 +187,18 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(Los
         if (works) {
 #pragma unroll
             for (int b = 0; b < kStep; b += 32) {
-                f32x16 s = scores<T, DP>(lds, tile + b * Tile<DP>::kRowBytes, c, lane);
+                f32x16 s = scores<T, DP>(lds, tile + b * Tile<DP>::kRowBytes, c, lane, by_row(&start[buffer][b], g));
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&stats[buffer][0][b + 8 * n + 4 * g]);
-                    const f32x4 dl = *reinterpret_cast<const f32x4*>(&stats[buffer][1][b + 8 * n + 4 * g]);
+                for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * kLog2e);
+                if (negative[buffer]) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[4 * n + i] = exp2_fast(__builtin_fmaf(s[4 * n + i], kLog2e, -lse2[i])) * dl[i];
+                    for (int i = 0; i < 16; ++i) s[i] = dloss[buffer][b + row_of(i, g)] < 0.f ? -s[i] : s[i];
                 }
                 if (__any((uint32_t)(labels[buffer][b + col] - first) < 32u)) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int n = b + row_of(i, g);
-                        s[i] -= labels[buffer][n] == cls ? stats[buffer][1][n] : 0.f;
+                        s[i] -= labels[buffer][n] == cls ? dloss[buffer][n] : 0.f;
                     }
                 }
                 accumulate<T, DP>(acc, lds, tile + b * Tile<DP>::kRowBytes, s, lane);   // (weights rounded to the inputs' 16 bits)
@@ -260,7 +272,7 @@ size_t lay_out(const LossArgs& a, const LossGradPlan& p, char* scratch, LossGrad
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    w->largest = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+    w->maxima = reinterpret_cast<float*>(take(kMaxima * sizeof(float)));
     // one after the other in one place: dh's parts are added up before dw's are written
     const size_t h = p.splits_h > 1 ? (size_t)p.splits_h * a.n_rows * a.dim * sizeof(float) : 0;
     const size_t c = p.splits_w > 1 ? (size_t)p.splits_w * a.n_classes * a.dim * sizeof(float) : 0;
@@ -294,9 +306,7 @@ hipError_t launch_width(hipStream_t stream, const LossArgs& a, const LossGradArg
 template <class T>
 hipError_t launch_type(hipStream_t stream, const LossArgs& a, const LossGradArgs& w, const LossGradPlan& p) {
     if (T::kNarrow) {
-        hipLaunchKernelGGL(clear_largest_kernel, dim3(1), dim3(1), 0, stream, w.largest);
-        const int blocks = (a.n_rows + kThreads - 1) / kThreads;
-        hipLaunchKernelGGL(largest_kernel, dim3((unsigned)(blocks < 256 ? blocks : 256)), dim3(kThreads), 0, stream, a, w);
+        hipLaunchKernelGGL(largest_kernel, dim3((unsigned)w.n_maxima), dim3(kThreads), 0, stream, a, w);
         const hipError_t rc = hipGetLastError();
         if (rc != hipSuccess) return rc;
     }
@@ -304,7 +314,9 @@ hipError_t launch_type(hipStream_t stream, const LossArgs& a, const LossGradArgs
            : a.dim <= 64  ? launch_width<T, 64>(stream, a, w, p)
            : a.dim <= 96  ? launch_width<T, 96>(stream, a, w, p)
            : a.dim <= 128 ? launch_width<T, 128>(stream, a, w, p)
+           : a.dim <= 160 ? launch_width<T, 160>(stream, a, w, p)
            : a.dim <= 192 ? launch_width<T, 192>(stream, a, w, p)
+           : a.dim <= 224 ? launch_width<T, 224>(stream, a, w, p)
                           : launch_width<T, 256>(stream, a, w, p);
 }
 
@@ -326,6 +338,8 @@ hipError_t launch_loss_grad(hipStream_t stream, int n_cu, const LossArgs& a, boo
     w.dw = dw;
     w.splits_h = p.splits_h;
     w.splits_w = p.splits_w;
+    const int blocks = (a.n_rows + kThreads - 1) / kThreads;
+    w.n_maxima = blocks < kMaxima ? blocks : kMaxima;
     return half ? launch_type<Fp16>(stream, a, w, p) : launch_type<Bf16>(stream, a, w, p);
 }
 
