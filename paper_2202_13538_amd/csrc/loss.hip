@@ -178,7 +178,7 @@ LossPlan loss_plan(const LossArgs& a, int n_cu) {
     p.few = a.n_rows <= 32;
     const int rows = p.few ? 32 : 256, keys = p.few ? 128 : 64;
     p.tiles = (a.n_rows + rows - 1) / rows;
-    p.splits = parts_for(p.tiles, (a.n_classes + keys - 1) / keys, 2 * n_cu, 1024);
+    p.splits = parts_for(p.tiles, (a.n_classes + keys - 1) / keys, 2 * n_cu, 1024, 0.0);
     p.row_parts = p.splits * (p.few ? 4 : 1);
     return p;
 }

@@ -55,7 +55,7 @@ __device__ __forceinline__ int lift_of(const LossGradArgs& w, int lane) {
 
 // dh of 128 rows, 32 a wave, from a part of the classes.
 template <class T, int DP>
-__global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(LossArgs a, LossGradArgs w) {
+__global__ __launch_bounds__(kThreads, DP > 224 ? 1 : 2) void loss_dh_kernel(LossArgs a, LossGradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dh_kernel(Los
 
 // dw of 128 classes, 32 a wave, from a part of the rows.
 template <class T, int DP>
-__global__ __launch_bounds__(kThreads, DP > 192 ? 1 : 2) void loss_dw_kernel(LossArgs a, LossGradArgs w) {
+__global__ __launch_bounds__(kThreads, DP > 224 ? 1 : 2) void loss_dw_kernel(LossArgs a, LossGradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kStep * Tile<DP>::kRowBytes;
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) float start[2][kStep];   // [buffer][row]: log |dloss| - lse
@@ -259,9 +259,12 @@ LossGradPlan loss_grad_plan(const LossArgs& a, int n_cu) {
     LossGradPlan p;
     p.tiles_h = (a.n_rows + 127) / 128;
     p.tiles_w = ((int64_t)a.n_classes + 127) / 128;
-    const int slots = a.dim > 192 ? n_cu : 2 * n_cu;
-    p.splits_h = parts_for(p.tiles_h, (a.n_classes + kStep - 1) / kStep, slots, 256);
-    p.splits_w = parts_for(p.tiles_w, (a.n_rows + kStep - 1) / kStep, slots, 64);
+    const int slots = a.dim > 224 ? n_cu : 2 * n_cu;
+    // A part's sums are written and read again, 8 bytes an element; a step is 4 * 64 * 128 operations an
+    // element of a row on one of the slots: at 4.5 TB/s and 1.1 PFLOP/s 0.06 / slots of a step a row of sums.
+    const double cost = 0.06 / slots;
+    p.splits_h = parts_for(p.tiles_h, (a.n_classes + kStep - 1) / kStep, slots, 256, cost * a.n_rows);
+    p.splits_w = parts_for(p.tiles_w, (a.n_rows + kStep - 1) / kStep, slots, 64, cost * a.n_classes);
     return p;
 }
 
