@@ -634,8 +634,8 @@ def attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     last key, rows see keys up to their own.  scale None: 1 / sqrt(dim).  bias [buckets][heads] and bucket
     int32[2 * reach + 1] (see distance_buckets): a learned bias by the distance of key and row."""
     args = _attention_args(q, k, v, q_off, k_off, causal, scale, bias, bucket)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    out = q.new_empty(q.shape)
+    lse = q.new_empty(q.shape[:2], dtype=torch.float32)
     rc = load().surel_attention(ctx.handle, ctypes.byref(args), out.data_ptr(), lse.data_ptr())
     if rc != OK:
         raise SurelError(rc, "surel_attention")
@@ -703,8 +703,8 @@ def softmax_loss(ctx: Context, h: torch.Tensor, w: torch.Tensor, labels: torch.T
     classes w [classes][dim] (bfloat16 or float16, dense), of which labels int32[rows] names each row's; a
     negative label: the row does not count, its loss is 0.  Logits are not kept."""
     kind, n, classes, dim = _loss_shape(h, w, labels)
-    loss = torch.empty(n, dtype=torch.float32, device=h.device)
-    lse = torch.empty(n, dtype=torch.float32, device=h.device)
+    loss = h.new_empty(n, dtype=torch.float32)
+    lse = h.new_empty(n, dtype=torch.float32)
     rc = load().surel_softmax_loss(ctx.handle, kind, _ptr(h, h.dtype, "h"), _ptr(w, h.dtype, "w"),
                                    _ptr(labels, torch.int32, "labels"), n, classes, dim, loss.data_ptr(),
                                    lse.data_ptr())

@@ -104,6 +104,8 @@ int surel_create(surel_ctx** out, int device, void* hip_stream) {
     ok = ok && hipMemsetAsync(ctx->d_err, 0, 256, ctx->stream) == hipSuccess;
     ok = ok && hipMalloc(&ctx->d_small, surel::small_scan_bytes()) == hipSuccess;
     ok = ok && hipMemsetAsync(ctx->d_small, 0, surel::small_scan_bytes(), ctx->stream) == hipSuccess;
+    ok = ok && hipMalloc(reinterpret_cast<void**>(&ctx->d_turns), 256) == hipSuccess;
+    ok = ok && hipMemsetAsync(ctx->d_turns, 0, 256, ctx->stream) == hipSuccess;
     ok = ok && hipEventCreateWithFlags(&ctx->done, hipEventDisableTiming) == hipSuccess;
     ok = ok && hipHostMalloc(reinterpret_cast<void**>(&ctx->h_pinned), 3 * sizeof(int64_t),
                              hipHostMallocDefault) == hipSuccess;
@@ -114,6 +116,7 @@ int surel_create(surel_ctx** out, int device, void* hip_stream) {
     if (!ok) {
         if (ctx->d_err) (void)hipFree(ctx->d_err);
         if (ctx->d_small) (void)hipFree(ctx->d_small);
+        if (ctx->d_turns) (void)hipFree(ctx->d_turns);
         if (ctx->done) (void)hipEventDestroy(ctx->done);
         if (ctx->h_pinned) (void)hipHostFree(ctx->h_pinned);
         delete ctx;
@@ -141,6 +144,7 @@ void surel_destroy(surel_ctx* ctx) {
     if (ctx->d_model) (void)hipFree(ctx->d_model);
     if (ctx->d_err) (void)hipFree(ctx->d_err);
     if (ctx->d_small) (void)hipFree(ctx->d_small);
+    if (ctx->d_turns) (void)hipFree(ctx->d_turns);
     if (ctx->done) (void)hipEventDestroy(ctx->done);
     if (ctx->h_pinned) (void)hipHostFree(ctx->h_pinned);
     delete ctx;

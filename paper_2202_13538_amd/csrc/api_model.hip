@@ -134,7 +134,8 @@ int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void
     if (!guard.ok) return SUREL_E_HIP;
     if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::loss_scratch_bytes(ctx->n_cu, a))) return rc;
     KernelSpan span(ctx, SUREL_K_LOSS);
-    if (surel::launch_loss(ctx->stream, ctx->n_cu, a, type == SUREL_FP16, d_loss, d_lse, ctx->d_model) != hipSuccess)
+    if (surel::launch_loss(ctx->stream, ctx->n_cu, a, type == SUREL_FP16, d_loss, d_lse, ctx->d_model, ctx->d_turns) !=
+        hipSuccess)
         return SUREL_E_HIP;
     return SUREL_OK;
 }

@@ -31,6 +31,7 @@ struct surel_ctx {
     size_t prune_clean = 0;       // bytes of the hash slots in it that are known to be empty
     void* d_batch = nullptr;      // grow-only workspace: sort arrays of the incidence lists, hash
     size_t batch_bytes = 0;       // tables of the mini-batch search
+    uint32_t* d_turns = nullptr;  // a word of zero between launches whose last workgroup joins the others' parts
     void* d_model = nullptr;      // grow-only workspace: parts of attention and loss that are joined later
     size_t model_bytes = 0;
     void* d_scratch = nullptr;    // this device's copy of the file-scope `scratch` array below

@@ -221,7 +221,9 @@ hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionAr
 // loss.hip, loss_grad.hip.  scratch: that many bytes of device memory.  Need a.n_rows, a.n_classes >= 1.
 struct LossArgs;
 size_t loss_scratch_bytes(int n_cu, const LossArgs& a);
-hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch);
+// turns: a word of zero (it is one again afterwards).
+hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch,
+                       uint32_t* turns);
 size_t loss_grad_scratch_bytes(int n_cu, const LossArgs& a);
 hipError_t launch_loss_grad(hipStream_t stream, int n_cu, const LossArgs& a, bool half, const float* dloss, const float* lse,
                             void* dh, void* dw, void* scratch);

@@ -27,7 +27,7 @@ __device__ __forceinline__ int label_of(const LossArgs& a, int row) {
 inline int parts_for(int64_t tiles, int64_t steps, int slots, int most, double part_cost) {
     int best = 1;
     double least = 1e300;
-    for (int parts = 1; parts <= most && (parts == 1 || steps / parts >= 4); parts = parts < 8 ? 2 * parts : parts + 8) {
+    for (int parts = 1; parts <= most && parts <= steps; parts = parts < 8 ? 2 * parts : parts + 8) {
         const double rounds = ceil((double)(tiles * parts) / slots);
         // (2: what a workgroup costs beside its steps)
         const double time = rounds * (ceil((double)steps / parts) + 2) + (parts > 1 ? parts * part_cost : 0.0);

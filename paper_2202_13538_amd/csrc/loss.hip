@@ -22,7 +22,33 @@ struct LossOut {
     float *loss = nullptr, *lse = nullptr;
     int splits = 1;
     int row_parts = 1;      // splits times the waves that share a row
+    uint32_t* turns = nullptr;  // [tiles] of zeros, or null: a launch of its own joins the parts
 };
+
+// Joining the parts of a row's classes: 64 lanes, then (where there are several) the waves.
+struct Joined {
+    float top = -INFINITY, sum = 0.f, hit = 0.f;
+    __device__ __forceinline__ void add(float other, float other_sum, float other_hit) {
+        const float now = fmaxf(top, other), base = now == -INFINITY ? 0.f : now;
+        sum = sum * exp2_fast(top - base) + other_sum * exp2_fast(other - base);
+        top = now;
+        hit += other_hit;
+    }
+    __device__ __forceinline__ void add_lanes() {
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) add(__shfl_xor(top, m), __shfl_xor(sum, m), __shfl_xor(hit, m));
+    }
+    __device__ __forceinline__ void write(const LossArgs& a, const LossOut& o, int row) const {
+        const float lse = (top + log2_fast(sum)) * kLn2;
+        const int label = a.labels[row];
+        o.lse[row] = lse;
+        o.loss[row] = label < 0 || label >= a.n_classes ? 0.f : lse - hit;
+    }
+};
+
+// Words that workgroups on other XCDs read in the same launch: past the caches in between.
+__device__ __forceinline__ void put(float* at, float x) { __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get(const float* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 template <int DP, int WR>
 struct LossShape {
@@ -124,8 +150,36 @@ __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o
         const float now = fmaxf(top[r], other), base = now == -INFINITY ? 0.f : now;
         const float total = sum[r] * exp2_fast(top[r] - base) + other_sum * exp2_fast(other - base);
         const int row = first + 32 * r + col;
-        if (g == 0 && row < a.n_rows)
-            o.part[(int64_t)row * o.row_parts + split * Shape::WK + wk] = f32x4{now, total, hit[r] + other_hit, 0.f};
+        if (g == 0 && row < a.n_rows) {
+            f32x4* const part = &o.part[(int64_t)row * o.row_parts + split * Shape::WK + wk];
+            if (o.turns == nullptr) {
+                *part = f32x4{now, total, hit[r] + other_hit, 0.f};
+            } else {
+                float* const word = reinterpret_cast<float*>(part);
+                put(word, now), put(word + 1, total), put(word + 2, hit[r] + other_hit);
+            }
+        }
+    }
+    if (o.turns == nullptr) return;
+    // the last workgroup of a tile's joins its rows' parts, in the same order whoever is last
+    __shared__ bool last;
+    wait_memory();
+    __syncthreads();
+    if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(&o.turns[row_tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = before == (uint32_t)o.splits - 1;
+        if (last) __hip_atomic_store(&o.turns[row_tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int row = row_tile * Shape::kRows + wave; row < min((row_tile + 1) * Shape::kRows, a.n_rows); row += kThreads / 64) {
+        Joined x;
+        for (int p = lane; p < o.row_parts; p += 64) {
+            const float* const word = reinterpret_cast<const float*>(&o.part[(int64_t)row * o.row_parts + p]);
+            x.add(get(word), get(word + 1), get(word + 2));
+        }
+        x.add_lanes();
+        if (lane == 0) x.write(a, o, row);
     }
 }
 
@@ -136,40 +190,25 @@ __global__ __launch_bounds__(kThreads) void loss_join_kernel(LossArgs a, LossOut
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int row = WAVES == 1 ? blockIdx.x * (kThreads / 64) + wave : blockIdx.x;
     if (row >= a.n_rows) return;
-    float top = -INFINITY, sum = 0.f, hit = 0.f;
+    Joined x;
 #pragma unroll 4
     for (int p = WAVES == 1 ? lane : threadIdx.x; p < o.row_parts; p += 64 * WAVES) {
-        const f32x4 x = o.part[(int64_t)row * o.row_parts + p];
-        const float now = fmaxf(top, x[0]), base = now == -INFINITY ? 0.f : now;
-        sum = sum * exp2_fast(top - base) + x[1] * exp2_fast(x[0] - base);
-        top = now;
-        hit += x[2];
+        const f32x4 y = o.part[(int64_t)row * o.row_parts + p];
+        x.add(y[0], y[1], y[2]);
     }
-    auto add = [&](float other, float other_sum, float other_hit) {
-        const float now = fmaxf(top, other), base = now == -INFINITY ? 0.f : now;
-        sum = sum * exp2_fast(top - base) + other_sum * exp2_fast(other - base);
-        top = now;
-        hit += other_hit;
-    };
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) add(__shfl_xor(top, m), __shfl_xor(sum, m), __shfl_xor(hit, m));
+    x.add_lanes();
     if (WAVES > 1) {
-        if (lane == 0) of_wave[0][wave] = top, of_wave[1][wave] = sum, of_wave[2][wave] = hit;
+        if (lane == 0) of_wave[0][wave] = x.top, of_wave[1][wave] = x.sum, of_wave[2][wave] = x.hit;
         __syncthreads();
-        top = of_wave[0][0], sum = of_wave[1][0], hit = of_wave[2][0];
+        x = Joined{of_wave[0][0], of_wave[1][0], of_wave[2][0]};
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) add(of_wave[0][w], of_wave[1][w], of_wave[2][w]);
+        for (int w = 1; w < WAVES; ++w) x.add(of_wave[0][w], of_wave[1][w], of_wave[2][w]);
     }
-    if (lane == 0 && (WAVES == 1 || wave == 0)) {
-        const float lse = (top + log2_fast(sum)) * kLn2;
-        const int label = a.labels[row];
-        o.lse[row] = lse;
-        o.loss[row] = label < 0 || label >= a.n_classes ? 0.f : lse - hit;
-    }
+    if (lane == 0 && (WAVES == 1 || wave == 0)) x.write(a, o, row);
 }
 
 struct LossPlan {
-    bool few;
+    bool few, alone;   // alone: the last workgroup of a tile joins its parts
     int splits, row_parts;
     int64_t tiles;
 };
@@ -180,6 +219,8 @@ LossPlan loss_plan(const LossArgs& a, int n_cu) {
     p.tiles = (a.n_rows + rows - 1) / rows;
     p.splits = parts_for(p.tiles, (a.n_classes + keys - 1) / keys, 2 * n_cu, 1024, 0.0);
     p.row_parts = p.splits * (p.few ? 4 : 1);
+    // (one launch less, 2 us; a tile's rows are joined by 4 waves then, so there are not to be many parts)
+    p.alone = p.few && p.row_parts <= 256;
     return p;
 }
 
@@ -217,7 +258,8 @@ size_t loss_scratch_bytes(int n_cu, const LossArgs& a) {
     return (size_t)a.n_rows * loss_plan(a, n_cu).row_parts * sizeof(f32x4);
 }
 
-hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch) {
+hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool half, float* loss, float* lse, void* scratch,
+                       uint32_t* turns) {
     const LossPlan p = loss_plan(a, n_cu);
     LossOut o;
     o.part = static_cast<f32x4*>(scratch);
@@ -225,8 +267,9 @@ hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool hal
     o.lse = lse;
     o.splits = p.splits;
     o.row_parts = p.row_parts;
+    o.turns = p.alone ? turns : nullptr;
     const hipError_t rc = half ? launch_type<Fp16>(stream, a, o, p) : launch_type<Bf16>(stream, a, o, p);
-    if (rc != hipSuccess) return rc;
+    if (rc != hipSuccess || p.alone) return rc;
     if (p.row_parts > 64) hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)a.n_rows), dim3(kThreads), 0, stream, a, o);
     else hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(kThreads), 0, stream, a, o);
     return hipGetLastError();
