@@ -107,17 +107,26 @@ inline int64_t tiles_of_rows(int64_t n, int64_t total, int64_t rows, bool across
     return across ? (total + rows - 1) / rows : total / rows + n;
 }
 
-// A bucket's bias, in units of log 2, for every distance -reach .. reach of one head.
+// One head's bias, in units of log 2, for every distance -reach .. reach, and kBeyond places more at both ends that
+// repeat the last ones: a tile of 64 keys (or rows) by 32 rows (or keys) that reaches into -reach .. reach
+// anywhere finds all of its distances there, by one address and constant offsets.
+constexpr int kBeyond = 96;
+__host__ __device__ constexpr int bias_width(int reach) { return 2 * reach + 1 + 2 * kBeyond; }
 template <class T>
 __device__ __forceinline__ void fill_bias(float* table, const AttentionArgs& a, int head, int tid, int threads) {
-    for (int d = tid; d < 2 * a.reach + 1; d += threads) {
-        int b = a.bucket[d];
+    for (int i = tid; i < bias_width(a.reach); i += threads) {
+        int b = a.bucket[min(max(i - kBeyond, 0), 2 * a.reach)];
         if (b < 0 || b >= a.n_buckets) {
             atomicOr(a.err, kDevBadBucket);
             b = 0;
         }
-        table[d] = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head] * kLog2e;
+        table[i] = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head] * kLog2e;
     }
+}
+// Where a lane's smallest distance of a tile lies (59 places are read from there on), kept inside the table: beyond it all
+// places are alike.
+__device__ __forceinline__ const float* bias_from(const float* table, int reach, int distance) {
+    return table + min(max(distance + reach + kBeyond, 0), 2 * reach + 2 * kBeyond - 59);
 }
 
 // (the same in every lane, and the compiler is told so: branches on it are scalar)

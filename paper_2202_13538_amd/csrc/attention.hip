@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
     const int all_lo = wave_max(lo), all_hi = wave_min(hi);   // every row sees what lies between
     const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x3FFFFFFF);
+    if (!counts) diag = diag_min;
     int tile_lo = wave_lo, tile_hi = wave_hi;
     if (WR > 1) {
         if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
@@ -97,13 +98,13 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     }
 
     const float c = a.scale * kLog2e;   // scores in units of log 2
-    const int width = 2 * a.reach + 1;
+    const int width = bias_width(a.reach);
     if (a.bias != nullptr)
         for (int p = 0; p < o.pack; ++p) fill_bias<T>(bias + p * width, a, head0 + p, tid, kThreads);
     const float* const my_bias = bias + (row % o.pack) * width;
     __syncthreads();
     float bias_behind = 0.f, bias_ahead = 0.f;
-    if (a.bias != nullptr) bias_behind = my_bias[0], bias_ahead = my_bias[2 * a.reach];
+    if (a.bias != nullptr) bias_behind = my_bias[0], bias_ahead = my_bias[width - 1];
 
     const int kv_head = head0 / (a.heads / a.kv_heads);
     const char* const k_src = a.k + (int64_t)kv_head * a.k_head;
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
             for (int i = 0; i < 16; ++i) acc[db][i] *= shrink;
     };
     auto bias_at = [&](int key) {
-        return a.bias == nullptr ? 0.f : my_bias[min(max(key - diag, -a.reach), a.reach) + a.reach];
+        return a.bias == nullptr ? 0.f : my_bias[min(max(key - diag, -a.reach), a.reach) + a.reach + kBeyond];
     };
 
     if (key_begin < key_end) fetch(key_begin, 0);
@@ -153,13 +154,24 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
             const bool plain = whole && (a.bias == nullptr || behind || ahead);
             const float far = behind ? bias_behind : bias_ahead;
             if (!plain) {   // scores, in units of log 2, of what the row sees
+                if (a.bias != nullptr) {
+                    const float* const from = bias_from(my_bias, a.reach, key0 + 4 * g - diag);
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
+                    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int j = key0 + 32 * b + row_of(i, g);
-                        s[b][i] = j >= lo && j < last ? __builtin_fmaf(s[b][i], c, bias_at(j)) : -INFINITY;
-                    }
+                        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_fmaf(s[b][i], c, from[32 * b + row_of(i, 0)]);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) s[b] *= c;
+                }
+                if (!whole) {
+                    const uint32_t first = key0 + 4 * g - lo, span = max(last - lo, 0);
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            s[b][i] = first + (32 * b + row_of(i, 0)) < span ? s[b][i] : -INFINITY;
+                }
             }
             // Weights relative to a maximum of earlier keys: 32-bit sums and 16-bit floats are as exact
             // for weights of some hundreds as for those below one, so that most tiles need no rescaling.  With few
@@ -342,9 +354,11 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
     ForwardPlan p;
     const int group = a.heads / a.kv_heads;
     const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
-    // the bias of every head of a tile lies in LDS: 32 KB of it at most
-    auto fits = [&](int pack) { return a.bias == nullptr || pack == 1 || (int64_t)pack * (2 * a.reach + 1) * 4 <= 32768; };
-    p.across = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q;
+    // the bias of every head of a tile lies in LDS: 24 KB of it at most
+    auto fits = [&](int pack) { return a.bias == nullptr || pack == 1 || (int64_t)pack * bias_width(a.reach) * 4 <= 24576; };
+    // Tiles across sequences where these are short and alike.  With a bias the rows of a tile have to stand at
+    // neighbouring keys, which those of several sequences do only where queries and keys lie alike.
+    p.across = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q && (a.bias == nullptr || a.q_off == a.k_off);
     if (!p.across) {
         for (int d = 1; d <= group && d <= 32; ++d)
             if (group % d == 0 && fits(d) && mean_q * d <= 32) p.rows = 32, p.pack = d;
@@ -366,7 +380,7 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
 template <class T, int DP, int WR>
 hipError_t launch(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int64_t blocks) {
     const size_t bytes = ForwardShape<DP, WR>::kLds +
-                         (a.bias != nullptr ? (size_t)o.pack * (2 * a.reach + 1) * sizeof(float) : 0);
+                         (a.bias != nullptr ? (size_t)o.pack * bias_width(a.reach) * sizeof(float) : 0);
     auto kernel = attention_kernel<T, DP, WR>;
     if (bytes > 65536) {
         const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),

@@ -140,6 +140,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
     const int all_lo = wave_max(lo), all_hi = wave_min(hi);
     const int diag_min = wave_min(counts ? diag : 0x7FFFFFFF), diag_max = wave_max(counts ? diag : -0x3FFFFFFF);
+    if (!counts) diag = diag_min;
     if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
     if (a.bias != nullptr) fill_bias<T>(bias, a, head, tid, kThreads);
     __syncthreads();
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     const int lift = lift_of<T>(w, maxima, tid);
     const float c = a.scale * kLog2e, base = lse2 - (float)lift;   // ds comes out lifted
     float bias_behind = 0.f, bias_ahead = 0.f;
-    if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
+    if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[bias_width(a.reach) - 1];
 
     const int kv_head = head / (a.heads / a.kv_heads);
     const char* const k_src = a.k + (int64_t)kv_head * a.k_head;
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
         copy_tile<DP, kTileRows, kThreads>(k_tile + buffer * kTileBytes, k_src + (int64_t)key * a.k_row, a.k_row, rows, a.dim, tid);
         copy_tile<DP, kTileRows, kThreads>(v_tile + buffer * kTileBytes, v_src + (int64_t)key * a.v_row, a.v_row, rows, a.dim, tid);
     };
-    auto bias_at = [&](int key) { return a.bias == nullptr ? 0.f : bias[min(max(key - diag, -a.reach), a.reach) + a.reach]; };
+    auto bias_at = [&](int key) { return a.bias == nullptr ? 0.f : bias[min(max(key - diag, -a.reach), a.reach) + a.reach + kBeyond]; };
 
     f32x16 acc[NB];
 #pragma unroll
@@ -198,11 +199,18 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], c, add)) * (dp[i] - delta);
                 } else {
+                    if (a.bias != nullptr) {
+                        const float* const from = bias_from(bias, a.reach, key0 + 4 * g - diag);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, from[row_of(i, 0)]);
+                    } else {
+                        s *= c;
+                    }
+                    const uint32_t first = key0 + 4 * g - lo, span = hi - lo;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int j = key0 + row_of(i, g);
-                        const float p = exp2_fast(__builtin_fmaf(s[i], c, bias_at(j) - base));
-                        s[i] = j >= lo && j < hi ? p * (dp[i] - delta) : 0.f;
+                        const float ds = exp2_fast(s[i] - base) * (dp[i] - delta);
+                        s[i] = whole || first + row_of(i, 0) < span ? ds : 0.f;
                     }
                 }
 #pragma unroll
@@ -253,11 +261,13 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     char* const q_tile = lds;
     char* const o_tile = lds + 2 * kTileBytes;
     const int width = 2 * a.reach + 1;
-    float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);   // [width], the waves' sums [4][width], then
+    float* const sums_of_waves = reinterpret_cast<float*>(lds + 4 * kTileBytes);   // [4][width]
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int wr = wave % WR, wk = wave / WR;
-    float* const sums = bias + (1 + wave) * width;
-    float* const diagonals = bias + 5 * width + wave * 16 * kDiagonals;   // [4][16][kDiagonals]
+    float* const sums = sums_of_waves + wave * width;
+    float* const all_diagonals = sums_of_waves + 4 * width;                        // [4][16][kDiagonals]
+    float* const diagonals = all_diagonals + wave * 16 * kDiagonals;
+    float* const bias = all_diagonals + 4 * 16 * kDiagonals;
 
     const int kv_head = blockIdx.x % a.kv_heads, tile_no = blockIdx.x / a.kv_heads;
     const TileOfRows tile = tile_of_rows(a.k_off, a.n_seqs, a.n_k, 32 * WR, w.across_k, tile_no);
@@ -281,14 +291,14 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         lo = a.causal ? max(seq.q0, place) : seq.q0;
         if (hi <= lo || key < seq.k0 || key >= seq.k1) lo = hi = 0;
     }
-    const bool sees = counts && hi > lo;
+    const bool sees = counts && hi > lo, full = __all(counts);
     const int wave_lo = wave_min(sees ? lo : 0x7FFFFFFF), wave_hi = wave_max(sees ? hi : 0);
     const int all_lo = wave_max(counts ? lo : 0), all_hi = wave_min(counts ? hi : 0x7FFFFFFF);
     const int place_min = wave_min(counts ? place : 0x7FFFFFFF), place_max = wave_max(counts ? place : -0x3FFFFFFF);
     const int place0 = place_min;   // of the wave's first key: the others' lie behind it one by one
     if (lane == 0) range[0][wave] = wave_lo, range[1][wave] = wave_hi;
     if (a.bias != nullptr)
-        for (int i = tid; i < 4 * 16 * kDiagonals; i += kThreads) bias[5 * width + i] = 0.f;
+        for (int i = tid; i < 4 * 16 * kDiagonals; i += kThreads) all_diagonals[i] = 0.f;
     __syncthreads();
     int row_begin = 0x7FFFFFFF, row_end = 0;
 #pragma unroll
@@ -326,13 +336,13 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         }
         if (a.bias != nullptr) {
             fill_bias<T>(bias, a, h, tid, kThreads);
-            for (int d = tid; d < 4 * width; d += kThreads) bias[width + d] = 0.f;
+            for (int d = tid; d < 4 * width; d += kThreads) sums_of_waves[d] = 0.f;
         }
         float sum_behind = 0.f, sum_ahead = 0.f;   // of ds, distances of reach and more
         tile_arrived();
         __syncthreads();
         float bias_behind = 0.f, bias_ahead = 0.f;
-        if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[2 * a.reach];
+        if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[bias_width(a.reach) - 1];
         int buffer = 0;
 #pragma unroll 1
         for (int row = row_begin; row < row_end; row += kTileRows, buffer ^= 1) {
@@ -354,14 +364,22 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
 #pragma unroll
                     for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(p[i], c, add);
                 } else {
+                    if (a.bias != nullptr) {
+                        // (rows ahead lie at smaller distances: counted from the last of them)
+                        const float* const from = bias_from(bias, a.reach, place - (row0 + 4 * g) - 27);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int t = row0 + row_of(i, g);
-                        float add = 0.f;
-                        if (a.bias != nullptr) add = bias[min(max(place - t, -a.reach), a.reach) + a.reach];
-                        const bool seen = t >= lo && t < hi;
-                        p[i] = seen ? __builtin_fmaf(p[i], c, add) : -INFINITY;
-                        ds[i] = seen ? ds[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(p[i], c, from[27 - row_of(i, 0)]);
+                    } else {
+                        p *= c;
+                    }
+                    if (!whole || !full) {
+                        const uint32_t first = row0 + 4 * g - lo, span = hi - lo;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const bool seen = first + row_of(i, 0) < span;
+                            p[i] = seen ? p[i] : -INFINITY;
+                            ds[i] = seen ? ds[i] : 0.f;
+                        }
                     }
                 }
 #pragma unroll
@@ -423,7 +441,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
             }
             __syncthreads();
             for (int d = tid; d < width; d += kThreads)
-                by_distance(h)[d] = (bias[width + d] + bias[2 * width + d]) + (bias[3 * width + d] + bias[4 * width + d]);
+                by_distance(h)[d] = (sums_of_waves[d] + sums_of_waves[width + d]) + (sums_of_waves[2 * width + d] + sums_of_waves[3 * width + d]);
             __syncthreads();
         }
     }
@@ -534,10 +552,11 @@ struct GradPlan {
 GradPlan grad_plan(const AttentionArgs& a, int n_cu) {
     GradPlan p;
     const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
-    // Tiles across sequences where these are short and alike.  With a bias the keys of a tile have to lie at
-    // different places, which those of several sequences do only where queries and keys lie alike.
-    p.across_q = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q;
-    p.across_k = mean_k < 128 && mean_q <= 256 && mean_q <= 2 * mean_k && (a.bias == nullptr || a.q_off == a.k_off);
+    // Tiles across sequences where these are short and alike.  With a bias the rows (keys) of a tile have to
+    // stand at neighbouring keys (rows), which those of several sequences do only where queries and keys lie alike.
+    const bool may = a.bias == nullptr || a.q_off == a.k_off;
+    p.across_q = may && mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q;
+    p.across_k = may && mean_k < 128 && mean_q <= 256 && mean_q <= 2 * mean_k;
     p.twice = mean_k <= 256;
     p.q_tiles = tiles_of_rows(a.n_seqs, a.n_q, 128, p.across_q);
     p.keys = 128;
@@ -566,12 +585,12 @@ hipError_t launch_width(hipStream_t stream, const AttentionArgs& a, const GradAr
     const size_t tiles = 4 * (size_t)kTileRows * Tile<DP>::kRowBytes;
     const size_t width = a.bias != nullptr ? 2 * (size_t)a.reach + 1 : 0;
     auto kernel = attention_dq_kernel<T, DP>;
-    const size_t bytes = tiles + width * sizeof(float);
+    const size_t bytes = tiles + (width == 0 ? 0 : bias_width(a.reach) * sizeof(float));
     hipError_t rc = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (rc != hipSuccess) return rc;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.q_tiles * a.heads)), dim3(kThreads), bytes, stream, a, w);
     if ((rc = hipGetLastError()) != hipSuccess) return rc;
-    const size_t sums = width == 0 ? 0 : (5 * width + 4 * 16 * kDiagonals) * sizeof(float);
+    const size_t sums = width == 0 ? 0 : (4 * width + 4 * 16 * kDiagonals + bias_width(a.reach)) * sizeof(float);
     return p.keys == 64 ? launch_dkv<T, DP, 2>(stream, a, w, p, tiles + sums) : launch_dkv<T, DP, 4>(stream, a, w, p, tiles + sums);
 }
 
