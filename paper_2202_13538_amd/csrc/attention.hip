@@ -19,10 +19,11 @@ struct AttentionOut {
     int across = 0;
 };
 
-template <int DP, int WR>
+template <int DP, int WR, int WAVES>
 struct ForwardShape {
-    static constexpr int WK = 4 / WR;
-    static constexpr int kKeys = WK == 1 ? 64 : 32;  // keys that a wave takes at a time
+    static constexpr int WK = WAVES / WR;
+    static constexpr int kThreads = 64 * WAVES;
+    static constexpr int kKeys = WR > 1 ? 64 : 32;   // keys that a wave takes at a time
     static constexpr int kTileKeys = kKeys * WK;
     static constexpr int kBuffers = 2;
     static constexpr int kTileBytes = kTileKeys * Tile<DP>::kRowBytes;
@@ -34,12 +35,13 @@ struct ForwardShape {
 // rows in registers and computes scores^T = K q^T, so that a row's scores lie in one lane and its partner, the
 // softmax runs inside lanes, and the weights are the operand of out^T += V^T p^T as they come.
 //   WR = 4: four waves, 128 rows, all waves take every key tile.
-//   WR = 1: 32 rows (single tokens, a pooling row a set); the four waves take different keys of a tile of 128
-//           and join their sums at the end.
-template <class T, int DP, int WR>
-__global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_kernel(AttentionArgs a, AttentionOut o) {
-    using Shape = ForwardShape<DP, WR>;
-    constexpr int WK = Shape::WK, kBlocks = Shape::kKeys / 32, NB = DP / 32;
+//   WR = 1: 32 rows (single tokens, a pooling row a set); four waves take different keys of a tile of 128
+//           and join their sums at the end, or one wave takes all (WAVES = 1) where there are at most 64 or so: a
+//           workgroup is mostly waiting for its few loads then, and a quarter of the LDS lets more of them wait.
+template <class T, int DP, int WR, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_kernel(AttentionArgs a, AttentionOut o) {
+    using Shape = ForwardShape<DP, WR, WAVES>;
+    constexpr int WK = Shape::WK, kThreads = Shape::kThreads, kBlocks = Shape::kKeys / 32, NB = DP / 32;
     extern __shared__ __align__(16) char lds[];
     __shared__ int range[2][4];
     char* const k_tile = lds;
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionOut o
 }
 
 struct ForwardPlan {
-    int rows = 128, pack = 1, splits = 1;
+    int rows = 128, pack = 1, splits = 1, waves = 4;
     bool across = false;
     int64_t tiles = 0;
 };
@@ -366,44 +368,47 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
             for (int d = group; d >= 1; --d)
                 if (group % d == 0 && d <= 128 && fits(d) && (mean_q * d >= 128 || p.pack == 1 || d > p.pack)) p.pack = d;
     }
+    if (p.rows == 32 && mean_k <= 64) p.waves = 1;
     const int64_t heads = a.heads / p.pack;
     p.tiles = tiles_of_rows(a.n_seqs, a.n_q, p.rows / p.pack, p.across);
     const double full = p.across ? (double)p.tiles : a.n_seqs * ceil(mean_q * p.pack / p.rows);
     const double blocks = full * heads;
     if (blocks < 2 * n_cu) {
-        const double most = mean_k / (p.rows == 32 ? 256 : 256);
+        const double most = mean_k / 256;
         p.splits = (int)fmax(1.0, fmin(fmin(ceil(2.0 * n_cu / blocks), most), 128.0));
     }
     return p;
 }
 
-template <class T, int DP, int WR>
+template <class T, int DP, int WR, int WAVES>
 hipError_t launch(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int64_t blocks) {
-    const size_t bytes = ForwardShape<DP, WR>::kLds +
+    const size_t bytes = ForwardShape<DP, WR, WAVES>::kLds +
                          (a.bias != nullptr ? (size_t)o.pack * bias_width(a.reach) * sizeof(float) : 0);
-    auto kernel = attention_kernel<T, DP, WR>;
+    auto kernel = attention_kernel<T, DP, WR, WAVES>;
     if (bytes > 65536) {
         const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (rc != hipSuccess) return rc;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, stream, a, o);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), bytes, stream, a, o);
     return hipGetLastError();
 }
 
 template <class T, int DP>
-hipError_t launch_rows(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int rows, int64_t blocks) {
-    return rows == 32 ? launch<T, DP, 1>(stream, a, o, blocks) : launch<T, DP, 4>(stream, a, o, blocks);
+hipError_t launch_rows(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, const ForwardPlan& p, int64_t blocks) {
+    return p.rows == 128 ? launch<T, DP, 4, 4>(stream, a, o, blocks)
+           : p.waves == 4 ? launch<T, DP, 1, 4>(stream, a, o, blocks)
+                          : launch<T, DP, 1, 1>(stream, a, o, blocks);
 }
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, const ForwardPlan& p) {
     const int64_t blocks = p.tiles * (a.heads / p.pack) * p.splits;
     if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-    hipError_t rc = a.dim <= 32   ? launch_rows<T, 32>(stream, a, o, p.rows, blocks)
-                    : a.dim <= 64 ? launch_rows<T, 64>(stream, a, o, p.rows, blocks)
-                    : a.dim <= 96 ? launch_rows<T, 96>(stream, a, o, p.rows, blocks)
-                                  : launch_rows<T, 128>(stream, a, o, p.rows, blocks);
+    hipError_t rc = a.dim <= 32   ? launch_rows<T, 32>(stream, a, o, p, blocks)
+                    : a.dim <= 64 ? launch_rows<T, 64>(stream, a, o, p, blocks)
+                    : a.dim <= 96 ? launch_rows<T, 96>(stream, a, o, p, blocks)
+                                  : launch_rows<T, 128>(stream, a, o, p, blocks);
     if (rc != hipSuccess || p.splits == 1) return rc;
     const int64_t n_rows = (int64_t)a.n_q * a.heads;
     hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((n_rows + 3) / 4)), dim3(kThreads), 0, stream, o,
