@@ -467,7 +467,9 @@ typedef struct surel_attention_args {
  * rounded to `type` for their product with the values, the result once more.
  *   d_out   [n_q][heads][dim] of `type`, dense, on a 16-byte boundary (device, written).
  *   d_lse   float[n_q][heads] (device, written): the logarithm of the sum of exponentials.
- * A row that sees no key gets zeros, and a d_lse of minus infinity.  What a row does not see, another
+ * A bias of -65504 (fp16's lowest value) or less, minus infinity included, masks: keys at its distances have a
+ * weight of zero, and it has a gradient of zero.  A row that sees no key, or masked ones only, gets zeros and a
+ * d_lse of minus infinity.  What a row does not see, another
  * sequence's rows or later keys, has no influence on it, whatever it holds.
  * Where few rows meet many keys the keys are split over workgroups and the context's workspace grows
  * by 4 (dim + 2) bytes a row, head and part (128 parts at most).  Results are the same every time.

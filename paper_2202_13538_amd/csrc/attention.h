@@ -111,6 +111,13 @@ inline int64_t tiles_of_rows(int64_t n, int64_t total, int64_t rows, bool across
 // repeat the last ones: a tile of 64 keys (or rows) by 32 rows (or keys) that reaches into -reach .. reach
 // anywhere finds all of its distances there, by one address and constant offsets.
 constexpr int kBeyond = 96;
+// A bias of fp16's lowest value or less is a mask: minus infinity, which no 32-bit sum with a score rounds, so that the
+// weights that the gradients make again are zero as well, and a row that it leaves nothing is found by its sum of zero.
+template <class T>
+__device__ __forceinline__ float bias_of(const AttentionArgs& a, int bucket, int head) {
+    const float x = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)bucket * a.heads + head];
+    return x <= -65504.f ? -INFINITY : x * kLog2e;
+}
 __host__ __device__ constexpr int bias_width(int reach) { return 2 * reach + 1 + 2 * kBeyond; }
 template <class T>
 __device__ __forceinline__ void fill_bias(float* table, const AttentionArgs& a, int head, int tid, int threads) {
@@ -120,7 +127,7 @@ __device__ __forceinline__ void fill_bias(float* table, const AttentionArgs& a, 
             atomicOr(a.err, kDevBadBucket);
             b = 0;
         }
-        table[i] = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head] * kLog2e;
+        table[i] = bias_of<T>(a, b, head);
     }
 }
 // Where a lane's smallest distance of a tile lies (59 places are read from there on), kept inside the table: beyond it all

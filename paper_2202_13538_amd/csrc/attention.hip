@@ -248,7 +248,6 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
         }
     }
 
-
     if (WK > 1) {   // the waves' sums: 2 and 3 to 0 and 1, then 1 to 0
         float* const ml = reinterpret_cast<float*>(lds);            // [2][64]
         float* const sums = ml + 2 * 64;                            // [2][NB * 16][64]
@@ -298,8 +297,9 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
         return;
     }
     if (counts && g == 0) o.lse[at] = sees ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
-    const float scale = sees ? 1.f / sum : 0.f;
-    store_rows<T, DP>(acc, scale, !sees, lds + wr * 32 * Tile<DP>::kRowBytes, a.dim, lane, [&](int r) -> char* {
+    const bool none = !sees || sum == 0.f;   // (or all that it sees is masked by a bias)
+    const float scale = none ? 0.f : 1.f / sum;
+    store_rows<T, DP>(acc, scale, none, lds + wr * 32 * Tile<DP>::kRowBytes, a.dim, lane, [&](int r) -> char* {
         const int row_there = 32 * wr + r, token_there = tile.first + row_there / o.pack;
         if (token_there >= tile.last || row_there >= tokens * o.pack) return nullptr;
         return static_cast<char*>(o.out) + ((int64_t)token_there * a.heads + head0 + row_there % o.pack) * a.dim * 2;

@@ -36,6 +36,9 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* dst, int64_t n
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) dst[i] = 0;
 }
 
+// (a row that sees nothing, or nothing that its bias does not mask: all of its weights become zero)
+__device__ __forceinline__ float in_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
 // delta and lse by head, so that a tile's 64 rows lie behind one another (unless `twice`), and the largest |dout|.
 // 16 lanes a row and head, four of these at a time.
 template <class T>
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(Attention
             if (row < n_rows && c == 0) {
                 const int64_t at = (row % a.heads) * a.n_q + row / a.heads;
                 w.delta[at] = sum;
-                w.lse2[at] = w.lse[row] * kLog2e;
+                w.lse2[at] = in_log2(w.lse[row]);
             }
         }
     }
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     const int64_t by_head = (int64_t)head * a.n_q + token;
     float lse2 = 0.f, delta = 0.f;
     if (counts) {
-        if (w.twice) lse2 = w.lse[(int64_t)token * a.heads + head] * kLog2e;
+        if (w.twice) lse2 = in_log2(w.lse[(int64_t)token * a.heads + head]);
         else lse2 = w.lse2[by_head], delta = w.delta[by_head];
     }
     const int lift = lift_of<T>(w, maxima, tid);
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                     if (a.bias != nullptr) {
                         const int d = a.bucket[min(max(place - t, -a.reach), a.reach) + a.reach];
                         const int b = d < 0 || d >= a.n_buckets ? 0 : d;
-                        add = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + h] * kLog2e;
+                        add = bias_of<T>(a, b, h);
                     }
                     const int64_t at = (int64_t)h * a.n_q + t;
                     const float p = exp2_fast(__builtin_fmaf(dot, c, add - w.lse2[at]));

@@ -210,3 +210,43 @@ def test_offsets_of_elements_beyond_32_bits(ctx):
     near(out[1:], r["out"], b_out, "out")
     near(lse[1:], r["lse"], b_lse, "lse")
     assert not out[0].any() and torch.allclose(lse[0], torch.full((4,), float(np.log(n - 300)), device="cuda"), rtol=1e-5)
+
+
+MASKED = [  # lengths, keys' lengths or None, heads, kv_heads, dim
+    ([1, 16, 0, 16, 5], None, 2, 1, 32), ([300, 7], None, 4, 2, 64), ([200], None, 1, 1, 128), ([9, 2], [700, 3], 4, 2, 64),
+    ([1, 1, 1], [900, 2, 3000], 2, 1, 96), ([1] * 40, [3] * 40, 4, 4, 40),
+]
+
+
+def masked_inputs(shape, dtype, value, which):
+    """Inputs whose bias masks some distances, and what stands for them in 64 bits: (args, how, bias with -100 for
+    the mask, rows that it leaves nothing)."""
+    q_lens, k_lens, heads, kv_heads, dim = shape
+    q, k, v, q_off, k_off, how = inputs(q_lens, k_lens, heads, kv_heads, dim, dtype, seed=sum(q_lens), reach=16, buckets=9)
+    near = torch.arange(-16, 17).abs()
+    hidden = {"own": near == 0, "far": near == 16, "all": near >= 0}[which]
+    bucket = torch.where(hidden, 8, near % 8).int().cuda()
+    bias, stands = how["bias"].clone(), how["bias"].clone()
+    bias[8], stands[8] = value, -100.0
+    empty = torch.zeros(sum(q_lens), dtype=torch.bool)
+    off_q, off_k = q_off.tolist(), k_off.tolist()
+    for s in range(len(q_lens)):
+        for i in range(off_q[s], off_q[s + 1]):
+            at = off_k[s + 1] - (off_q[s + 1] - i)
+            seen = torch.arange(off_k[s], min(at + 1, off_k[s + 1]))
+            empty[i] = bool(hidden[(seen - at).clamp(-16, 16) + 16].all())
+    return (q, k, v, q_off, k_off), dict(bias=bias, bucket=bucket), dict(bias=stands, bucket=bucket), empty
+
+
+@pytest.mark.parametrize("dtype,value", [(BF, -float("inf")), (BF, torch.finfo(BF).min), (HF, torch.finfo(HF).min)], ids=str)
+@pytest.mark.parametrize("which", ["own", "far", "all"])
+@pytest.mark.parametrize("shape", MASKED, ids=str)
+def test_a_bias_that_masks(ctx, shape, which, dtype, value):
+    args, how, stands, empty = masked_inputs(shape, dtype, value, which)
+    out, lse = binding.attention(ctx, *args, causal=True, **how)
+    assert not out[empty].any() and (lse[empty] == -float("inf")).all()
+    r = reference(*args, True, shape[4] ** -0.5, **stands)
+    b_out, b_lse = bounds(r, dtype, shape[4], args[1].shape[0])
+    some = ~empty.numpy()
+    near(out[~empty], r["out"][some], b_out[some], "out")
+    near(lse[~empty], r["lse"][some], b_lse[some], "lse")

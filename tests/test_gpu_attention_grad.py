@@ -5,7 +5,7 @@ import torch
 
 from attention_cases import UNIT, inputs, offsets, reference
 from paper_2202_13538_amd import binding
-from test_gpu_attention import BF, CROSS, HF, SELF, near
+from test_gpu_attention import BF, CROSS, HF, MASKED, SELF, masked_inputs, near
 
 pytestmark = pytest.mark.gpu
 
@@ -164,3 +164,21 @@ def test_nothing_to_do(ctx):
         out, lse = binding.attention(ctx, q, k, k, qo, ko)
         for x in binding.attention_grad(ctx, torch.ones_like(q), q, k, k, out, lse, qo, ko)[:3]:
             assert not x.any()
+
+
+@pytest.mark.parametrize("dtype,value", [(BF, -float("inf")), (BF, torch.finfo(BF).min), (HF, torch.finfo(HF).min)], ids=str)
+@pytest.mark.parametrize("which", ["own", "far", "all"])
+@pytest.mark.parametrize("shape", MASKED, ids=str)
+def test_a_bias_that_masks(ctx, shape, which, dtype, value):
+    """What it hides has no part in any gradient; rows that it leaves nothing have none."""
+    args, how, stands, empty = masked_inputs(shape, dtype, value, which)
+    dout = torch.randn(args[0].shape, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    out, lse = binding.attention(ctx, *args, causal=True, **how)
+    got = binding.attention_grad(ctx, dout, *args[:3], out, lse, *args[3:], causal=True, **how)
+    scale = shape[4] ** -0.5
+    kept = torch.where(empty[:, None, None].cuda(), 0, dout)
+    r = reference(*args, True, scale, dout=kept, **stands)
+    b = bounds(r, *args[:3], dout, scale)
+    assert not got[0][empty].any() and not got[3][8].any()
+    for name, x in zip(("dq", "dk", "dv", "dbias"), got):
+        near(x, r[name], np.broadcast_to(b[name], r[name].shape), name)
