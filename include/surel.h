@@ -31,7 +31,8 @@
  *     contexts may work at the same time, on streams of their own.
  *   - The context owns grow-only device workspaces (per-seed / per-query row counts, scan
  *     partials, the walk's per-edge neighbour records, the fused kernel's look-back words,
- *     the hash tables and sort arrays of pruning and mini-batching)
+ *     the hash tables and sort arrays of pruning and mini-batching, what attention and the softmax
+ *     loss keep between their launches)
  *     and a device error word; nothing else is allocated.
  *   - Stream capture: a call that is given no h_* pointer only enqueues kernels (no memset,
  *     no copy, no wait), so once an eager call of the same shape has grown the workspaces it
@@ -469,8 +470,8 @@ typedef struct surel_attention_args {
  *   d_lse   float[n_q][heads] (device, written): the logarithm of the sum of exponentials.
  * A bias of -65504 (fp16's lowest value) or less, minus infinity included, masks: keys at its distances have a
  * weight of zero, and it has a gradient of zero.  A row that sees no key, or masked ones only, gets zeros and a
- * d_lse of minus infinity.  What a row does not see, another
- * sequence's rows or later keys, has no influence on it, whatever it holds.
+ * d_lse of minus infinity.  What a row does not see, another sequence's rows or later keys, has no influence on
+ * it, whatever it holds.  (Masked keys are seen: their values have to be finite.)
  * Where few rows meet many keys the keys are split over workgroups and the context's workspace grows
  * by 4 (dim + 2) bytes a row, head and part (128 parts at most).  Results are the same every time.
  * Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
@@ -485,9 +486,9 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
  * d_dout, d_out, d_dq, d_dk and d_dv start on 16-byte boundaries.  All sums are 32-bit; weights and score
  * gradients are rounded to `type` for their products (fp16: score gradients scaled by a power of two that
  * brings the largest |d_dout| below 1), results once more.  A query row that sees no key, and a
- * key that no row sees, get zeros.  The context's workspace grows by 8 bytes a row and head, and with a bias by
- * 4 (2 reach + 1) bytes a head and tile of 128 rows (as many tiles more as there are sequences).  Results are
- * the same every time.  Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
+ * key that no row sees, get zeros.  The context's workspace grows to 8 bytes a row and head, 4 KB, and with a bias
+ * 4 (2 reach + 1) bytes a head and tile of 64 or 128 keys (with as many tiles more as there are sequences).
+ * Results are the same every time.  Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
 int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
                          const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias);
 
@@ -499,7 +500,7 @@ int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const
  *   d_labels   int32[n_rows] (device, read-only); a negative one: the row does not count, its loss is 0.
  *   d_loss, d_lse   float[n_rows] (device, written); d_lse also of rows that do not count.
  * Logits and sums are 32-bit.  Classes stream by in parts, several of them at a time: the context's
- * workspace grows by 16 bytes a row and part (1,024 parts at most, 4,096 for up to 32 rows).  Results are the
+ * workspace grows by 16 bytes a row and part (1,024 parts at most, 4,096 for up to 128 rows).  Results are the
  * same every time.  Limits: n_rows >= 0 up to SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, dim a multiple of 8
  * up to SUREL_MAX_CLASS_DIM.  Asynchronous.  Device-detected: BAD_LABEL. */
 int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void* d_w, const int32_t* d_labels,

@@ -36,8 +36,8 @@ struct ForwardShape {
 // softmax runs inside lanes, and the weights are the operand of out^T += V^T p^T as they come.
 //   WR = 4: four waves, 128 rows, all waves take every key tile.
 //   WR = 1: 32 rows (single tokens, a pooling row a set); four waves take different keys of a tile of 128
-//           and join their sums at the end, or one wave takes all (WAVES = 1) where there are at most 64 or so: a
-//           workgroup is mostly waiting for its few loads then, and a quarter of the LDS lets more of them wait.
+//           and join their sums at the end, or one wave takes all (WAVES = 1): a quarter of the LDS and no barrier
+//           between waves, so that more tiles of a compute unit have loads in flight (see forward_plan).
 template <class T, int DP, int WR, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_kernel(AttentionArgs a, AttentionOut o) {
     using Shape = ForwardShape<DP, WR, WAVES>;
@@ -358,8 +358,10 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
     const double mean_q = (double)a.n_q / a.n_seqs, mean_k = (double)a.n_k / a.n_seqs;
     // the bias of every head of a tile lies in LDS: 24 KB of it at most
     auto fits = [&](int pack) { return a.bias == nullptr || pack == 1 || (int64_t)pack * bias_width(a.reach) * 4 <= 24576; };
-    // Tiles across sequences where these are short and alike.  With a bias the rows of a tile have to stand at
-    // neighbouring keys, which those of several sequences do only where queries and keys lie alike.
+    // Tiles across sequences where these are short and alike (8,192 walks of 17
+    // nodes 157 us against 269, 2,048 sequences of up to 80 rows 110 against 207, of 120 rows 147 against 152).  With a
+    // bias the rows of a tile have to stand at neighbouring keys, which those of several sequences do only where
+    // queries and keys lie alike.
     p.across = mean_q < 128 && mean_k <= 256 && mean_k <= 2 * mean_q && (a.bias == nullptr || a.q_off == a.k_off);
     if (!p.across) {
         for (int d = 1; d <= group && d <= 32; ++d)
@@ -368,11 +370,18 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
             for (int d = group; d >= 1; --d)
                 if (group % d == 0 && d <= 128 && fits(d) && (mean_q * d >= 128 || p.pack == 1 || d > p.pack)) p.pack = d;
     }
-    if (p.rows == 32 && mean_k <= 64) p.waves = 1;
     const int64_t heads = a.heads / p.pack;
     p.tiles = tiles_of_rows(a.n_seqs, a.n_q, p.rows / p.pack, p.across);
     const double full = p.across ? (double)p.tiles : a.n_seqs * ceil(mean_q * p.pack / p.rows);
     const double blocks = full * heads;
+    // 32 rows: one wave a tile where there are enough of these, or of their keys, to keep loads in flight; four, which take
+    // four times the LDS, where a tile's own keys have to be shared for that.  Four against one, in us: 32,768 tiles
+    // of 64 elements over 16 keys each 449 / 97, over 200 680 / 330, over 800 1,472 / 1,309, 2,048 of them over 2,000 239 / 262;
+    // 128 of 128 elements over 2,000 40 / 31, over 200 14.7 / 19.1; 32 over 500 14.5 / 21.9, over 32,768 119 / 105.  Of up to
+    // 64 elements in few tiles (8 over 100,000 keys 58 / 62) two workgroups of four waves fit a compute unit.
+    if (p.rows == 32 && ((blocks >= 2 * n_cu && mean_k <= 1024) || (a.dim > 64 && blocks * mean_k >= 256.0 * n_cu))) p.waves = 1;
+    // Keys are split where tiles do not fill the device, into parts of 256 at least, since a row's parts are
+    // written and joined: 32 tiles over 32,768 keys 542 us in one part, 119 in 16; four times the parts 129.
     if (blocks < 2 * n_cu) {
         const double most = mean_k / 256;
         p.splits = (int)fmax(1.0, fmin(fmin(ceil(2.0 * n_cu / blocks), most), 128.0));
