@@ -112,6 +112,11 @@ __device__ __forceinline__ int lift_of(const GradArgs& w, float* scratch, int ti
 // itself would need the keys' weighted sum as a fourth product.  With few keys a row the error is as
 // large as that of rounding ds, and the keys are there again at once: their ds are summed up in a round of
 // its own first (`twice`; walks of 16 steps, 262,144 rows of 8 heads of 64 elements: dq 0.0029 -> 0.0024 off).
+//
+// What bounds it: over walks, memory, keys and values once a round (16,384 walks of 16 steps with 8 heads of 64 elements
+// 0.37 ms); else vector instructions between three products a tile, at two waves a SIMD (5 causal sequences of 333 to
+// 4,096 rows with 16 heads of 128 elements 0.31 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.28).  Turns
+// unrolled over buffers, which gains elsewhere, lose here (378 -> 422 us with two rounds).
 template <class T, int DP>
 __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_dq_kernel(AttentionArgs a, GradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes;
@@ -254,6 +259,12 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 //   WR = 4: 128 keys, every wave takes all rows of a tile;
 //   WR = 2: 64 keys for twice as many workgroups: two waves share keys, take every other 32 rows, and add their
 //           sums up at the end.
+// What bounds it: over walks, memory and the sums by distance (16,384 walks of 16 steps with 8 heads of 64 elements
+// 0.48 ms); else the wait of one product for another, since keys, values and both sums leave registers for one
+// wave a SIMD of rows of 128 elements, two of shorter ones (5 causal sequences of 333 to 4,096 rows with 16 heads of
+// 128 elements to 4 of keys 0.79 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.46).  Tried at those sizes and slower:
+// dk and dv in launches of their own (448 + 720 us), p and ds by two waves that exchange them (805 and 718 us),
+// two blocks of rows at a time (over 900 us).
 template <class T, int DP, int WR>
 __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kernel(AttentionArgs a, GradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes, WK = 4 / WR;
@@ -509,7 +520,8 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     store_rows<T, DP>(dv, 1.f, !sees, mine, a.dim, lane, row_of_key(w.dv));
 }
 
-// A head's buckets: the tiles' sums of every distance, then the distances of every bucket, in a fixed order.
+// A head's buckets: the tiles' sums of every distance, then the distances of every bucket, in a fixed order.  One
+// workgroup a head, by its trips to memory: 8 heads of 2,048 tiles and 31 distances 10 us, 12 of 257 distances 18.
 constexpr int kBiasThreads = 1024;
 template <class T>
 __global__ __launch_bounds__(kBiasThreads) void attention_dbias_kernel(AttentionArgs a, GradArgs w) {
