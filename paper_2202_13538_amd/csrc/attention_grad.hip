@@ -17,6 +17,7 @@ constexpr int kThreads = 256;
 constexpr int kTileRows = 64;      // streamed rows of a tile
 constexpr int kMaxima = 1024;      // workgroups that look for the largest |dout|, at most
 constexpr int kDiagonals = 48;     // distances between 16 query rows and 32 keys (47), a row of LDS
+constexpr int kMaxReach = 1024;    // SUREL_MAX_REACH
 
 struct GradArgs {
     const char *dout = nullptr, *out = nullptr;  // [n_q][heads][dim]
@@ -520,43 +521,52 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     store_rows<T, DP>(dv, 1.f, !sees, mine, a.dim, lane, row_of_key(w.dv));
 }
 
-// A head's buckets: the tiles' sums of every distance, then the distances of every bucket, in a fixed order.  One
-// workgroup a head, by its trips to memory: 8 heads of 2,048 tiles and 31 distances 10 us, 12 of 257 distances 18.
+// One workgroup a head and bucket: the tiles' sums of all distances in it, in a fixed order.  By its trips to memory
+// (8 heads of 2,048 tiles of 31 distances in 16 buckets 6 us, one head of 1,466 of 257 in 16 buckets 15, and with a workgroup for
+// all buckets of a head 10 and 51).
 constexpr int kBiasThreads = 1024;
 template <class T>
 __global__ __launch_bounds__(kBiasThreads) void attention_dbias_kernel(AttentionArgs a, GradArgs w) {
-    __shared__ float part[kBiasThreads];
-    __shared__ float sums[2 * 1024 + 1];
-    __shared__ int bucket[2 * 1024 + 1];
-    const int width = 2 * a.reach + 1, head = blockIdx.x, tid = threadIdx.x;
+    __shared__ int bucket[2 * kMaxReach + 1];
+    __shared__ int mine[2 * kMaxReach + 1];   // the bucket's distances
+    __shared__ int n_mine;
+    __shared__ float part[kBiasThreads / 64];
+    const int width = 2 * a.reach + 1, head = blockIdx.x % a.heads, b = blockIdx.x / a.heads, tid = threadIdx.x;
+    const int wave = tid >> 6, lane = tid & 63;
+    for (int d = tid; d < width; d += kBiasThreads) {
+        const int x = a.bucket[d];
+        bucket[d] = x < 0 || x >= a.n_buckets ? 0 : x;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        int n = 0;
+        for (int d0 = 0; d0 < width; d0 += 64) {
+            const int d = d0 + lane;
+            const bool hit = d < width && bucket[d] == b;
+            const uint64_t hits = __ballot(hit);
+            if (hit) mine[n + __popcll(hits & ((1ull << lane) - 1))] = d;
+            n += __popcll(hits);
+        }
+        if (lane == 0) n_mine = n;
+    }
+    __syncthreads();
     // threads: as many distances as there are, up to 256 at a time, times slices of the tiles
-    int across = 16;
-    while (across < 256 && across < width) across *= 2;
+    int across = 1;
+    while (across < 256 && across < n_mine) across *= 2;
     const int slices = kBiasThreads / across, slice = tid / across;
-    for (int d0 = 0; d0 < width; d0 += across) {
-        const int d = d0 + tid % across;
-        float sum = 0.f;
-        if (d < width) {
+    float sum = 0.f;
+    for (int n = tid % across; n < n_mine; n += across) {
+        const float* const from = w.by_distance + (int64_t)head * w.k_tiles * width + mine[n];
 #pragma unroll 8
-            for (int t = slice; t < w.k_tiles; t += slices) sum += w.by_distance[((int64_t)head * w.k_tiles + t) * width + d];
-        }
-        part[tid] = sum;
-        __syncthreads();
-        if (slice == 0 && d < width) {
-            for (int s = 1; s < slices; ++s) sum += part[s * across + tid];
-            sums[d] = sum;
-            const int b = a.bucket[d];
-            bucket[d] = b < 0 || b >= a.n_buckets ? 0 : b;
-        }
-        __syncthreads();
+        for (int t = slice; t < w.k_tiles; t += slices) sum += from[(int64_t)t * width];
     }
-    for (int b = tid >> 6; b < a.n_buckets; b += kBiasThreads / 64) {
-        float sum = 0.f;
-        for (int d = tid & 63; d < width; d += 64) sum += bucket[d] == b ? sums[d] : 0.f;
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-        if ((tid & 63) == 0) static_cast<typename T::elem*>(w.dbias)[(int64_t)b * a.heads + head] = (typename T::elem)sum;
-    }
+    for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    if (tid != 0) return;
+    for (int n = 1; n < kBiasThreads / 64; ++n) sum += part[n];
+    static_cast<typename T::elem*>(w.dbias)[(int64_t)b * a.heads + head] = (typename T::elem)sum;
 }
 
 struct GradPlan {
@@ -629,7 +639,7 @@ hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArg
          : a.dim <= 96 ? launch_width<T, 96>(stream, a, w, p)
                        : launch_width<T, 128>(stream, a, w, p);
     if (rc != hipSuccess || a.bias == nullptr) return rc;
-    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)a.heads), dim3(kBiasThreads), 0, stream, a, w);
+    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)(a.heads * a.n_buckets)), dim3(kBiasThreads), 0, stream, a, w);
     return hipGetLastError();
 }
 
