@@ -589,9 +589,10 @@ GradPlan grad_plan(const AttentionArgs& a, int n_cu) {
     p.q_tiles = tiles_of_rows(a.n_seqs, a.n_q, 128, p.across_q);
     // Tiles of 64 keys where those of 128 are too few, or the longest of them too long: 4 causal sequences of 4,096 rows
     // with 16 heads of 128 elements to 4 of keys 1.32 ms against 1.57, 24 of 700 rows 0.48 both, but 200 of 700 rows
-    // with 8 heads of their own 2.87 against 2.40, and 8,192 walks of 17 nodes 0.53 against 0.44.
-    p.keys = 128;
-    if (a.kv_heads * ((double)a.n_k / 128 + (p.across_k ? 0 : 0.5 * a.n_seqs)) < 8 * n_cu) p.keys = 64;
+    // with 8 heads of their own 2.87 against 2.40.  Tiles of short sequences are all alike: 94 of them (1,000 of 12
+    // rows, 128 elements) 36 us against 39, but 375 70 against 61, 1,500 228 against 174.
+    const double full = a.kv_heads * ((double)a.n_k / 128 + (p.across_k ? 0 : 0.5 * a.n_seqs));
+    p.keys = full < (p.across_k ? 1 : 8) * n_cu ? 64 : 128;
     p.k_tiles = tiles_of_rows(a.n_seqs, a.n_k, p.keys, p.across_k);
     return p;
 }
