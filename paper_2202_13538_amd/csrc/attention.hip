@@ -234,13 +234,14 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
         __syncthreads();
     });
     sum += from_other_half(sum);
-    if (__any(has_nan(acc))) {   // once more, without what a row does not see
+    if (__any(has_nan(acc))) {   // the wave's keys once more, without what a row does not see
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
         top = sees ? -INFINITY : 0.f;
         sum = 0.f;
 #pragma unroll 1
-        for (int j = max(key_begin, wave_lo) + wk; j < min(key_end, wave_hi); j += WK) {
+        for (int j = max(key_begin, wave_lo); j < min(key_end, wave_hi); ++j) {
+            if (WK > 1 && (j - key_begin) / Shape::kKeys % WK != wk) continue;   // (another wave's, which may keep its sums)
             const float dot = dot_row<T, DP>(q, k_src + (int64_t)j * a.k_row, a.dim, lane);
             const bool seen = j >= lo && j < last;
             const float x = seen ? __builtin_fmaf(dot, c, bias_at(j)) : -INFINITY;
