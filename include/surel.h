@@ -450,7 +450,9 @@ int surel_bfs_batches(surel_ctx* ctx, const int32_t* d_queries, int64_t n_querie
  *                  place minus the place that the query row stands at.
  *   d_bucket       int32[2 * reach + 1] (device, read-only), entries in [0, n_buckets).
  * Limits: n_seqs >= 0, n_q and n_k up to SUREL_MAX_ROWS, dim a multiple of 8 up to SUREL_MAX_HEAD_DIM, strides
- * >= 0 up to SUREL_MAX_STRIDE, 0 <= reach <= SUREL_MAX_REACH, 1 <= heads <= 65535. */
+ * >= 0 up to SUREL_MAX_STRIDE, 0 <= reach <= SUREL_MAX_REACH, 1 <= heads <= 65535.  A call has less than 2^31
+ * workgroups, which (n_seqs + n_q / 16) * heads and, for gradients, (n_seqs + n_k / 64) * kv_heads below that
+ * always are (SUREL_E_RANGE otherwise). */
 typedef struct surel_attention_args {
     const void *d_q, *d_k, *d_v;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;

@@ -13,6 +13,8 @@
 
 namespace {
 
+constexpr int64_t kMostBlocks = 0x7FFFFFFF;   // workgroups of one launch
+
 bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 bool bad_stride(int64_t elements) { return elements < 0 || elements > SUREL_MAX_STRIDE || elements % 8 != 0; }
@@ -87,6 +89,7 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
     if (a.n_q > 0 && (!d_out || !d_lse)) return SUREL_E_NULL;
     if (misaligned16(d_out)) return SUREL_E_RANGE;
     if (a.n_q == 0) return SUREL_OK;
+    if (surel::attention_blocks(ctx->n_cu, a) > kMostBlocks) return SUREL_E_RANGE;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SUREL_E_HIP;
     if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::attention_scratch_bytes(ctx->n_cu, a)))
@@ -107,6 +110,7 @@ int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const
     if ((a.bias == nullptr) != (d_dbias == nullptr)) return SUREL_E_NULL;
     if (misaligned16(d_dout) || misaligned16(d_out) || misaligned16(d_dq) || misaligned16(d_dk) || misaligned16(d_dv))
         return SUREL_E_RANGE;
+    if (a.n_q > 0 && a.n_k > 0 && surel::attention_grad_blocks(ctx->n_cu, a) > kMostBlocks) return SUREL_E_RANGE;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SUREL_E_HIP;
     if (a.n_q == 0 || a.n_k == 0) {   // nothing meets anything

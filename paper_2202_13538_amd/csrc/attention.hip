@@ -17,6 +17,7 @@ struct AttentionOut {
     int splits = 1;
     int pack = 1;               // heads of a group that share a tile
     int across = 0;
+    int tiles = 0;              // of rows
 };
 
 template <int DP, int WR, int WAVES>
@@ -56,15 +57,15 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
     const int wr = WR == 1 ? 0 : wave, wk = WR == 1 ? wave : 0;
     const int n_head_tiles = a.heads / o.pack;
-    int block = blockIdx.x;
+    uint32_t block = block_number();
+    if (block == 0 && tid == 0) check_ends(a);
     const int head0 = block % n_head_tiles * o.pack;
     block /= n_head_tiles;
     const int split = block % o.splits;
     block /= o.splits;
-    const int n_tiles = gridDim.x / (n_head_tiles * o.splits);
-    if (blockIdx.x == 0 && tid == 0) check_ends(a);
+    if (block >= (uint32_t)o.tiles) return;
     // a causal sequence's last rows see the most keys: they come first
-    const int tile_no = a.causal ? n_tiles - 1 - block : block;
+    const int tile_no = a.causal ? o.tiles - 1 - (int)block : (int)block;
     const int tokens = 32 * WR / o.pack;
     const TileOfRows tile = tile_of_rows(a.q_off, a.n_seqs, a.n_q, tokens, o.across, tile_no);
     if (tile.first >= tile.last) return;
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
 // and a few trips to memory: 192 rows of 22 parts of 128 elements 8 us.
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionOut o, int64_t n_rows, int dim) {
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t row = (int64_t)block_number() * (kThreads / 64) + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (row >= n_rows) return;
     float m[2], l[2], top = -INFINITY, sum = 0.f;
@@ -396,6 +397,8 @@ ForwardPlan forward_plan(const AttentionArgs& a, int n_cu) {
     return p;
 }
 
+int64_t blocks_of(const AttentionArgs& a, const ForwardPlan& p) { return p.tiles * (a.heads / p.pack) * p.splits; }
+
 template <class T, int DP, int WR, int WAVES>
 hipError_t launch(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, int64_t blocks) {
     const size_t bytes = ForwardShape<DP, WR, WAVES>::kLds +
@@ -406,7 +409,7 @@ hipError_t launch(hipStream_t stream, const AttentionArgs& a, const AttentionOut
                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (rc != hipSuccess) return rc;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), bytes, stream, a, o);
+    hipLaunchKernelGGL(kernel, grid_of(blocks), dim3(64 * WAVES), bytes, stream, a, o);
     return hipGetLastError();
 }
 
@@ -419,7 +422,7 @@ hipError_t launch_rows(hipStream_t stream, const AttentionArgs& a, const Attenti
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const AttentionOut& o, const ForwardPlan& p) {
-    const int64_t blocks = p.tiles * (a.heads / p.pack) * p.splits;
+    const int64_t blocks = blocks_of(a, p);
     if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
     hipError_t rc = a.dim <= 32   ? launch_rows<T, 32>(stream, a, o, p, blocks)
                     : a.dim <= 64 ? launch_rows<T, 64>(stream, a, o, p, blocks)
@@ -427,8 +430,7 @@ hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const Attenti
                                   : launch_rows<T, 128>(stream, a, o, p, blocks);
     if (rc != hipSuccess || p.splits == 1) return rc;
     const int64_t n_rows = (int64_t)a.n_q * a.heads;
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((n_rows + 3) / 4)), dim3(kThreads), 0, stream, o,
-                       n_rows, a.dim);
+    hipLaunchKernelGGL(attention_join_kernel<T>, grid_of((n_rows + 3) / 4), dim3(kThreads), 0, stream, o, n_rows, a.dim);
     return hipGetLastError();
 }
 
@@ -439,6 +441,8 @@ size_t attention_scratch_bytes(int n_cu, const AttentionArgs& a) {
     return p.splits == 1 ? 0 : (size_t)p.splits * a.n_q * a.heads * (a.dim + 2) * sizeof(float);
 }
 
+int64_t attention_blocks(int n_cu, const AttentionArgs& a) { return blocks_of(a, forward_plan(a, n_cu)); }
+
 hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, void* out, float* lse,
                             void* scratch) {
     const ForwardPlan p = forward_plan(a, n_cu);
@@ -448,6 +452,7 @@ hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a
     o.splits = p.splits;
     o.pack = p.pack;
     o.across = p.across;
+    o.tiles = (int)p.tiles;
     if (p.splits > 1) {
         o.part_o = static_cast<float*>(scratch);
         o.part_ml = o.part_o + (int64_t)p.splits * a.n_q * a.heads * a.dim;

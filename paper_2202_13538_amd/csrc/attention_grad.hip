@@ -129,9 +129,10 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     float* const bias = reinterpret_cast<float*>(lds + 4 * kTileBytes);
     const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, g = lane >> 5, col = lane & 31;
 
-    const int head = blockIdx.x % a.heads;
-    const int block = blockIdx.x / a.heads, tile_no = a.causal ? w.q_tiles - 1 - block : block;
-    if (blockIdx.x == 0 && tid == 0) check_ends(a);
+    const uint32_t number = block_number();
+    const int head = number % a.heads, block = number / a.heads, tile_no = a.causal ? w.q_tiles - 1 - block : block;
+    if (number == 0 && tid == 0) check_ends(a);
+    if (block >= w.q_tiles) return;
     const TileOfRows tile = tile_of_rows(a.q_off, a.n_seqs, a.n_q, 128, w.across_q, tile_no);
     if (tile.first >= tile.last) return;
     const int token = tile.first + 32 * wave + col;
@@ -284,7 +285,9 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     float* const diagonals = all_diagonals + wave * 16 * kDiagonals;
     float* const bias = all_diagonals + 4 * 16 * kDiagonals;
 
-    const int kv_head = blockIdx.x % a.kv_heads, tile_no = blockIdx.x / a.kv_heads;
+    const uint32_t number = block_number();
+    const int kv_head = number % a.kv_heads, tile_no = number / a.kv_heads;
+    if (tile_no >= w.k_tiles) return;
     const TileOfRows tile = tile_of_rows(a.k_off, a.n_seqs, a.n_k, 32 * WR, w.across_k, tile_no);
     auto by_distance = [&](int head) { return w.by_distance + ((int64_t)head * w.k_tiles + tile_no) * width; };
     const int group = a.heads / a.kv_heads;
@@ -531,8 +534,10 @@ __global__ __launch_bounds__(kBiasThreads) void attention_dbias_kernel(Attention
     __shared__ int mine[2 * kMaxReach + 1];   // the bucket's distances
     __shared__ int n_mine;
     __shared__ float part[kBiasThreads / 64];
-    const int width = 2 * a.reach + 1, head = blockIdx.x % a.heads, b = blockIdx.x / a.heads, tid = threadIdx.x;
+    const uint32_t number = block_number();
+    const int width = 2 * a.reach + 1, head = number % a.heads, b = number / a.heads, tid = threadIdx.x;
     const int wave = tid >> 6, lane = tid & 63;
+    if (b >= a.n_buckets) return;
     for (int d = tid; d < width; d += kBiasThreads) {
         const int x = a.bucket[d];
         bucket[d] = x < 0 || x >= a.n_buckets ? 0 : x;
@@ -597,6 +602,10 @@ GradPlan grad_plan(const AttentionArgs& a, int n_cu) {
     return p;
 }
 
+int64_t blocks_of(const AttentionArgs& a, const GradPlan& p) {   // (buckets: below 2^28)
+    return p.q_tiles * a.heads > p.k_tiles * a.kv_heads ? p.q_tiles * a.heads : p.k_tiles * a.kv_heads;
+}
+
 size_t aligned(size_t x) { return (x + 255) / 256 * 256; }
 
 hipError_t allow_lds(const void* kernel, size_t bytes) {
@@ -608,7 +617,7 @@ hipError_t launch_dkv(hipStream_t stream, const AttentionArgs& a, const GradArgs
     auto kernel = attention_dkv_kernel<T, DP, WR>;
     const hipError_t rc = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (rc != hipSuccess) return rc;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.k_tiles * a.kv_heads)), dim3(kThreads), bytes, stream, a, w);
+    hipLaunchKernelGGL(kernel, grid_of(p.k_tiles * a.kv_heads), dim3(kThreads), bytes, stream, a, w);
     return hipGetLastError();
 }
 
@@ -620,7 +629,7 @@ hipError_t launch_width(hipStream_t stream, const AttentionArgs& a, const GradAr
     const size_t bytes = tiles + (width == 0 ? 0 : bias_width(a.reach) * sizeof(float));
     hipError_t rc = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (rc != hipSuccess) return rc;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.q_tiles * a.heads)), dim3(kThreads), bytes, stream, a, w);
+    hipLaunchKernelGGL(kernel, grid_of(p.q_tiles * a.heads), dim3(kThreads), bytes, stream, a, w);
     if ((rc = hipGetLastError()) != hipSuccess) return rc;
     const size_t sums = width == 0 ? 0 : (4 * width + 4 * 16 * kDiagonals + bias_width(a.reach)) * sizeof(float);
     return p.keys == 64 ? launch_dkv<T, DP, 2>(stream, a, w, p, tiles + sums) : launch_dkv<T, DP, 4>(stream, a, w, p, tiles + sums);
@@ -628,7 +637,7 @@ hipError_t launch_width(hipStream_t stream, const AttentionArgs& a, const GradAr
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
-    if (p.q_tiles * a.heads > 0x7FFFFFFF || p.k_tiles * a.kv_heads > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (blocks_of(a, p) > 0x7FFFFFFF) return hipErrorInvalidValue;
     hipError_t rc = hipSuccess;
     if (T::kNarrow || !p.twice) {
         hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)w.n_maxima), dim3(kThreads), 0, stream, a, w);
@@ -640,7 +649,7 @@ hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArg
          : a.dim <= 96 ? launch_width<T, 96>(stream, a, w, p)
                        : launch_width<T, 128>(stream, a, w, p);
     if (rc != hipSuccess || a.bias == nullptr) return rc;
-    hipLaunchKernelGGL(attention_dbias_kernel<T>, dim3((unsigned)(a.heads * a.n_buckets)), dim3(kBiasThreads), 0, stream, a, w);
+    hipLaunchKernelGGL(attention_dbias_kernel<T>, grid_of((int64_t)a.heads * a.n_buckets), dim3(kBiasThreads), 0, stream, a, w);
     return hipGetLastError();
 }
 
@@ -675,6 +684,8 @@ size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a) {
     GradArgs w;
     return lay_out(a, grad_plan(a, n_cu), nullptr, &w);
 }
+
+int64_t attention_grad_blocks(int n_cu, const AttentionArgs& a) { return blocks_of(a, grad_plan(a, n_cu)); }
 
 hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, const void* dout, const void* out,
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch) {

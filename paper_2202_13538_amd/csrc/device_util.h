@@ -22,6 +22,9 @@ constexpr uint32_t kDevBadOffsets = 0x200u;
 constexpr uint32_t kDevBadBucket = 0x400u;
 constexpr uint32_t kDevBadLabel = 0x800u;
 
+// The workgroup's number in a launch of grid_of(blocks): some more start than there are blocks.
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 __device__ __forceinline__ int lane_id() {
     return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
 }

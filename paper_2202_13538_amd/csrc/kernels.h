@@ -203,10 +203,20 @@ hipError_t launch_exclusive_scan(hipStream_t stream, int n_cu, const int32_t* co
                                  int64_t* off, int64_t* partials, void* small_scan,
                                  uint32_t spin_limit);
 
+// A grid for any number of workgroups below 2^31.  A launch counts the threads of a dimension in 32 bits; more are
+// not refused, their workgroups just never run.  Kernels take their number from block_number().
+inline dim3 grid_of(int64_t blocks) {
+    const int64_t rows = (blocks + (1 << 21) - 1) >> 21;   // 2^31 threads at most of workgroups of up to 1,024
+    return rows <= 1 ? dim3((unsigned)blocks) : dim3((unsigned)((blocks + rows - 1) / rows), (unsigned)rows);
+}
+// Whether one dimension is enough; launches whose plans keep workgroups few say so by this.
+inline bool fits_a_row(int64_t blocks, int threads) { return blocks * threads <= 0xFFFFFFFFll; }
+
 // attention.hip.  scratch: attention_scratch_bytes of device memory (0 where no keys are split).  half: fp16
 // instead of bf16.  Needs a.n_q >= 1 and a.n_seqs >= 1.
 struct AttentionArgs;
 size_t attention_scratch_bytes(int n_cu, const AttentionArgs& a);
+int64_t attention_blocks(int n_cu, const AttentionArgs& a);   // workgroups, to be below 2^31
 hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, void* out, float* lse,
                             void* scratch);
 
@@ -215,6 +225,7 @@ hipError_t launch_zero(hipStream_t stream, void* dst, int64_t n);
 // scratch: attention_grad_scratch_bytes of device memory.  dbias as a.bias (null or not).
 // Needs a.n_seqs, a.n_q, a.n_k >= 1.
 size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a);
+int64_t attention_grad_blocks(int n_cu, const AttentionArgs& a);   // of its largest launch, to be below 2^31
 hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, const void* dout, const void* out,
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch);
 

@@ -192,8 +192,9 @@ template <int WAVES>
 __global__ __launch_bounds__(kThreads) void loss_join_kernel(LossArgs a, LossOut o) {
     __shared__ float of_wave[3][kThreads / 64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int row = WAVES == 1 ? blockIdx.x * (kThreads / 64) + wave : blockIdx.x;
-    if (row >= a.n_rows) return;
+    const int64_t place = WAVES == 1 ? (int64_t)block_number() * (kThreads / 64) + wave : block_number();
+    if (place >= a.n_rows) return;
+    const int row = (int)place;
     Joined x;
 #pragma unroll 4
     for (int p = WAVES == 1 ? lane : threadIdx.x; p < o.row_parts; p += 64 * WAVES) {
@@ -234,6 +235,7 @@ LossPlan loss_plan(const LossArgs& a, int n_cu) {
 template <class T, int DP, int WR>
 hipError_t launch(hipStream_t stream, const LossArgs& a, const LossOut& o, const LossPlan& p) {
     const size_t bytes = 2 * LossShape<DP, WR>::kTileBytes;
+    if (!fits_a_row(p.tiles * p.splits, kThreads)) return hipErrorInvalidValue;
     auto kernel = loss_kernel<T, DP, WR>;
     if (bytes > 65536) {
         const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -277,8 +279,8 @@ hipError_t launch_loss(hipStream_t stream, int n_cu, const LossArgs& a, bool hal
     o.turns = p.alone ? turns : nullptr;
     const hipError_t rc = half ? launch_type<Fp16>(stream, a, o, p) : launch_type<Bf16>(stream, a, o, p);
     if (rc != hipSuccess || p.alone) return rc;
-    if (p.row_parts > 64) hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)a.n_rows), dim3(kThreads), 0, stream, a, o);
-    else hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(kThreads), 0, stream, a, o);
+    if (p.row_parts > 64) hipLaunchKernelGGL(loss_join_kernel<4>, grid_of(a.n_rows), dim3(kThreads), 0, stream, a, o);
+    else hipLaunchKernelGGL(loss_join_kernel<1>, grid_of(((int64_t)a.n_rows + 3) / 4), dim3(kThreads), 0, stream, a, o);
     return hipGetLastError();
 }
 

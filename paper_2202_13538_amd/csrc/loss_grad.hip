@@ -292,6 +292,7 @@ size_t lay_out(const LossArgs& a, const LossGradPlan& p, char* scratch, LossGrad
 template <class T>
 hipError_t add_parts(hipStream_t stream, const float* part, int splits, int64_t elements, void* out) {
     const int64_t n4 = elements / 4;
+    if (!fits_a_row((n4 + kThreads - 1) / kThreads, kThreads)) return hipErrorInvalidValue;
     hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)((n4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, part,
                        splits, n4, out);
     return hipGetLastError();
@@ -300,6 +301,7 @@ hipError_t add_parts(hipStream_t stream, const float* part, int splits, int64_t 
 template <class T, int DP>
 hipError_t launch_width(hipStream_t stream, const LossArgs& a, const LossGradArgs& w, const LossGradPlan& p) {
     const size_t bytes = 2 * (size_t)kStep * Tile<DP>::kRowBytes;   // 64 KB at most
+    if (!fits_a_row(p.tiles_h * p.splits_h, kThreads) || !fits_a_row(p.tiles_w * p.splits_w, kThreads)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((loss_dh_kernel<T, DP>), dim3((unsigned)(p.tiles_h * p.splits_h)), dim3(kThreads), bytes, stream, a, w);
     hipError_t rc = hipGetLastError();
     if (rc == hipSuccess && p.splits_h > 1)
