@@ -486,10 +486,11 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
  *                    (device, written): sums over all that read a row, heads of a group among them.
  *   d_dbias          [n_buckets][heads] of `type` (device, written) if there is a bias, else NULL.
  * d_dout, d_out, d_dq, d_dk and d_dv start on 16-byte boundaries.  All sums are 32-bit; weights and score
- * gradients are rounded to `type` for their products (fp16: score gradients scaled by a power of two that
- * brings the largest |d_dout| below 1), results once more.  A query row that sees no key, and a
- * key that no row sees, get zeros.  The context's workspace grows to 8 bytes a row and head, 4 KB, and with a bias
- * 4 (2 reach + 1) bytes a head and tile of 64 or 128 keys (with as many tiles more as there are sequences).
+ * gradients are rounded to `type` for their products (fp16: score gradients after a multiplication by a power of two, one
+ * of each query row and of each key, so that none overflows and small ones keep their bits), results once more.  A query
+ * row that sees no key, and a key that no row sees, get zeros.  The context's workspace grows to 8 bytes a row and head
+ * (fp16: 12, and 4 a key and key head), and with a bias 4 (2 reach + 1) bytes a head and tile of 64 or 128 keys (with as
+ * many tiles more as there are sequences).
  * Results are the same every time.  Asynchronous.  Device-detected: BAD_OFFSETS, BAD_BUCKET. */
 int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
                          const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias);

@@ -120,7 +120,8 @@ int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const
         if (rc == hipSuccess) rc = surel::launch_zero(ctx->stream, d_dbias, (int64_t)a.n_buckets * a.heads);
         return rc == hipSuccess ? SUREL_OK : SUREL_E_HIP;
     }
-    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::attention_grad_scratch_bytes(ctx->n_cu, a))) return rc;
+    if (int rc = grow_buffer(ctx, &ctx->d_model, &ctx->model_bytes, surel::attention_grad_scratch_bytes(ctx->n_cu, a, args->type == SUREL_FP16)))
+        return rc;
     KernelSpan span(ctx, SUREL_K_ATTENTION_GRAD);
     if (surel::launch_attention_grad(ctx->stream, ctx->n_cu, a, args->type == SUREL_FP16, d_dout, d_out, d_lse, d_dq, d_dk, d_dv,
                                      d_dbias, ctx->d_model) != hipSuccess)

@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTileRows = 64;      // streamed rows of a tile
-constexpr int kMaxima = 1024;      // workgroups that look for the largest |dout|, at most
+constexpr int kRowBlocks = 1024;   // workgroups of attention_grad_rows_kernel, at most
 constexpr int kDiagonals = 48;     // distances between 16 query rows and 32 keys (47), a row of LDS
 constexpr int kMaxReach = 1024;    // SUREL_MAX_REACH
 
@@ -25,9 +25,9 @@ struct GradArgs {
     char *dq = nullptr, *dk = nullptr, *dv = nullptr;
     void* dbias = nullptr;
     float *lse2 = nullptr, *delta = nullptr;  // [heads][n_q]: lse in units of log 2
-    float* maxima = nullptr;                  // [n_maxima], of parts of |dout| (fp16 only)
+    float* dout_size = nullptr;               // [heads][n_q]: lengths of dout's rows (fp16 only)
+    float* v_size = nullptr;                  // [kv_heads][n_k]: of values (fp16 only, unless `twice`)
     float* by_distance = nullptr;             // [heads][tiles][2 reach + 1]: ds of a tile of keys
-    int n_maxima = 0;
     int q_tiles = 0, k_tiles = 0;
     int across_q = 0, across_k = 0;
     int twice = 0;                            // delta from the weights themselves, see attention_dq_kernel
@@ -37,18 +37,30 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* dst, int64_t n
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) dst[i] = 0;
 }
 
+// The sum of eight fp16's squares.  (By dot products of packed pairs: unpacked ones would stay in registers until the
+// second look of the kernels below, which unpacks them too.  They may take subnormal numbers for zeros: lengths get
+// what 128 of those have at most, 2^-10.5, and a little more.)
+constexpr float kUnder = 0x1p-10f;
+__device__ __forceinline__ float square_of(const u32x4& x) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const Fp16::x2 p = __builtin_bit_cast(Fp16::x2, x[e]);
+        sum = __builtin_amdgcn_fdot2(p, p, sum, false);
+    }
+    return sum;
+}
+
 // (a row that sees nothing, or nothing that its bias does not mask: all of its weights become zero)
 __device__ __forceinline__ float in_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
-// delta and lse by head, so that a tile's 64 rows lie behind one another (unless `twice`), and the largest |dout|.
-// 16 lanes a row and head, four of these at a time.
+// delta and lse by head, so that a tile's 64 rows lie behind one another, and for fp16 the lengths of values.  16 lanes a
+// row and head, four of these at a time.
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(AttentionArgs a, GradArgs w) {
     constexpr int kEach = 4, kRows = kThreads / 16;
-    __shared__ float most_of[kThreads / 64];
     const int64_t n_rows = (int64_t)a.n_q * a.heads;
     const int c = threadIdx.x & 15;
-    float most = 0.f;
     for (int64_t first = (int64_t)blockIdx.x * kRows * kEach; first < n_rows; first += (int64_t)gridDim.x * kRows * kEach) {
         u32x4 x[kEach], y[kEach];
 #pragma unroll
@@ -57,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(Attention
             x[n] = y[n] = u32x4{0, 0, 0, 0};
             if (row < n_rows && c * 8 < a.dim) {
                 x[n] = *reinterpret_cast<const u32x4*>(w.dout + (row * a.dim + c * 8) * 2);
-                if (!w.twice) y[n] = *reinterpret_cast<const u32x4*>(w.out + (row * a.dim + c * 8) * 2);
+                y[n] = *reinterpret_cast<const u32x4*>(w.out + (row * a.dim + c * 8) * 2);
             }
         }
 #pragma unroll
@@ -68,9 +80,7 @@ __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(Attention
             for (int e = 0; e < 4; ++e) {
                 const f32x2 p = unpack2<T>(x[n][e]), q = unpack2<T>(y[n][e]);
                 sum = __builtin_fmaf(p[0], q[0], __builtin_fmaf(p[1], q[1], sum));
-                most = fmaxf(most, fmaxf(fabsf(p[0]), fabsf(p[1])));
             }
-            if (w.twice) continue;
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m);
             if (row < n_rows && c == 0) {
@@ -80,30 +90,43 @@ __global__ __launch_bounds__(kThreads) void attention_grad_rows_kernel(Attention
             }
         }
     }
-    if (T::kNarrow) {
+    if (!T::kNarrow) return;
+    const int64_t n_values = (int64_t)a.n_k * a.kv_heads;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + (threadIdx.x >> 4); row < n_values; row += (int64_t)gridDim.x * kRows) {
+        const int64_t key = row / a.kv_heads, head = row % a.kv_heads;
+        u32x4 x = {0, 0, 0, 0};
+        if (c * 8 < a.dim) x = *reinterpret_cast<const u32x4*>(a.v + key * a.v_row + head * a.v_head + c * 16);
+        float sum = square_of(x);
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-        if ((threadIdx.x & 63) == 0) most_of[threadIdx.x >> 6] = most;
-        __syncthreads();
-        if (threadIdx.x == 0) w.maxima[blockIdx.x] = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+        for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m);
+        if (c == 0) w.v_size[head * a.n_k + key] = sqrtf(sum) + kUnder;
     }
 }
 
-// What ds is multiplied by before it is rounded to fp16, a power of two: the largest |dout| becomes
-// 1/2 .. 1, so that a loss's small gradients do not fall below what fp16 can hold.  bf16 has the range
-// of 32-bit floats.  For all threads of a workgroup; `scratch` holds 4 words of LDS.
-template <class T>
-__device__ __forceinline__ int lift_of(const GradArgs& w, float* scratch, int tid) {
-    if (!T::kNarrow) return 0;
-    float most = 0.f;
-    for (int i = tid; i < w.n_maxima; i += kThreads) most = fmaxf(most, w.maxima[i]);
+// fp16 only.  What ds is multiplied by before it is rounded is a power of two of each query row (for dq) or key (for dk): it
+// brings a bound of the largest |ds| that the row or key can meet to 2^14 .. 2^15.  So nothing overflows, whatever values and
+// gradients are; rounded away is 2^-39 of the bound.  |ds_ij| = p |dp_ij - delta_i| is at most |dp_ij| + |delta_i|, and
+// |dp_ij| at most the length of do_i times that of v_j.  What is not finite has no say: who sees it is not finite anyway.
+// bf16 has the range of 32-bit floats.
+__device__ __forceinline__ int lift_for(float bound) {
+    return bound > 0.f && bound < INFINITY ? min(max(14 - ilogbf(bound), -60), 60) : 0;
+}
+__device__ __forceinline__ float finite_or_zero(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+// The largest of all threads of a workgroup; `scratch` holds 4 words of LDS of this call's own.
+__device__ __forceinline__ float largest_of_all(float x, float* scratch, int tid) {
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-    if ((tid & 63) == 0) scratch[tid >> 6] = most;
+    for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+    if ((tid & 63) == 0) scratch[tid >> 6] = x;
     __syncthreads();
-    most = fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3]));
-    if (!(most > 0.f) || !(most < INFINITY)) return 0;
-    return min(max(-1 - ilogbf(most), -60), 60);
+    return fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3]));
+}
+// The length of a lane's row (of fp16).
+template <int DP>
+__device__ __forceinline__ float size_of(const Stationary<DP>& row) {
+    float sum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) sum += square_of(row.k[ks]);
+    return sqrtf(sum + from_other_half(sum)) + kUnder;
 }
 
 // dq of 128 query rows of one head, 32 a wave.
@@ -167,8 +190,18 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
         if (w.twice) lse2 = in_log2(w.lse[(int64_t)token * a.heads + head]);
         else lse2 = w.lse2[by_head], delta = w.delta[by_head];
     }
-    const int lift = lift_of<T>(w, maxima, tid);
-    const float c = a.scale * kLog2e, base = lse2 - (float)lift;   // ds comes out lifted
+    const float c = a.scale * kLog2e;
+    int lift = 0;
+    float base = lse2, most = 0.f;   // base: less the lift, with which ds then comes out; most: |ds| and delta's share of it
+    if (T::kNarrow) {
+        const float size = size_of(dout);
+        if (counts && g == 0) w.dout_size[by_head] = size;
+        if (!w.twice) {
+            const float* const sizes = w.v_size + (int64_t)(head / (a.heads / a.kv_heads)) * a.n_k;
+            for (int i = tid; i < key_end - key_begin; i += kThreads) most = fmaxf(most, finite_or_zero(sizes[key_begin + i]));
+            most = size * largest_of_all(most, maxima, tid);
+        }
+    }
     float bias_behind = 0.f, bias_ahead = 0.f;
     if (a.bias != nullptr) bias_behind = bias[0], bias_ahead = bias[bias_width(a.reach) - 1];
 
@@ -188,6 +221,10 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
     float sum = 0.f;   // of ds
 #pragma unroll 1
     for (int round = w.twice ? 0 : 1; round < 2; ++round) {
+        if (T::kNarrow && round == 1) {
+            lift = lift_for(fmaxf(most, from_other_half(most)) + fabsf(delta));
+            base = lse2 - (float)lift;
+        }
         if (key_begin < key_end) fetch(key_begin, 0);
         tile_arrived();
         __syncthreads();
@@ -225,6 +262,10 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum += s[i];
+                if (T::kNarrow && round == 0) {   // (delta is zero still)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(s[i]));
+                }
                 if (round == 1) accumulate<T, DP>(acc, lds, kt, s, lane);   // (ds rounded to the inputs' 16 bits)
             }
             tile_arrived();
@@ -272,7 +313,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes, WK = 4 / WR;
     extern __shared__ __align__(16) char lds[];
     __shared__ int range[2][4];
-    __shared__ float maxima[4];
+    __shared__ float maxima[2][4];
     __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][-lse / scale, -delta][row]
     char* const q_tile = lds;
     char* const o_tile = lds + 2 * kTileBytes;
@@ -325,8 +366,20 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     Stationary<DP> k, v;
     k.load(a.k + (int64_t)key * a.k_row + (int64_t)kv_head * a.k_head, counts, a.dim, lane);
     v.load(a.v + (int64_t)key * a.v_row + (int64_t)kv_head * a.v_head, counts, a.dim, lane);
-    const int lift = lift_of<T>(w, maxima, tid);
-    const float c = a.scale * kLog2e, up = ldexpf(1.f, lift);
+    const float c = a.scale * kLog2e;
+    int lift = 0;
+    if (T::kNarrow) {
+        float size = 0.f, delta = 0.f;
+        for (int h = kv_head * group; h < (kv_head + 1) * group; ++h)
+            for (int i = tid; i < row_end - row_begin; i += kThreads) {   // (begin is beyond end where no row sees a key)
+                const int64_t at = (int64_t)h * a.n_q + row_begin + i;
+                size = fmaxf(size, finite_or_zero(w.dout_size[at]));
+                delta = fmaxf(delta, finite_or_zero(w.delta[at]));
+            }
+        size = largest_of_all(size, maxima[0], tid);
+        lift = lift_for(size * size_of(v) + largest_of_all(delta, maxima[1], tid));
+    }
+    const float up = ldexpf(1.f, lift);
 
     f32x16 dk[NB], dv[NB];
 #pragma unroll
@@ -488,7 +541,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                 }
             }
     }
-    if (WK > 1) {   // the second wave of a pair to the first
+    if (WK > 1) {   // the second wave of a pair to the first (they have the same keys, and lifts)
         float* const there = reinterpret_cast<float*>(lds) + wr * 2 * NB * 16 * 64 + lane;   // [WR][2 NB 16][64]
         __syncthreads();
         if (wk == 1) {
@@ -639,8 +692,10 @@ template <class T>
 hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArgs& w, const GradPlan& p) {
     if (blocks_of(a, p) > 0x7FFFFFFF) return hipErrorInvalidValue;
     hipError_t rc = hipSuccess;
-    if (T::kNarrow || !p.twice) {
-        hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)w.n_maxima), dim3(kThreads), 0, stream, a, w);
+    if (!p.twice) {
+        const int64_t blocks = ((int64_t)(a.n_q > a.n_k ? a.n_q : a.n_k) * a.heads + 63) / 64;
+        hipLaunchKernelGGL(attention_grad_rows_kernel<T>, dim3((unsigned)(blocks < kRowBlocks ? blocks : kRowBlocks)), dim3(kThreads), 0,
+                           stream, a, w);
         rc = hipGetLastError();
     }
     if (rc != hipSuccess) return rc;
@@ -654,7 +709,7 @@ hipError_t launch_type(hipStream_t stream, const AttentionArgs& a, const GradArg
 }
 
 // Where the parts of the scratch lie; returns its size.
-size_t lay_out(const AttentionArgs& a, const GradPlan& p, char* scratch, GradArgs* w) {
+size_t lay_out(const AttentionArgs& a, const GradPlan& p, bool half, char* scratch, GradArgs* w) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
         char* const here = scratch + at;
@@ -665,7 +720,8 @@ size_t lay_out(const AttentionArgs& a, const GradPlan& p, char* scratch, GradArg
     const size_t width = a.bias != nullptr ? (2 * (size_t)a.reach + 1) * sizeof(float) : 0;
     w->lse2 = reinterpret_cast<float*>(take(rows));
     w->delta = reinterpret_cast<float*>(take(rows));
-    w->maxima = reinterpret_cast<float*>(take(kMaxima * sizeof(float)));
+    w->dout_size = reinterpret_cast<float*>(take(half ? rows : 0));
+    w->v_size = reinterpret_cast<float*>(take(half && !p.twice ? (size_t)a.n_k * a.kv_heads * sizeof(float) : 0));
     w->by_distance = reinterpret_cast<float*>(take((size_t)p.k_tiles * a.heads * width));
     return at;
 }
@@ -680,9 +736,9 @@ hipError_t launch_zero(hipStream_t stream, void* dst, int64_t n) {
     return hipGetLastError();
 }
 
-size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a) {
+size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a, bool half) {
     GradArgs w;
-    return lay_out(a, grad_plan(a, n_cu), nullptr, &w);
+    return lay_out(a, grad_plan(a, n_cu), half, nullptr, &w);
 }
 
 int64_t attention_grad_blocks(int n_cu, const AttentionArgs& a) { return blocks_of(a, grad_plan(a, n_cu)); }
@@ -691,7 +747,7 @@ hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionAr
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch) {
     const GradPlan p = grad_plan(a, n_cu);
     GradArgs w;
-    lay_out(a, p, static_cast<char*>(scratch), &w);
+    lay_out(a, p, half, static_cast<char*>(scratch), &w);
     w.dout = static_cast<const char*>(dout);
     w.out = static_cast<const char*>(out);
     w.lse = lse;
@@ -704,8 +760,6 @@ hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionAr
     w.across_q = p.across_q;
     w.across_k = p.across_k;
     w.twice = p.twice;
-    const int64_t blocks = ((int64_t)a.n_q * a.heads + 63) / 64;   // of the kernel that goes over the rows
-    w.n_maxima = (int)(blocks < kMaxima ? blocks : kMaxima);
     return half ? launch_type<Fp16>(stream, a, w, p) : launch_type<Bf16>(stream, a, w, p);
 }
 

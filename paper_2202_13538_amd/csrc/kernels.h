@@ -224,7 +224,7 @@ hipError_t launch_attention(hipStream_t stream, int n_cu, const AttentionArgs& a
 hipError_t launch_zero(hipStream_t stream, void* dst, int64_t n);
 // scratch: attention_grad_scratch_bytes of device memory.  dbias as a.bias (null or not).
 // Needs a.n_seqs, a.n_q, a.n_k >= 1.
-size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a);
+size_t attention_grad_scratch_bytes(int n_cu, const AttentionArgs& a, bool half);
 int64_t attention_grad_blocks(int n_cu, const AttentionArgs& a);   // of its largest launch, to be below 2^31
 hipError_t launch_attention_grad(hipStream_t stream, int n_cu, const AttentionArgs& a, bool half, const void* dout, const void* out,
                                  const float* lse, void* dq, void* dk, void* dv, void* dbias, void* scratch);
