@@ -311,10 +311,14 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 template <class T, int DP, int WR>
 __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kernel(AttentionArgs a, GradArgs w) {
     constexpr int NB = DP / 32, kTileBytes = kTileRows * Tile<DP>::kRowBytes, WK = 4 / WR;
+    // fp16: weights, at most 1, are multiplied by 2^14 before they are rounded for dv, and ds with them: one of 2^-28, of a
+    // row that sees 2^28 keys alike, still has all its bits.  (As they are, weights of rows of 16,000 keys would be subnormal.)
+    constexpr int kWeightLift = T::kNarrow ? 14 : 0;
+    constexpr float kWeightDown = 1.f / (1 << kWeightLift);
     extern __shared__ __align__(16) char lds[];
     __shared__ int range[2][4];
     __shared__ float maxima[2][4];
-    __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][-lse / scale, -delta][row]
+    __shared__ __align__(16) float stats[2][2][kTileRows];   // [buffer][(lift of weights - lse) / scale, -delta][row]
     char* const q_tile = lds;
     char* const o_tile = lds + 2 * kTileBytes;
     const int width = 2 * a.reach + 1;
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         size = largest_of_all(size, maxima[0], tid);
         lift = lift_for(size * size_of(v) + largest_of_all(delta, maxima[1], tid));
     }
-    const float up = ldexpf(1.f, lift);
+    const float up = ldexpf(1.f, lift - kWeightLift);
 
     f32x16 dk[NB], dv[NB];
 #pragma unroll
@@ -399,7 +403,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
         };
         auto keep = [&](int buffer) {
             const int t = tid;
-            if (t < 2 * kTileRows) stats[buffer][t / kTileRows][t & (kTileRows - 1)] = stat * (t < kTileRows ? -1.f / c : -1.f);
+            if (t < 2 * kTileRows) stats[buffer][t / kTileRows][t & (kTileRows - 1)] = t < kTileRows ? (stat - kWeightLift) * (-1.f / c) : -stat;
         };
         if (row_begin < row_end) {
             fetch(row_begin, 0);
@@ -424,7 +428,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                 const int row0 = row + b;
                 if (row0 >= wave_hi || row0 + 32 <= wave_lo) continue;
                 const uint32_t qt = buffer * kTileBytes + b * Tile<DP>::kRowBytes, ot = qt + 2 * kTileBytes;
-                // (products start from -lse / scale and -delta, so that these need neither registers nor additions)
+                // (products start from these, so that these need neither registers nor additions)
                 f32x16 p = scores<T, DP>(lds, qt, k, lane, by_row(&stats[buffer][0][b], g));
                 f32x16 ds = scores<T, DP>(lds, ot, v, lane, by_row(&stats[buffer][1][b], g));
                 const bool whole = row0 >= all_lo && row0 + 32 <= all_hi;
@@ -512,7 +516,8 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
             }
             __syncthreads();
             for (int d = tid; d < width; d += kThreads)
-                by_distance(h)[d] = (sums_of_waves[d] + sums_of_waves[width + d]) + (sums_of_waves[2 * width + d] + sums_of_waves[3 * width + d]);
+                by_distance(h)[d] = ((sums_of_waves[d] + sums_of_waves[width + d]) +
+                                     (sums_of_waves[2 * width + d] + sums_of_waves[3 * width + d])) * kWeightDown;
             __syncthreads();
         }
     }
@@ -535,7 +540,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                         add = bias_of<T>(a, b, h);
                     }
                     const int64_t at = (int64_t)h * a.n_q + t;
-                    const float p = exp2_fast(__builtin_fmaf(dot, c, add - w.lse2[at]));
+                    const float p = exp2_fast(__builtin_fmaf(dot, c, add - w.lse2[at] + kWeightLift));
                     accumulate_row<T, DP>(dv, o_row, p, a.dim, g);
                     accumulate_row<T, DP>(dk, q_row, p * (dp - w.delta[at]) * up, a.dim, g);
                 }
@@ -574,7 +579,7 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
     };
     char* const mine = lds + wr * 32 * Tile<DP>::kRowBytes;
     store_rows<T, DP>(dk, ldexpf(a.scale, -lift), !sees, mine, a.dim, lane, row_of_key(w.dk));
-    store_rows<T, DP>(dv, 1.f, !sees, mine, a.dim, lane, row_of_key(w.dv));
+    store_rows<T, DP>(dv, kWeightDown, !sees, mine, a.dim, lane, row_of_key(w.dv));
 }
 
 // One workgroup a head and bucket: the tiles' sums of all distances in it, in a fixed order.  By its trips to memory

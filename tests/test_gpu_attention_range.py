@@ -1,4 +1,5 @@
-"""What fp16 can hold: score gradients of large values and of rows whose gradients are far smaller than others'."""
+"""What fp16 can hold: score gradients of large values and of rows whose gradients are far smaller than others', and weights of
+values over many keys."""
 import numpy as np
 import pytest
 import torch
@@ -75,3 +76,17 @@ def test_sequences_with_far_smaller_gradients_than_others(ctx, lens):
     dout[:sum(lens) // 2] *= 1e-4
     dout[sum(lens) // 2:] *= 10
     gradients(ctx, (q * 64).half(), (k / 64).half(), v, dout.half(), off, off, 32 ** -0.5)
+
+
+def test_values_over_many_keys_seen_alike(ctx):
+    """All weights are 1 / n, 100.5 of fp16's smallest steps: rounded as they are, they would be half a percent off."""
+    n, rows = 166_937, 64
+    g = torch.Generator().manual_seed(7)
+    q = torch.zeros(rows, 1, 8, dtype=HF, device="cuda")
+    k, v = torch.randn(n, 1, 8, generator=g).half().cuda(), torch.zeros(n, 1, 8, dtype=HF, device="cuda")
+    dout = (torch.rand(rows, 1, 8, generator=g) + 0.5).half().cuda()
+    offs = offsets([rows]), offsets([n])
+    out, lse = binding.attention(ctx, q, k, v, *offs)
+    dv = binding.attention_grad(ctx, dout, q, k, v, out, lse, *offs)[2].double()
+    want = dout.double().sum(0) / n
+    assert ((dv - want).abs() <= 2.25 * U * want).all(), ((dv - want).abs() / want).max().item()
