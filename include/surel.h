@@ -467,7 +467,8 @@ typedef struct surel_attention_args {
 
 /* Attention: for every query row i and head, out_i = sum_j p_ij v_j with p_i the softmax over the keys j
  * that row i sees of scale (q_i . k_j) + bias.  Scores, softmax and sums are 32-bit; the weights are
- * rounded to `type` for their product with the values, the result once more.
+ * rounded to `type` for their product with the values (fp16: those below 2^-21 of a row's largest lose bits, those below
+ * 2^-32 count for nothing), the result once more.
  *   d_out   [n_q][heads][dim] of `type`, dense, on a 16-byte boundary (device, written).
  *   d_lse   float[n_q][heads] (device, written): the logarithm of the sum of exponentials.
  * A bias of -65504 (fp16's lowest value) or less, minus infinity included, masks: keys at its distances have a

@@ -6,8 +6,13 @@ namespace surel {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kSlack = 8.f;    // how far (base 2) scores may lie above what weights are relative to, see the kernel
-constexpr float kMost = 1024.f;  // what a lane's weights of a tile may add up to
+constexpr float kSlack = 8.f;    // how far (base 2) scores may rise before weights are made relative to another one, see the kernel
+// fp16: weights are relative to 2^-7 of the largest, so that those down to 2^-21 of it keep all their bits, and stay below 2^15;
+// bf16 has the range of 32-bit floats.
+template <class T>
+constexpr float kBelow = T::kNarrow ? 7.f : 0.f;
+template <class T>
+constexpr float kMost = T::kNarrow ? 32768.f : 1024.f;  // what a lane's weights of a tile may add up to
 
 struct AttentionOut {
     void* out = nullptr;        // [n_q][heads][dim]
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
                                                   a.v_row, rows, a.dim, tid);
     };
     auto raise_top = [&](float most, bool mine) {
-        const float now = mine ? fmaxf(top, most) : top;
+        const float now = mine ? fmaxf(top, most - kBelow<T>) : top;
         const float shrink = now == top ? 1.f : exp2_fast(top - now);
         top = now;
         sum *= shrink;
@@ -211,14 +216,14 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
             };
             if constexpr (kBlocks > 1) {
                 const float most = largest();
-                const bool over = most > top + kSlack;
+                const bool over = most > top + (kSlack + kBelow<T>);
                 if (__any(over)) raise_top(most, over);
                 sum += weights(s);
             } else {
                 if (__any(top == -INFINITY)) raise_top(largest(), top == -INFINITY);
                 f32x16 p[kBlocks];
                 float part = weights(p);
-                const bool over = !(fmaxf(part, from_other_half(part)) < kMost);
+                const bool over = !(fmaxf(part, from_other_half(part)) < kMost<T>);
                 if (__any(over)) {
                     raise_top(largest(), over);
                     part = weights(p);

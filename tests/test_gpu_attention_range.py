@@ -1,12 +1,12 @@
-"""What fp16 can hold: score gradients of large values and of rows whose gradients are far smaller than others', and weights of
-values over many keys."""
+"""What fp16 can hold: score gradients of large values and of rows whose gradients are far smaller than others', weights of
+values over many keys, and weights far below the largest."""
 import numpy as np
 import pytest
 import torch
 
 from attention_cases import UNIT, inputs, offsets, reference
 from paper_2202_13538_amd import binding
-from test_gpu_attention import HF, near
+from test_gpu_attention import HF, bounds, near
 
 pytestmark = pytest.mark.gpu
 U = UNIT[HF]
@@ -90,3 +90,22 @@ def test_values_over_many_keys_seen_alike(ctx):
     dv = binding.attention_grad(ctx, dout, q, k, v, out, lse, *offs)[2].double()
     want = dout.double().sum(0) / n
     assert ((dv - want).abs() <= 2.25 * U * want).all(), ((dv - want).abs() / want).max().item()
+
+
+SINKS = [([1], [512], 1), ([1], [512], 300), ([300], [512], 1), ([1] * 600, [512] * 600, 1)]  # few rows, one wave a tile, 128 rows
+
+
+@pytest.mark.parametrize("q_lens,k_lens,heads", SINKS, ids=lambda x: str(x) if not isinstance(x, list) else f"{len(x)}x{x[0]}")
+def test_weights_far_below_the_largest(ctx, q_lens, k_lens, heads):
+    """One key of 32 scores 11.75, the others 0: their weights are 132.4 of fp16's smallest steps of the largest."""
+    n = sum(k_lens)
+    q, k = torch.zeros(sum(q_lens), heads, 8, dtype=HF, device="cuda"), torch.zeros(n, heads, 8, dtype=HF, device="cuda")
+    v = torch.ones(n, heads, 8, dtype=HF, device="cuda")
+    q[..., 0] = 4.0
+    k[7::32, :, 0], v[7::32] = 2.9375, 0.0
+    out, lse = binding.attention(ctx, q, k, v, offsets(q_lens), offsets(k_lens), scale=1.0)
+    r = reference(q[:1, :1], k[:512, :1], v[:512, :1], offsets([1]), offsets([512]), False, 1.0)
+    b_out, b_lse = bounds(r, HF, 8, 512)
+    shape = tuple(out.shape)
+    near(lse, np.broadcast_to(r["lse"], shape[:2]), np.broadcast_to(b_lse, shape[:2]), "lse")
+    near(out, np.broadcast_to(r["out"], shape), np.broadcast_to(b_out, shape), "out")
