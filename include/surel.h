@@ -439,7 +439,8 @@ int surel_bfs_batches(surel_ctx* ctx, const int32_t* d_queries, int64_t n_querie
  *   d_q            [n_q][heads][dim], d_k and d_v [n_k][kv_heads][dim] of `type` (device, read-only);
  *                  q_row, q_head, ... are the elements between rows and between heads, so that parts
  *                  of one larger tensor serve.  A head's row is contiguous.  Every head's row starts on a
- *                  16-byte boundary: pointers are multiples of 16 bytes, strides of 8 elements.
+ *                  16-byte boundary: pointers are multiples of 16 bytes, strides of 8 elements (any, >= 0, where
+ *                  there is one row or head).
  *   heads          a multiple of kv_heads: query head h reads key head h / (heads / kv_heads).
  *   d_q_off, d_k_off  int64[n_seqs+1] (device, read-only), from 0 to n_q and n_k; may be one array.
  *   causal         0, or 1: a sequence's last query row stands at its last key, and a row sees the keys

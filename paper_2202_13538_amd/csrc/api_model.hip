@@ -17,7 +17,11 @@ constexpr int64_t kMostBlocks = 0x7FFFFFFF;   // workgroups of one launch
 
 bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
-bool bad_stride(int64_t elements) { return elements < 0 || elements > SUREL_MAX_STRIDE || elements % 8 != 0; }
+// A stride between `count` rows or heads, and what the kernels get for it: one that leads nowhere may be any.
+bool bad_stride(int64_t elements, int64_t count) {
+    return elements < 0 || (count > 1 && (elements > SUREL_MAX_STRIDE || elements % 8 != 0));
+}
+uint32_t stride_bytes(int64_t elements, int64_t count) { return count > 1 ? (uint32_t)(2 * elements) : 0; }
 
 // Checks what an attention call was given, and says it in the kernels' words.
 int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::AttentionArgs* a) {
@@ -28,8 +32,8 @@ int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::A
         return SUREL_E_RANGE;
     if (x->dim < 8 || x->dim > SUREL_MAX_HEAD_DIM || x->dim % 8 != 0) return SUREL_E_RANGE;
     if (x->heads < 1 || x->heads > 65535 || x->kv_heads < 1 || x->heads % x->kv_heads != 0) return SUREL_E_RANGE;
-    if (bad_stride(x->q_row) || bad_stride(x->q_head) || bad_stride(x->k_row) || bad_stride(x->k_head) ||
-        bad_stride(x->v_row) || bad_stride(x->v_head))
+    if (bad_stride(x->q_row, x->n_q) || bad_stride(x->q_head, x->heads) || bad_stride(x->k_row, x->n_k) ||
+        bad_stride(x->k_head, x->kv_heads) || bad_stride(x->v_row, x->n_k) || bad_stride(x->v_head, x->kv_heads))
         return SUREL_E_RANGE;
     if (!(x->scale > 0.f) || !isfinite(x->scale)) return SUREL_E_RANGE;
     if (x->causal != 0 && x->causal != 1) return SUREL_E_RANGE;
@@ -46,9 +50,9 @@ int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::A
     a->q = static_cast<const char*>(x->d_q);
     a->k = static_cast<const char*>(x->d_k);
     a->v = static_cast<const char*>(x->d_v);
-    a->q_row = (uint32_t)(2 * x->q_row), a->q_head = (uint32_t)(2 * x->q_head);
-    a->k_row = (uint32_t)(2 * x->k_row), a->k_head = (uint32_t)(2 * x->k_head);
-    a->v_row = (uint32_t)(2 * x->v_row), a->v_head = (uint32_t)(2 * x->v_head);
+    a->q_row = stride_bytes(x->q_row, x->n_q), a->q_head = stride_bytes(x->q_head, x->heads);
+    a->k_row = stride_bytes(x->k_row, x->n_k), a->k_head = stride_bytes(x->k_head, x->kv_heads);
+    a->v_row = stride_bytes(x->v_row, x->n_k), a->v_head = stride_bytes(x->v_head, x->kv_heads);
     a->q_off = x->d_q_off, a->k_off = x->d_k_off;
     a->n_seqs = (int32_t)x->n_seqs, a->n_q = (int32_t)x->n_q, a->n_k = (int32_t)x->n_k;
     a->heads = x->heads, a->kv_heads = x->kv_heads, a->dim = x->dim;
