@@ -487,6 +487,7 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
  *   d_dq             [n_q][heads][dim], d_dk and d_dv [n_k][kv_heads][dim], of `type`, dense
  *                    (device, written): sums over all that read a row, heads of a group among them.
  *   d_dbias          [n_buckets][heads] of `type` (device, written) if there is a bias, else NULL.
+ * The scale has to be 2^-100 or more.
  * d_dout, d_out, d_dq, d_dk and d_dv start on 16-byte boundaries.  All sums are 32-bit; weights and score
  * gradients are rounded to `type` for their products (fp16: score gradients after a multiplication by a power of two, one
  * of each query row and of each key, so that none overflows and small ones keep their bits), results once more.  A query

@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int64_t kMostBlocks = 0x7FFFFFFF;   // workgroups of one launch
+constexpr float kLeastGradScale = 0x1p-100f;  // products of the gradients start from lse / scale, in 32 bits
 
 bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
@@ -24,7 +25,7 @@ bool bad_stride(int64_t elements, int64_t count) {
 uint32_t stride_bytes(int64_t elements, int64_t count) { return count > 1 ? (uint32_t)(2 * elements) : 0; }
 
 // Checks what an attention call was given, and says it in the kernels' words.
-int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::AttentionArgs* a) {
+int attention_args(const surel_ctx* ctx, const surel_attention_args* x, float least_scale, surel::AttentionArgs* a) {
     if (!x) return SUREL_E_NULL;
     if (x->type != SUREL_BF16 && x->type != SUREL_FP16) return SUREL_E_RANGE;
     if (x->n_seqs < 0 || x->n_seqs > SUREL_MAX_ROWS || x->n_q < 0 || x->n_q > SUREL_MAX_ROWS || x->n_k < 0 ||
@@ -35,7 +36,7 @@ int attention_args(const surel_ctx* ctx, const surel_attention_args* x, surel::A
     if (bad_stride(x->q_row, x->n_q) || bad_stride(x->q_head, x->heads) || bad_stride(x->k_row, x->n_k) ||
         bad_stride(x->k_head, x->kv_heads) || bad_stride(x->v_row, x->n_k) || bad_stride(x->v_head, x->kv_heads))
         return SUREL_E_RANGE;
-    if (!(x->scale > 0.f) || !isfinite(x->scale)) return SUREL_E_RANGE;
+    if (!(x->scale > 0.f) || x->scale < least_scale || !isfinite(x->scale)) return SUREL_E_RANGE;
     if (x->causal != 0 && x->causal != 1) return SUREL_E_RANGE;
     if ((x->d_bias == nullptr) != (x->d_bucket == nullptr)) return SUREL_E_NULL;
     if (x->d_bias && (x->n_buckets < 1 || x->n_buckets > 2 * SUREL_MAX_REACH + 1 || x->reach < 0 ||
@@ -89,7 +90,7 @@ extern "C" {
 
 int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_out, float* d_lse) {
     surel::AttentionArgs a;
-    if (int rc = attention_args(ctx, args, &a)) return rc;
+    if (int rc = attention_args(ctx, args, 0.f, &a)) return rc;
     if (a.n_q > 0 && (!d_out || !d_lse)) return SUREL_E_NULL;
     if (misaligned16(d_out)) return SUREL_E_RANGE;
     if (a.n_q == 0) return SUREL_OK;
@@ -108,7 +109,7 @@ int surel_attention(surel_ctx* ctx, const surel_attention_args* args, void* d_ou
 int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const void* d_dout, const void* d_out,
                          const float* d_lse, void* d_dq, void* d_dk, void* d_dv, void* d_dbias) {
     surel::AttentionArgs a;
-    if (int rc = attention_args(ctx, args, &a)) return rc;
+    if (int rc = attention_args(ctx, args, kLeastGradScale, &a)) return rc;
     if (a.n_q > 0 && (!d_dout || !d_out || !d_lse || !d_dq)) return SUREL_E_NULL;
     if (a.n_k > 0 && (!d_dk || !d_dv)) return SUREL_E_NULL;
     if ((a.bias == nullptr) != (d_dbias == nullptr)) return SUREL_E_NULL;
