@@ -453,7 +453,6 @@ static hipError_t launch_join_fill_cfg(const JoinJob& j) {
     if (lds_bytes > (size_t)j.max_lds_bytes) return hipErrorInvalidValue;
     hipError_t rc = allow_lds(reinterpret_cast<const void*>(join_fill_kernel<K, LT>), lds_bytes);
     if (rc != hipSuccess) return rc;
-    if (j.n_queries > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const int first_place = join_first_place(j.out_ids, j.out_cnt, 2 * K * LT);
     hipLaunchKernelGGL((join_fill_kernel<K, LT>), dim3((unsigned)j.n_queries), dim3(kWave),
                        lds_bytes, j.stream, j.rpe_off, j.rpe_ids, j.rpe_cnt, j.n_blocks, j.max_set,
@@ -525,11 +524,15 @@ hipError_t launch_join_count(hipStream_t stream, int max_lds_bytes, int n_cu, co
     JoinJob j{};
     j.stream = stream, j.max_lds_bytes = max_lds_bytes, j.n_cu = n_cu;
     j.rpe_off = rpe_off, j.rpe_ids = rpe_ids, j.n_blocks = n_blocks, j.m = 1, j.max_set = max_set;
-    j.queries = queries, j.n_queries = n_queries, j.counts = counts, j.err = err;
-    if (n_queries == 0) return hipSuccess;
-    if (k == 2) return launch_join_count_k<2>(j);
-    if (k == 3) return launch_join_count_k<3>(j);
-    return hipErrorInvalidValue;
+    j.err = err;
+    if (k != 2 && k != 3) return n_queries == 0 ? hipSuccess : hipErrorInvalidValue;
+    for (int64_t first = 0; first < n_queries; first += kSeedsOfALaunch) {
+        j.queries = queries + first * k, j.counts = counts + first;
+        j.n_queries = n_queries - first < kSeedsOfALaunch ? n_queries - first : kSeedsOfALaunch;
+        const hipError_t rc = k == 2 ? launch_join_count_k<2>(j) : launch_join_count_k<3>(j);
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_join_fill(hipStream_t stream, int max_lds_bytes, const int64_t* rpe_off,
@@ -540,13 +543,17 @@ hipError_t launch_join_fill(hipStream_t stream, int max_lds_bytes, const int64_t
     JoinJob j{};
     j.stream = stream, j.max_lds_bytes = max_lds_bytes;
     j.rpe_off = rpe_off, j.rpe_ids = rpe_ids, j.rpe_cnt = rpe_cnt, j.n_blocks = n_blocks, j.m = m;
-    j.max_set = max_set, j.queries = queries, j.n_queries = n_queries, j.join_off = join_off;
+    j.max_set = max_set;
     j.cap_rows = cap_rows, j.out_ids = out_ids, j.out_cnt = out_cnt, j.absent16 = absent16;
     j.err = err;
-    if (n_queries == 0) return hipSuccess;
-    if (k == 2) return launch_join_lt<2, false>(j);
-    if (k == 3) return launch_join_lt<3, false>(j);
-    return hipErrorInvalidValue;
+    if (k != 2 && k != 3) return n_queries == 0 ? hipSuccess : hipErrorInvalidValue;
+    for (int64_t first = 0; first < n_queries; first += kSeedsOfALaunch) {
+        j.queries = queries + first * k, j.join_off = join_off + first;
+        j.n_queries = n_queries - first < kSeedsOfALaunch ? n_queries - first : kSeedsOfALaunch;
+        const hipError_t rc = k == 2 ? launch_join_lt<2, false>(j) : launch_join_lt<3, false>(j);
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 // The one-launch join (up to 4,096 queries on 256 compute units; at that size it still takes half

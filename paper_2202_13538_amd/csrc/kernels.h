@@ -20,6 +20,17 @@ inline void launch_and_mark(Kernel kernel, dim3 grid, dim3 block, size_t lds_byt
     }
 }
 
+// A grid for any number of workgroups below 2^31.  A launch counts the threads of a dimension in 32 bits; more are
+// not refused, their workgroups just never run.  Kernels take their number from block_number().
+inline dim3 grid_of(int64_t blocks) {
+    const int64_t rows = (blocks + (1 << 21) - 1) >> 21;   // 2^31 threads at most of workgroups of up to 1,024
+    return rows <= 1 ? dim3((unsigned)blocks) : dim3((unsigned)((blocks + rows - 1) / rows), (unsigned)rows);
+}
+// Launches of a wavefront a seed or query go over these many at a time, so that their kernels need no second dimension.
+constexpr int64_t kSeedsOfALaunch = 1 << 25;
+// Whether one dimension is enough; launches whose plans keep workgroups few say so by this.
+inline bool fits_a_row(int64_t blocks, int threads) { return blocks * threads <= 0xFFFFFFFFll; }
+
 // walk.hip.  The per-edge neighbour records that launch_edge_records makes of a CSR (layouts in
 // walk_core.h; worth making when walks_want_records says so): edge_record_plan picks the layout
 // for a graph, the caller provides edge_record_bytes(plan, n_nodes, n_edges) bytes in plan.data.
@@ -202,15 +213,6 @@ int64_t scan_partials_len(int64_t n);
 hipError_t launch_exclusive_scan(hipStream_t stream, int n_cu, const int32_t* counts, int64_t n,
                                  int64_t* off, int64_t* partials, void* small_scan,
                                  uint32_t spin_limit);
-
-// A grid for any number of workgroups below 2^31.  A launch counts the threads of a dimension in 32 bits; more are
-// not refused, their workgroups just never run.  Kernels take their number from block_number().
-inline dim3 grid_of(int64_t blocks) {
-    const int64_t rows = (blocks + (1 << 21) - 1) >> 21;   // 2^31 threads at most of workgroups of up to 1,024
-    return rows <= 1 ? dim3((unsigned)blocks) : dim3((unsigned)((blocks + rows - 1) / rows), (unsigned)rows);
-}
-// Whether one dimension is enough; launches whose plans keep workgroups few say so by this.
-inline bool fits_a_row(int64_t blocks, int threads) { return blocks * threads <= 0xFFFFFFFFll; }
 
 // attention.hip.  scratch: attention_scratch_bytes of device memory (0 where no keys are split).  half: fp16
 // instead of bf16.  Needs a.n_q >= 1 and a.n_seqs >= 1.

@@ -121,10 +121,15 @@ hipError_t launch_rpe_count(hipStream_t stream, const int32_t* walks, int64_t n_
                                             (int)lds_bytes);
         if (rc != hipSuccess) return rc;
     }
-    const int64_t blocks = (n_seeds + kRpeWaves - 1) / kRpeWaves;
-    hipLaunchKernelGGL(rpe_count_kernel, dim3((unsigned)blocks), dim3(kRpeWaves * kWave), lds_bytes,
-                       stream, walks, n_seeds, n_key, n_nodes, slots, set_sizes, err);
-    return hipGetLastError();
+    for (int64_t first = 0; first < n_seeds; first += kSeedsOfALaunch) {
+        const int64_t n = n_seeds - first < kSeedsOfALaunch ? n_seeds - first : kSeedsOfALaunch;
+        const int64_t blocks = (n + kRpeWaves - 1) / kRpeWaves;
+        hipLaunchKernelGGL(rpe_count_kernel, dim3((unsigned)blocks), dim3(kRpeWaves * kWave), lds_bytes,
+                           stream, walks + first * n_key, n, n_key, n_nodes, slots, set_sizes + first, err);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 template <int E>
@@ -139,13 +144,19 @@ static hipError_t launch_rpe_fill_e(hipStream_t stream, const int32_t* walks, in
     const int words = (rpe_row_words(lds_rows, L) + 3) & ~3;
     const size_t lds_bytes = (size_t)kRpeWaves * words * 4;
     if (lds_bytes > 48 * 1024) return hipErrorInvalidValue;
-    const int64_t blocks = (n_seeds + kRpeWaves - 1) / kRpeWaves;
     const uint32_t magic_L = 65536u / (uint32_t)L + 1u;
     const auto kernel = table_goes_past(n_seeds, M, m) ? rpe_fill_kernel<E, kRpeWaves, true>
                                                        : rpe_fill_kernel<E, kRpeWaves, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRpeWaves * kWave), lds_bytes, stream, walks,
-                       n_seeds, M, m, n_nodes, magic_L, rpe_off, cap_rows, ids, cnt, words, lds_rows, err);
-    return hipGetLastError();
+    for (int64_t first = 0; first < n_seeds; first += kSeedsOfALaunch) {
+        const int64_t n = n_seeds - first < kSeedsOfALaunch ? n_seeds - first : kSeedsOfALaunch;
+        const int64_t blocks = (n + kRpeWaves - 1) / kRpeWaves;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRpeWaves * kWave), lds_bytes, stream,
+                           walks + first * M * L, n, M, m, n_nodes, magic_L, rpe_off + first, cap_rows, ids, cnt,
+                           words, lds_rows, err);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_rpe_fill(hipStream_t stream, const int32_t* walks, int64_t n_seeds, int32_t M,

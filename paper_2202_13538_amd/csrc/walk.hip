@@ -311,7 +311,6 @@ static hipError_t launch_walks_cfg(hipStream_t stream, const int32_t* row_ptr,
                                    int64_t n_edges, const int32_t* seeds, int64_t n_seeds,
                                    int32_t M, int32_t m, uint64_t rng_seed, int32_t* walks,
                                    int32_t* set_sizes, uint32_t* err) {
-    const int64_t blocks = (n_seeds + kWalkWavesPerBlock - 1) / kWalkWavesPerBlock;
     const int slots = !kCount ? 0 : kRec == kRecShort ? walk_table(M, m).slots : distinct_slots(1 + M * m);
     const size_t lds_bytes = (size_t)kWalkWavesPerBlock * (kWalkChains * kWave * (m + 1) + slots) * 4;
     if (lds_bytes > 48 * 1024) {
@@ -320,12 +319,18 @@ static hipError_t launch_walks_cfg(hipStream_t stream, const int32_t* row_ptr,
             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
         if (rc != hipSuccess) return rc;
     }
-    hipLaunchKernelGGL((walk_kernel<kCount, kRec>), dim3((unsigned)blocks),
-                       dim3(kWalkWavesPerBlock * kWave), lds_bytes, stream, row_ptr, col_idx,
-                       rec.data, rec.id_bits, rec.lo_bits, n_nodes, n_edges, seeds, n_seeds, M, m,
-                       (uint32_t)(rng_seed & 0xFFFFFFFFull), (uint32_t)(rng_seed >> 32), walks,
-                       set_sizes, slots, err);
-    return hipGetLastError();
+    for (int64_t first = 0; first < n_seeds; first += kSeedsOfALaunch) {
+        const int64_t n = n_seeds - first < kSeedsOfALaunch ? n_seeds - first : kSeedsOfALaunch;
+        const int64_t blocks = (n + kWalkWavesPerBlock - 1) / kWalkWavesPerBlock;
+        hipLaunchKernelGGL((walk_kernel<kCount, kRec>), dim3((unsigned)blocks),
+                           dim3(kWalkWavesPerBlock * kWave), lds_bytes, stream, row_ptr, col_idx,
+                           rec.data, rec.id_bits, rec.lo_bits, n_nodes, n_edges, seeds + first, n, M, m,
+                           (uint32_t)(rng_seed & 0xFFFFFFFFull), (uint32_t)(rng_seed >> 32),
+                           walks + first * M * (m + 1), kCount ? set_sizes + first : nullptr, slots, err);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_edge_records(hipStream_t stream, const int32_t* row_ptr, const int32_t* col_idx,
