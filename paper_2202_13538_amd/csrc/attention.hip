@@ -240,7 +240,10 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
         __syncthreads();
     });
     sum += from_other_half(sum);
-    if (__any(has_nan(acc))) {   // the wave's keys once more, without what a row does not see
+    // The wave's keys once more, without what a row does not see: for rows whose own scores are numbers.  (Where those are not, no
+    // result is.)
+    if (__any(sees && has_nan(acc) && sum == sum)) {
+        const float first_top = top, first_sum = sum;   // right whatever values are
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
         top = sees ? -INFINITY : 0.f;
@@ -256,6 +259,10 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
                 const float w = exp2_fast(x - (top == -INFINITY ? 0.f : top));
                 sum += w;
                 accumulate_row<T, DP>(acc, v_src + (int64_t)j * a.v_row, w, a.dim, g);
+            }
+            if ((j & 15) == 15 && __all(!sees || sum != sum || all_nan(acc))) {
+                top = first_top, sum = first_sum;
+                break;
             }
         }
     }

@@ -278,7 +278,8 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
         w.delta[by_head] = delta;
         if (w.twice) w.lse2[by_head] = lse2;
     }
-    if (__any(has_nan(acc))) {   // once more, without what a row does not see
+    // Once more, without what a row does not see: for rows whose score gradients are numbers, as their sum in delta shows.
+    if (__any(sees && has_nan(acc) && delta == delta)) {
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
 #pragma unroll 1
@@ -521,7 +522,26 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
             __syncthreads();
         }
     }
-    if (__any(has_nan(dk) || has_nan(dv))) {   // once more, without rows that do not see the key
+    // Once more, without rows that do not see the key: for sums that are not numbers though all that the key is seen by is.  (lse is
+    // none where a row's weights are, delta where its score gradients are.)
+    const bool dk_bad = sees && has_nan(dk), dv_bad = sees && has_nan(dv);
+    bool dk_none = false, dv_none = false;
+    auto unexplained = [&] { return __any((dk_bad && !dk_none) || (dv_bad && !dv_none)); };
+#pragma unroll 1
+    for (int h = kv_head * group; h < (kv_head + 1) * group && unexplained(); ++h)
+#pragma unroll 1
+        for (int t0 = wave_lo; t0 < wave_hi && unexplained(); t0 += 64) {
+            const int64_t at = (int64_t)h * a.n_q + min(t0 + lane, wave_hi - 1);
+            const bool weights = w.lse2[at] == w.lse2[at], scores = w.delta[at] == w.delta[at];
+#pragma unroll 1
+            for (uint64_t rows = __ballot(!weights || !scores), of_weights = __ballot(!weights); rows != 0; rows &= rows - 1) {
+                const int n = __builtin_ctzll(rows);
+                const bool seen = t0 + n >= lo && t0 + n < hi;
+                dk_none = dk_none || seen;
+                dv_none = dv_none || (seen && (of_weights >> n & 1) != 0);
+            }
+        }
+    if (unexplained()) {
 #pragma unroll
         for (int db = 0; db < NB; ++db) dk[db] = dv[db] = f32x16{};
 #pragma unroll 1
@@ -544,7 +564,13 @@ __global__ __launch_bounds__(kThreads, DP > 96 ? 1 : 2) void attention_dkv_kerne
                     accumulate_row<T, DP>(dv, o_row, p, a.dim, g);
                     accumulate_row<T, DP>(dk, q_row, p * (dp - w.delta[at]) * up, a.dim, g);
                 }
+                if ((t & 31) == 31 && __all(!sees || (dk_none && all_nan(dv)))) {   // nothing is left to find
+                    h = a.heads;
+                    break;
+                }
             }
+#pragma unroll
+        for (int db = 0; db < NB; ++db) dk[db] += dk_none ? NAN : 0.f;
     }
     if (WK > 1) {   // the second wave of a pair to the first (they have the same keys, and lifts)
         float* const there = reinterpret_cast<float*>(lds) + wr * 2 * NB * 16 * 64 + lane;   // [WR][2 NB 16][64]

@@ -233,8 +233,8 @@ __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const char* l
 
 // The same products one streamed row at a time, from global memory and in 32 bits throughout.  A tile's
 // product also multiplies what a row does not see, by a weight of zero: that is NaN where it is not finite.  Who
-// finds a sum that is not a number therefore goes over its rows again with these, and
-// leaves out what they do not see.
+// finds a sum that is not a number therefore goes over its rows again with these, and leaves out what they do
+// not see; but not, or no further, where all that it would find is that they see it themselves.
 template <class T, int DP>
 __device__ __forceinline__ float dot_row(const Stationary<DP>& b, const char* row, int dim, int lane) {
     float sum = 0.f;
@@ -307,6 +307,17 @@ __device__ __forceinline__ bool has_nan(const f32x16 (&acc)[NB]) {
     for (int db = 0; db < NB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) bad = bad || acc[db][i] != acc[db][i];
+    return bad;
+}
+
+// Whether nothing can change any more: what is not a number stays so.
+template <int NB>
+__device__ __forceinline__ bool all_nan(const f32x16 (&acc)[NB]) {
+    bool bad = true;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bad = bad && acc[db][i] != acc[db][i];
     return bad;
 }
 
