@@ -212,7 +212,15 @@ __global__ __launch_bounds__(kThreads, DP > 224 ? 1 : 2) void loss_dw_kernel(Los
         tile_arrived();
         __syncthreads();
     });
-    if (__any(has_nan(acc))) {   // once more, without the rows that do not count
+    // Once more, without the rows that do not count: unless one that does has no numbers, which no class's sum survives.
+    auto has_numbers = [&] {
+        bool none = false;
+#pragma unroll 1
+        for (int n = begin * kStep + lane; n < min(end * kStep, a.n_rows); n += 64)
+            none = none || (a.labels[n] >= 0 && a.labels[n] < a.n_classes && (w.lse[n] != w.lse[n] || w.dloss[n] != w.dloss[n]));
+        return !__any(none);
+    };
+    if (__any(has_nan(acc)) && has_numbers()) {
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
 #pragma unroll 1
