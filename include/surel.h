@@ -473,8 +473,8 @@ typedef struct surel_attention_args {
  *   d_out   [n_q][heads][dim] of `type`, dense, on a 16-byte boundary (device, written).
  *   d_lse   float[n_q][heads] (device, written): the logarithm of the sum of exponentials.
  * A bias of -65504 (fp16's lowest value) or less, minus infinity included, masks: keys at its distances have a
- * weight of zero, and it has a gradient of zero.  A row that sees no key, or masked ones only, gets zeros and a
- * d_lse of minus infinity.  What a row does not see, another sequence's rows or later keys, has no influence on
+ * weight of zero, and it has a gradient of zero.  A row that sees no key, or masked ones only (or
+ * none but keys whose scores are minus infinity), gets zeros and a d_lse of minus infinity.  What a row does not see, another sequence's rows or later keys, has no influence on
  * it, whatever it holds.  (Masked keys are seen: their values have to be finite.)
  * Where few rows meet many keys the keys are split over workgroups and the context's workspace grows
  * by 4 (dim + 2) bytes a row, head and part (128 parts at most).  Results are the same every time.
@@ -507,7 +507,9 @@ int surel_attention_grad(surel_ctx* ctx, const surel_attention_args* args, const
  *   d_loss, d_lse   float[n_rows] (device, written); d_lse also of rows that do not count.
  * Logits and sums are 32-bit.  Classes stream by in parts, several of them at a time: the context's
  * workspace grows by 16 bytes a row and part (1,024 parts at most, 4,096 for up to 128 rows).  Results are the
- * same every time.  Limits: n_rows >= 0 up to SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, dim a multiple of 8
+ * same every time.  Elements have to be finite, but for d_h of rows that do not count: a row with a logit that is not
+ * has NaN throughout (unless that is minus infinity and dim a multiple of 32).
+ * Limits: n_rows >= 0 up to SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, dim a multiple of 8
  * up to SUREL_MAX_CLASS_DIM.  Asynchronous.  Device-detected: BAD_LABEL. */
 int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void* d_w, const int32_t* d_labels,
                        int64_t n_rows, int32_t n_classes, int32_t dim, float* d_loss, float* d_lse);

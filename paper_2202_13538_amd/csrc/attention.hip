@@ -241,9 +241,9 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
     });
     sum += from_other_half(sum);
     // The wave's keys once more, without what a row does not see: for rows whose own scores are numbers.  (Where those are not, no
-    // result is.)
-    if (__any(sees && has_nan(acc) && sum == sum)) {
-        const float first_top = top, first_sum = sum;   // right whatever values are
+    // result is; but of heads that do not fill a tile's rows, what lies beyond them repeats their start, and 0 times infinity is none.)
+    if (__any(sees && has_nan(acc) && (sum == sum || a.dim != DP))) {
+        const float first_top = top, first_sum = sum;   // right whatever values are, if they are numbers
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
         top = sees ? -INFINITY : 0.f;
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 64 ? 2 : DP > 32 ? 3 : 4) void att
                 sum += w;
                 accumulate_row<T, DP>(acc, v_src + (int64_t)j * a.v_row, w, a.dim, g);
             }
-            if ((j & 15) == 15 && __all(!sees || sum != sum || all_nan(acc))) {
+            if ((j & 15) == 15 && __all(!sees || sum != sum || (first_sum == first_sum && all_nan(acc)))) {
                 top = first_top, sum = first_sum;
                 break;
             }

@@ -129,6 +129,21 @@ __device__ __forceinline__ float size_of(const Stationary<DP>& row) {
     return sqrtf(sum + from_other_half(sum)) + kUnder;
 }
 
+// The product of two rows in memory, by a lane and its partner.
+template <class T>
+__device__ __forceinline__ float dot_of_rows(const char* x, const char* y, int dim, int g) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c = g; c * 8 < dim; c += 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x2 p = unpack2<T>(reinterpret_cast<const uint32_t*>(x + c * 16)[e]);
+            const f32x2 q = unpack2<T>(reinterpret_cast<const uint32_t*>(y + c * 16)[e]);
+            sum = __builtin_fmaf(p[0], q[0], __builtin_fmaf(p[1], q[1], sum));
+        }
+    return sum + from_other_half(sum);
+}
+
 // dq of 128 query rows of one head, 32 a wave.
 //
 // delta_i = do_i . o_i comes from an o whose weights and results were rounded to 16 bits.  The sum of ds_ij over j
@@ -183,7 +198,8 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 
     Stationary<DP> q, dout;
     q.load(a.q + (int64_t)token * a.q_row + (int64_t)head * a.q_head, counts, a.dim, lane);
-    dout.load(w.dout + ((int64_t)token * a.heads + head) * a.dim * 2, counts, a.dim, lane);
+    const int64_t row_bytes = ((int64_t)token * a.heads + head) * a.dim * 2;
+    dout.load(w.dout + row_bytes, counts, a.dim, lane);
     const int64_t by_head = (int64_t)head * a.n_q + token;
     float lse2 = 0.f, delta = 0.f;
     if (counts) {
@@ -271,14 +287,17 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
             tile_arrived();
             __syncthreads();
         }
-        delta += ldexpf(sum + from_other_half(sum), -lift);
+        const float off = ldexpf(sum + from_other_half(sum), -lift);
         sum = 0.f;
+        if (off == off) delta += off;
+        else if (round == 0 && counts) delta = dot_of_rows<T>(w.dout + row_bytes, w.out + row_bytes, a.dim, g);
     }
     if (counts && g == 0) {
         w.delta[by_head] = delta;
         if (w.twice) w.lse2[by_head] = lse2;
     }
-    // Once more, without what a row does not see: for rows whose score gradients are numbers, as their sum in delta shows.
+    // Once more, without what a row does not see: for rows whose score gradients are numbers, as delta shows, which is do . out
+    // where their sum is none.  (It need not be theirs: beyond a head's width a tile repeats its start, and 0 times infinity is none.)
     if (__any(sees && has_nan(acc) && delta == delta)) {
 #pragma unroll
         for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
