@@ -632,7 +632,11 @@ def attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     tensor will do).  Sequence s has rows q_off[s] .. q_off[s+1]-1 and keys k_off[s] .. k_off[s+1]-1 (int64,
     like join_off and rpe_off; k_off None: the same as q_off).  causal: a sequence's last row stands at its
     last key, rows see keys up to their own.  scale None: 1 / sqrt(dim).  bias [buckets][heads] and bucket
-    int32[2 * reach + 1] (see distance_buckets): a learned bias by the distance of key and row."""
+    int32[2 * reach + 1] (see distance_buckets): a learned bias by the distance of key and row.
+
+    Sequences that attend to themselves share one q_off (k_off None, or the same tensor): with a bias, two tensors of the
+    same numbers are slower where sequences are short.  The result has no gradient of its own, whatever its inputs
+    require: attention_grad computes them (examples/walk_model.py makes a torch.autograd.Function of both)."""
     args = _attention_args(q, k, v, q_off, k_off, causal, scale, bias, bucket)
     out = q.new_empty(q.shape)
     lse = q.new_empty(q.shape[:2], dtype=torch.float32)
@@ -701,7 +705,8 @@ def _loss_shape(h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor) -> tuple
 def softmax_loss(ctx: Context, h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor):
     """(loss float32[rows], lse float32[rows]) on the GPU: softmax cross entropy of rows h [rows][dim] against all
     classes w [classes][dim] (bfloat16 or float16, dense), of which labels int32[rows] names each row's; a
-    negative label: the row does not count, its loss is 0.  Logits are not kept."""
+    negative label: the row does not count, its loss is 0.  Logits are not kept.  The result has no gradient of its own,
+    whatever its inputs require: softmax_loss_grad computes them."""
     kind, n, classes, dim = _loss_shape(h, w, labels)
     loss = h.new_empty(n, dtype=torch.float32)
     lse = h.new_empty(n, dtype=torch.float32)

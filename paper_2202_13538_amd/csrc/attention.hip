@@ -46,7 +46,7 @@ struct ForwardShape {
 //           between waves, so that more tiles of a compute unit have loads in flight (see forward_plan).
 // What bounds it: with 128 rows the matrix units, and beside them the seven vector instructions a score (16,384 causal rows of
 // 16 heads of 128 elements 1.07 ms, 1.03 PFLOP/s of the 1.12 of a large product; 5 causal sequences of 333 to 4,096 rows
-// with a bias 0.23 ms); over walks of 16 steps, memory (16,384 of them with 8 heads of 64 elements 0.26 ms, 4.1 TB/s).
+// with a bias 0.21 ms); over walks of 16 steps, memory (16,384 of them with 8 heads of 64 elements 0.25 ms, 4.3 TB/s).
 // With 32 rows, memory: 8,192 pooling rows over up to 1,602 keys 0.60 ms, 5.6 TB/s, nearly all of it read.
 // (A pooling row fills one of a wave's 32 columns a head; the other columns' products cost nothing that shows.)
 template <class T, int DP, int WR, int WAVES>

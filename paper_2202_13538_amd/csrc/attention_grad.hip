@@ -153,8 +153,8 @@ __device__ __forceinline__ float dot_of_rows(const char* x, const char* y, int d
 // its own first (`twice`; walks of 16 steps, 262,144 rows of 8 heads of 64 elements: dq 0.0029 -> 0.0024 off).
 //
 // What bounds it: over walks, memory, keys and values once a round (16,384 walks of 16 steps with 8 heads of 64 elements
-// 0.37 ms); else vector instructions between three products a tile, at two waves a SIMD (5 causal sequences of 333 to
-// 4,096 rows with 16 heads of 128 elements 0.31 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.28).  Turns
+// 0.36 ms); else vector instructions between three products a tile, at two waves a SIMD (5 causal sequences of 333 to
+// 4,096 rows with 16 heads of 128 elements 0.29 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.27).  Turns
 // unrolled over buffers, which gains elsewhere, lose here (378 -> 422 us with two rounds).
 template <class T, int DP>
 __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void attention_dq_kernel(AttentionArgs a, GradArgs w) {
@@ -323,9 +323,9 @@ __global__ __launch_bounds__(kThreads, DP > 64 ? 2 : DP > 32 ? 3 : 4) void atten
 //   WR = 2: 64 keys for twice as many workgroups: two waves share keys, take every other 32 rows, and add their
 //           sums up at the end.
 // What bounds it: over walks, memory and the sums by distance (16,384 walks of 16 steps with 8 heads of 64 elements
-// 0.48 ms); else the wait of one product for another, since keys, values and both sums leave registers for one
+// 0.46 ms); else the wait of one product for another, since keys, values and both sums leave registers for one
 // wave a SIMD of rows of 128 elements, two of shorter ones (5 causal sequences of 333 to 4,096 rows with 16 heads of
-// 128 elements to 4 of keys 0.79 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.46).  Tried at those sizes and slower:
+// 128 elements to 4 of keys 0.73 ms, 24 of up to 2,048 with 12 heads of 80 elements 0.45).  Tried at those sizes and slower:
 // dk and dv in launches of their own (448 + 720 us), p and ds by two waves that exchange them (805 and 718 us),
 // two blocks of rows at a time (over 900 us).
 template <class T, int DP, int WR>

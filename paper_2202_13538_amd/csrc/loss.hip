@@ -66,9 +66,9 @@ struct LossShape {
 //   WR = 4: 256 rows, every wave 64 of them and all classes of a tile;
 //   WR = 1: 32 rows, the waves take different classes of a tile.
 // What bounds it: 16 rows against 2,900,000 classes of 128 elements, reading these (120 us, 6.2 TB/s); 15,001 rows against
-// 99,991 classes of 200 elements, the matrix units (0.56 ms, 1.08 PFLOP/s; 8,192 rows against 235,000 of 128 0.55 ms,
-// 0.90); of 64 elements the exponentials between products that are as short as they (2,048 rows against 2,900,000
-// 1.24 ms, 0.61 PFLOP/s).
+// 99,991 classes of 200 elements, the matrix units (0.54 ms, 1.11 PFLOP/s; 8,192 rows against 235,000 of 128 0.48 ms,
+// 1.03); of 64 elements the exponentials between products that are as short as they (2,048 rows against 2,900,000
+// 1.19 ms, 0.64 PFLOP/s).  (Of a warm device, as all times here: the first passes take up to an eighth longer.)
 template <class T, int DP, int WR>
 __global__ __launch_bounds__(kThreads, 2) void loss_kernel(LossArgs a, LossOut o) {
     using Shape = LossShape<DP, WR>;

@@ -7,8 +7,8 @@
 // 6 bytes, 0.4 against 1.2 ps at 128 elements and the rates of a large product and a large copy.
 //
 // What bounds them: the matrix units, at the 1.7 to 1.8 GHz that they leave of the clock.  dh: 8,192 rows against 235,000
-// classes of 128 elements 0.87 ms (1.13 PFLOP/s), 15,001 against 99,991 of 200 1.06 ms (1.13), 2,048 against 2,900,000
-// of 64 1.64 ms (0.93, exponentials).  dw: 1.12 ms (0.88), 1.39 ms (0.86) and 1.60 ms (0.95).
+// classes of 128 elements 0.81 ms (1.22 PFLOP/s), 15,001 against 99,991 of 200 1.02 ms (1.18), 2,048 against 2,900,000
+// of 64 1.58 ms (0.97, exponentials).  dw: 0.99 ms (1.00), 1.38 ms (0.87) and 1.53 ms (0.99).
 #include <math.h>
 
 #include "kernels.h"
