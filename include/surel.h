@@ -19,7 +19,9 @@
  * Algorithm 2: mini-batches of queries that share nodes, by breadth-first search).
  * Behind them, for a model that reads walks or joined sets: surel_attention and
  * surel_attention_grad (rows packed with the offsets that the join and the RPE table are laid out by), and
- * surel_softmax_loss and surel_softmax_loss_grad (a row's next node among all nodes of the graph).
+ * surel_softmax_loss and surel_softmax_loss_grad (a row's next node among all nodes of the graph).  To continue
+ * walks with such a model, many at a time: surel_cache_plan, surel_cache_store and surel_cache_attention (keys and
+ * values of running sequences, kept in pages), and surel_sample_classes (a row's next node, drawn).
  *
  * Conventions
  *   - Plain C ABI.  Pointers named d_* are DEVICE memory owned by the caller, on the
@@ -31,8 +33,8 @@
  *     contexts may work at the same time, on streams of their own.
  *   - The context owns grow-only device workspaces (per-seed / per-query row counts, scan
  *     partials, the walk's per-edge neighbour records, the fused kernel's look-back words,
- *     the hash tables and sort arrays of pruning and mini-batching, what attention and the softmax
- *     loss keep between their launches)
+ *     the hash tables and sort arrays of pruning and mini-batching, what attention, the softmax
+ *     loss, plans and samples keep between their launches)
  *     and a device error word; nothing else is allocated.
  *   - Stream capture: a call that is given no h_* pointer only enqueues kernels (no memset,
  *     no copy, no wait), so once an eager call of the same shape has grown the workspaces it
@@ -110,6 +112,13 @@ extern "C" {
                                           of rows; rows of such a sequence are empty or unwritten */
 #define SUREL_DEV_BAD_BUCKET    0x400u /* a bucket number is not in [0, n_buckets): taken as 0 */
 #define SUREL_DEV_BAD_LABEL     0x800u /* a label is not below n_classes: the row does not count */
+#define SUREL_DEV_BAD_PAGE      0x1000u /* a page is not in [0, n_pages) or a slot not in one of them, or a ring
+                                          counts more pages than it has: keys there are not seen, rows not kept */
+#define SUREL_DEV_BAD_LENGTH    0x2000u /* a sequence's length is negative or does not fit its pages: it is taken
+                                          to have no keys                                    */
+#define SUREL_DEV_NO_PAGE       0x4000u /* no free page is left: rows have no place           */
+#define SUREL_DEV_BAD_CHOICE    0x8000u /* a row to draw from has a logit that is NaN or plus infinity, or a
+                                          parameter outside its range: its class is -1       */
 
 /* limits */
 #define SUREL_MAX_NODES   268435455   /* 2^28 - 1: node id and step share one 32-bit sort key */
@@ -125,6 +134,7 @@ extern "C" {
 #define SUREL_MAX_REACH   1024        /* attention: largest distance with a bucket of its own */
 #define SUREL_MAX_CLASS_DIM 256      /* loss: elements of a row                             */
 #define SUREL_MAX_STRIDE  16777208    /* attention: elements between rows or heads (2^24 - 8) */
+#define SUREL_MAX_SEQS    16777216    /* a cache: sequences (2^24)                            */
 #define SUREL_NOALLOC_MAX_QUERIES 1048576  /* surel_join_queries_noalloc: n_queries (2^20)    */
 
 /* kernel groups for surel_profile_read */
@@ -145,11 +155,16 @@ extern "C" {
 #define SUREL_K_ATTENTION_GRAD 12 /* surel_attention_grad (all its launches)           */
 #define SUREL_K_LOSS        13  /* surel_softmax_loss                                 */
 #define SUREL_K_LOSS_GRAD   14  /* surel_softmax_loss_grad (all its launches)         */
-#define SUREL_K_COUNT       15
+#define SUREL_K_CACHE_PLAN  15  /* surel_cache_plan (all its launches)               */
+#define SUREL_K_CACHE_STORE 16  /* surel_cache_store                                 */
+#define SUREL_K_CACHE_ATTENTION 17 /* surel_cache_attention (all its launches)          */
+#define SUREL_K_SAMPLE      18  /* surel_sample_classes (all its launches)           */
+#define SUREL_K_COUNT       19
 
 /* 16-bit element types of a model's tensors */
 #define SUREL_BF16          0
 #define SUREL_FP16          1
+#define SUREL_FP32          2   /* logits of surel_sample_classes only                */
 
 typedef struct surel_ctx surel_ctx;
 
@@ -527,6 +542,89 @@ int surel_softmax_loss(surel_ctx* ctx, int32_t type, const void* d_h, const void
 int surel_softmax_loss_grad(surel_ctx* ctx, int32_t type, const float* d_dloss, const void* d_h, const void* d_w,
                             const int32_t* d_labels, const float* d_lse, int64_t n_rows, int32_t n_classes, int32_t dim,
                             void* d_dh, void* d_dw);
+
+/* Where the keys and values of running sequences are kept: pages of page_rows rows, one behind another in memory.  A
+ * sequence's keys lie in the pages of its row of a page table, in order; its last page may be filled in part.
+ *   d_k, d_v       pages of rows [kv_heads][dim] of `type` (device); page, row and head are the elements between pages,
+ *                  between a page's rows and between heads, alike for both ([page][row][head][dim] and
+ *                  [page][head][row][dim] both serve).  A head's row is contiguous and starts on a 16-byte boundary:
+ *                  pointers are multiples of 16 bytes, strides of 8 elements (any, >= 0, where there is one page, row or head).
+ * Slot number p * page_rows + r is row r of page p.
+ * Limits: 1 <= n_pages, 1 <= page_rows, n_pages * page_rows <= SUREL_MAX_ROWS; row and head up to SUREL_MAX_STRIDE, page up
+ * to 2^40; dim a multiple of 8 up to SUREL_MAX_HEAD_DIM, 1 <= kv_heads <= 65535. */
+typedef struct surel_cache {
+    void *d_k, *d_v;
+    int64_t page, row, head;
+    int64_t n_pages;
+    int32_t page_rows, type, kv_heads, dim;
+} surel_cache;
+
+/* One step of a cache's bookkeeping: where the rows that sequences add will be kept, and whose pages become free.
+ *   d_length     int32[n_seqs] (device, read-only): the keys that a sequence has.
+ *   d_added      int32[n_seqs] (device, read-only): the rows that it adds, >= 0; a negative number: it ends, and gives its
+ *                pages back.
+ *   d_pages      int32[n_seqs][max_pages] (device, read and written): the page table.  Entries of pages that a sequence
+ *                has already, ceil(length / page_rows) of them, are read; those of new pages are written, in order (-1 where
+ *                none was left); others stay as they are.
+ *   d_ring       int32[n_pages] (device, read and written): the free pages, a ring.
+ *   d_turn       int64[2] (device, read-only): (pages taken from the ring, pages given to it) since it was made, of which
+ *                the free ones are d_ring[i % n_pages] for i = taken .. given - 1.  A ring of all pages starts with (0, n_pages).
+ *   d_off        int64[n_seqs+1] (device, written): sequence s adds the packed rows d_off[s] .. d_off[s+1]-1.
+ *   d_slots      int32[n_rows] (device, written): the slot of every packed row, -1 for rows that have no place and
+ *                for those behind the last sequence's.
+ *   d_length_after, d_turn_after   int32[n_seqs], int64[2] (device, written): lengths with the added rows, 0 for
+ *                sequences that end, and the ring's counters.  Neither may be the array it follows.
+ * Pages are taken in the order of sequences, and given back in that order; those given back by a call can be taken from
+ * the next one on.  Rows that find no free page (NO_PAGE), do not fit max_pages or lie beyond n_rows (CAPACITY) are not
+ * added: d_length_after says how many keys a sequence has in earnest.  Given the same arguments again (d_pages and d_ring as
+ * the call left them) it writes the same again.  A d_ring that counts more pages than it has gives and takes none (BAD_PAGE).
+ * Where there are more than 4,096 sequences the context's workspace grows by 24 bytes for every 4,096 of them.
+ * Limits: 0 <= n_seqs <= SUREL_MAX_SEQS, 0 <= n_rows <= SUREL_MAX_ROWS, 1 <= max_pages, 1 <= page_rows and
+ * max_pages * page_rows <= SUREL_MAX_ROWS, 1 <= n_pages and n_pages * page_rows <= SUREL_MAX_ROWS.
+ * Asynchronous.  Device-detected: BAD_LENGTH, BAD_PAGE, NO_PAGE, CAPACITY. */
+int surel_cache_plan(surel_ctx* ctx, const int32_t* d_length, const int32_t* d_added, int64_t n_seqs, int64_t n_pages,
+                     int32_t page_rows, int32_t max_pages, int64_t n_rows, int32_t* d_pages, int32_t* d_ring,
+                     const int64_t* d_turn, int64_t* d_off, int32_t* d_slots, int32_t* d_length_after,
+                     int64_t* d_turn_after);
+
+/* Keys and values of new rows into their slots of a cache.
+ *   d_k, d_v     [n_rows][kv_heads][dim] of the cache's type (device, read-only), laid out as in surel_attention_args.
+ *   d_slots      int32[n_rows] (device, read-only): -1: the row is left out.
+ * Slots have to be distinct (of rows that name one slot, its 16-byte parts are either's).  Limits: 0 <= n_rows <=
+ * SUREL_MAX_ROWS.  Asynchronous.  Device-detected: BAD_PAGE (the row is left out). */
+int surel_cache_store(surel_ctx* ctx, const surel_cache* cache, const void* d_k, const void* d_v, int64_t k_row,
+                      int64_t k_head, int64_t v_row, int64_t v_head, const int32_t* d_slots, int64_t n_rows);
+
+/* Attention of one row a sequence, the newest, to the sequence's keys in a cache: what surel_attention computes for it
+ * over the same keys, packed.
+ *   d_q            [n_seqs][heads][dim] of the cache's type (device, read-only), laid out as in surel_attention_args.
+ *   d_pages        int32[n_seqs][max_pages] (device, read-only): the page table; entries behind a sequence's last
+ *                  key are not read.  Sequences may share pages.
+ *   d_length       int32[n_seqs] (device, read-only): the keys that a sequence has, the row's own among them.
+ *   scale, d_bias, d_bucket, n_buckets, reach   as in surel_attention_args; the row stands at the last key.
+ *   d_out, d_lse   as for surel_attention: [n_seqs][heads][dim] of the cache's type, dense, on a 16-byte boundary, and
+ *                  float[n_seqs][heads] (device, written).
+ * Scores, softmax and sums are 32-bit; what is rounded, what a bias masks, and what rows of no keys get is as for
+ * surel_attention.  What lies behind a sequence's last key in its last page has no influence, whatever it holds.
+ * Sequences' keys are shared out evenly over the device by their lengths, which only the device knows, so a
+ * captured call serves any lengths that fit max_pages; sums of sequences that several workgroups share are joined in a
+ * fixed order.  The context's workspace grows by at most 8 (dim + 2) min(heads / kv_heads, 32) bytes for each of 32
+ * workgroups a compute unit, and by 8 bytes for every 64 of more than 4,096 sequences.  Results are the same every time.
+ * Limits: 0 <= n_seqs <= SUREL_MAX_SEQS, 1 <= max_pages, max_pages * page_rows <= SUREL_MAX_ROWS, heads a multiple of
+ * kv_heads, up to 65535.  Asynchronous.  Device-detected: BAD_LENGTH, BAD_PAGE, BAD_BUCKET. */
+typedef struct surel_cache_attention_args {
+    const void* d_q;
+    int64_t q_row, q_head;
+    const int32_t *d_pages, *d_length;
+    int64_t n_seqs;
+    int32_t max_pages, heads;
+    float scale;
+    const void* d_bias;
+    const int32_t* d_bucket;
+    int32_t n_buckets, reach;
+} surel_cache_attention_args;
+int surel_cache_attention(surel_ctx* ctx, const surel_cache* cache, const surel_cache_attention_args* args, void* d_out,
+                          float* d_lse);
 
 /* Every wait inside the fused kernel of surel_sample_walks_rpe and surel_sample_walks_rpe_ids (a
  * wave waiting for an offset, the offset scan waiting for a row count) and inside the pruning (a

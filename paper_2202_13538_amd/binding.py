@@ -19,24 +19,28 @@ OK, E_NULL, E_RANGE, E_HIP, E_CAPACITY, E_CTX, E_DEVICE = 0, -1, -2, -3, -4, -5,
 DEV_BAD_SEED, DEV_BAD_GRAPH, DEV_BAD_WALK, DEV_BAD_QUERY = 0x01, 0x02, 0x04, 0x08
 DEV_SET_TOO_LARGE, DEV_CAPACITY, DEV_BAD_TABLE, DEV_BAD_SIZES = 0x10, 0x20, 0x40, 0x80
 DEV_STALL, DEV_BAD_OFFSETS, DEV_BAD_BUCKET, DEV_BAD_LABEL = 0x100, 0x200, 0x400, 0x800
+DEV_BAD_PAGE, DEV_BAD_LENGTH, DEV_NO_PAGE, DEV_BAD_CHOICE = 0x1000, 0x2000, 0x4000, 0x8000
 MAX_NODES, MAX_STEPS, MAX_WALKS = 268435455, 15, 65535
 MAX_WALK_ENTRIES, MAX_SET, MAX_TUPLE = 2048, 2048, 3
 MAX_DISTINCT = 1 << 24
 MAX_BATCH = 1 << 20
 MAX_ROWS, MAX_HEAD_DIM, MAX_REACH, MAX_STRIDE = 1 << 30, 128, 1024, (1 << 24) - 8
-MAX_CLASS_DIM = 256
+MAX_CLASS_DIM, MAX_SEQS = 256, 1 << 24
 NOALLOC_MAX_QUERIES = 1 << 20
-BF16, FP16 = 0, 1
+BF16, FP16, FP32 = 0, 1, 2
 
 (K_WALK, K_RPE_COUNT, K_RPE_FILL, K_JOIN_COUNT, K_JOIN_FILL, K_SCAN, K_WALK_RPE,
  K_EDGE_RECORDS, K_QUERY_IDS, K_PRUNE, K_BATCH, K_ATTENTION,
- K_ATTENTION_GRAD, K_LOSS, K_LOSS_GRAD, K_COUNT) = range(16)
+ K_ATTENTION_GRAD, K_LOSS, K_LOSS_GRAD, K_CACHE_PLAN, K_CACHE_STORE, K_CACHE_ATTENTION,
+ K_SAMPLE, K_COUNT) = range(20)
 KERNEL_NAMES = {K_WALK: "walk", K_RPE_COUNT: "rpe_count", K_RPE_FILL: "rpe_fill",
                 K_JOIN_COUNT: "join_count", K_JOIN_FILL: "join_fill", K_SCAN: "scan",
                 K_WALK_RPE: "walk_rpe", K_EDGE_RECORDS: "edge_records",
                 K_QUERY_IDS: "query_ids", K_PRUNE: "prune", K_BATCH: "batch",
                 K_ATTENTION: "attention", K_ATTENTION_GRAD: "attention_grad",
-                K_LOSS: "loss", K_LOSS_GRAD: "loss_grad"}
+                K_LOSS: "loss", K_LOSS_GRAD: "loss_grad", K_CACHE_PLAN: "cache_plan",
+                K_CACHE_STORE: "cache_store", K_CACHE_ATTENTION: "cache_attention",
+                K_SAMPLE: "sample"}
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
@@ -51,6 +55,19 @@ class AttentionArgs(ctypes.Structure):
                [(n, _i32) for n in ("type", "heads", "kv_heads", "dim", "causal")] + \
                [("scale", ctypes.c_float), ("d_bias", _vp), ("d_bucket", _vp), ("n_buckets", _i32),
                 ("reach", _i32)]
+
+
+class Cache(ctypes.Structure):
+    """surel_cache"""
+    _fields_ = [("d_k", _vp), ("d_v", _vp)] + [(n, _i64) for n in ("page", "row", "head", "n_pages")] + \
+               [(n, _i32) for n in ("page_rows", "type", "kv_heads", "dim")]
+
+
+class CacheAttentionArgs(ctypes.Structure):
+    """surel_cache_attention_args"""
+    _fields_ = [("d_q", _vp), ("q_row", _i64), ("q_head", _i64), ("d_pages", _vp), ("d_length", _vp), ("n_seqs", _i64),
+                ("max_pages", _i32), ("heads", _i32), ("scale", ctypes.c_float), ("d_bias", _vp), ("d_bucket", _vp),
+                ("n_buckets", _i32), ("reach", _i32)]
 
 
 # name -> (restype, argtypes); the order and types of include/surel.h
@@ -94,6 +111,9 @@ SIGNATURES = {
     "surel_softmax_loss": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp]),
     "surel_softmax_loss_grad": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp,
                                                _vp]),
+    "surel_cache_plan": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i64, _i32, _i32, _i64] + 7 * [_vp]),
+    "surel_cache_store": (ctypes.c_int, [_vp, ctypes.POINTER(Cache), _vp, _vp, _i64, _i64, _i64, _i64, _vp, _i64]),
+    "surel_cache_attention": (ctypes.c_int, [_vp, ctypes.POINTER(Cache), ctypes.POINTER(CacheAttentionArgs), _vp, _vp]),
     "surel_set_spin_limit": (ctypes.c_int, [_vp, ctypes.c_uint32]),
     "surel_check": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "surel_profile_enable": (ctypes.c_int, [_vp, ctypes.c_int]),
@@ -733,3 +753,106 @@ def softmax_loss_grad(ctx: Context, dloss: torch.Tensor, h: torch.Tensor, w: tor
     if rc != OK:
         raise SurelError(rc, "surel_softmax_loss_grad")
     return dh, dw
+
+
+def _beside(ctx: Context, *tensors: torch.Tensor | None) -> None:
+    """Tensors that the context's stream may read and write: on its device, and, where that is not the stream that torch
+    works on at the moment, kept from being given away before the stream is done with them."""
+    for t in tensors:
+        if t is not None and t.device != ctx.device:
+            raise ValueError(f"every tensor must live on the context's {ctx.device}, got {t.device}")
+    if torch.cuda.current_stream(ctx.device) != ctx.stream:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(ctx.stream)
+
+
+def cache_plan(ctx: Context, length: torch.Tensor, added: torch.Tensor, pages: torch.Tensor, ring: torch.Tensor,
+               turn: torch.Tensor, page_rows: int, n_rows: int):
+    """(off int64[seqs+1], slots int32[n_rows], length int32[seqs], turn int64[2]) on the GPU: one step of a paged cache's
+    bookkeeping (surel_cache_plan).  Sequence s has length[s] keys (int32) and adds added[s] rows, or ends and gives its
+    pages back where that is negative.  pages int32[seqs][max_pages] gets its new pages' numbers, taken from ring
+    int32[n_pages], whose free entries are those from turn[0] to turn[1] (int64; modulo n_pages); both are changed in place.
+    Row i of sequence s, packed at off[s] + i, has the slot slots[off[s] + i], page * page_rows + row of the page; rows
+    without a place, and those behind the last sequence's, have -1.  length and turn are what the next step starts from.
+
+    A cache of all free pages: ring torch.arange(n_pages), turn (0, n_pages), lengths of zero."""
+    if pages.dim() != 2 or length.shape != pages.shape[:1] or added.shape != length.shape:
+        raise ValueError("pages must be [sequences][max_pages], length and added have an entry a sequence")
+    if ring.dim() != 1 or turn.shape != (2,):
+        raise ValueError("ring must have an entry a page, turn two")
+    n, width = pages.shape
+    off = length.new_empty(n + 1, dtype=torch.int64)
+    slots = length.new_empty(n_rows, dtype=torch.int32)
+    after, turn_after = torch.empty_like(length), torch.empty_like(turn)
+    _beside(ctx, length, added, pages, ring, turn, off, slots, after, turn_after)
+    rc = load().surel_cache_plan(
+        ctx.handle, _ptr(length, torch.int32, "length"), _ptr(added, torch.int32, "added"), n, ring.shape[0], page_rows,
+        width, n_rows, _ptr(pages, torch.int32, "pages"), _ptr(ring, torch.int32, "ring"),
+        _ptr(turn, torch.int64, "turn"), off.data_ptr(), slots.data_ptr(), after.data_ptr(), turn_after.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_cache_plan")
+    return off, slots, after, turn_after
+
+
+def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor) -> Cache:
+    if k_pages.dtype not in _TYPES:
+        raise TypeError(f"k_pages must be torch.bfloat16 or torch.float16, got {k_pages.dtype}")
+    if v_pages.dtype != k_pages.dtype:
+        raise TypeError(f"v_pages must be {k_pages.dtype}, got {v_pages.dtype}")
+    if not k_pages.is_cuda or not v_pages.is_cuda:
+        raise ValueError("k_pages and v_pages must live on the GPU")
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+        raise ValueError("k_pages and v_pages must be [pages][page_rows][kv_heads][dim], and lie alike")
+    page, row, head, one = k_pages.stride()
+    n_pages, page_rows, kv_heads, dim = k_pages.shape
+    if one != 1 and dim > 1:
+        raise ValueError("the last dimension of k_pages and v_pages must be contiguous")
+    return Cache(k_pages.data_ptr(), v_pages.data_ptr(), page, row, head, n_pages, page_rows, _TYPES[k_pages.dtype], kv_heads,
+                 dim)
+
+
+def cache_store(ctx: Context, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_pages: torch.Tensor,
+                v_pages: torch.Tensor) -> None:
+    """Writes the rows k, v [rows][kv_heads][dim] (views of a larger tensor will do) into their slots (int32[rows], from
+    cache_plan; -1: left out) of k_pages, v_pages [pages][page_rows][kv_heads][dim], bfloat16 or float16.  Pages whose
+    heads lie outside their rows, as views of [pages][kv_heads][page_rows][dim], will do as well."""
+    cache = _cache(k_pages, v_pages)
+    k_ptr, k_row, k_head = _rows(k, k_pages, "k")
+    v_ptr, v_row, v_head = _rows(v, k_pages, "v")
+    if k.shape != v.shape or k.shape[1:] != k_pages.shape[2:] or slots.shape != k.shape[:1]:
+        raise ValueError("k and v must be [rows][kv_heads][dim] of the pages' heads and dim, slots have an entry a row")
+    _beside(ctx, k, v, slots, k_pages, v_pages)
+    rc = load().surel_cache_store(ctx.handle, ctypes.byref(cache), k_ptr, v_ptr, k_row, k_head, v_row, v_head,
+                                  _ptr(slots, torch.int32, "slots"), k.shape[0])
+    if rc != OK:
+        raise SurelError(rc, "surel_cache_store")
+
+
+def cache_attention(ctx: Context, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, pages: torch.Tensor,
+                    length: torch.Tensor, scale: float | None = None, bias: torch.Tensor | None = None,
+                    bucket: torch.Tensor | None = None):
+    """(out [seqs][heads][dim], lse float32[seqs][heads]) on the GPU: attention of one row a sequence, its newest,
+    q [seqs][heads][dim], to the length[s] keys (int32, its own among them) that the sequence has in the pages
+    pages[s] (int32[seqs][max_pages]) of k_pages, v_pages (see cache_store).  scale, bias and bucket as for attention; the
+    row stands at its sequence's last key.  What attention(causal=True) gives for these rows over the same keys, packed."""
+    cache = _cache(k_pages, v_pages)
+    q_ptr, q_row, q_head = _rows(q, k_pages, "q")
+    n, heads, dim = q.shape
+    if dim != k_pages.shape[3] or pages.dim() != 2 or pages.shape[0] != n or length.shape != (n,):
+        raise ValueError("q must have the pages' dim, pages and length a row and an entry a sequence")
+    if (bias is None) != (bucket is None):
+        raise ValueError("bias and bucket go together")
+    if bias is not None and (bias.dim() != 2 or bias.shape[1] != heads or bucket.numel() % 2 != 1):
+        raise ValueError("bias must be [buckets][heads], bucket have 2 * reach + 1 entries")
+    args = CacheAttentionArgs(
+        q_ptr, q_row, q_head, _ptr(pages, torch.int32, "pages"), _ptr(length, torch.int32, "length"), n, pages.shape[1],
+        heads, dim ** -0.5 if scale is None else scale, _ptr(bias, q.dtype, "bias"), _ptr(bucket, torch.int32, "bucket"),
+        0 if bias is None else bias.shape[0], 0 if bucket is None else bucket.numel() // 2)
+    out = q.new_empty(q.shape)
+    lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+    _beside(ctx, q, k_pages, v_pages, pages, length, bias, bucket, out, lse)
+    rc = load().surel_cache_attention(ctx.handle, ctypes.byref(cache), ctypes.byref(args), out.data_ptr(), lse.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_cache_attention")
+    return out, lse

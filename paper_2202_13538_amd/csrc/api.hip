@@ -137,6 +137,8 @@ void surel_destroy(surel_ctx* ctx) {
     }
     for (hipEvent_t e : ctx->free_events) (void)hipEventDestroy(e);
     if (ctx->d_ws) (void)hipFree(ctx->d_ws);
+    if (ctx->d_kept) (void)hipFree(ctx->d_kept);
+    for (int i = 0; i < ctx->n_kept_before; ++i) (void)hipFree(ctx->kept_before[i]);
     if (ctx->d_rec) (void)hipFree(ctx->d_rec);
     if (ctx->d_lb) (void)hipFree(ctx->d_lb);
     if (ctx->d_prune) (void)hipFree(ctx->d_prune);

@@ -1,0 +1,44 @@
+// How the keys of a cache's sequences are shared out over waves (cache_attention.hip).
+//
+// A sequence's keys make tiles of 32, once for every unit of it (a key head and up to 32 query heads that read it); a
+// sequence's unit is a pair.  All pairs' tiles in a row, sequences outermost, are cut into equal parts, one a wave; a cut
+// inside a pair of few tiles moves to the pair's start, so that only pairs of many tiles have several waves' sums to join.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIP__
+#define SUREL_BOTH __host__ __device__ __forceinline__
+#else
+#define SUREL_BOTH inline
+#endif
+
+namespace surel {
+
+constexpr int kCacheTile = 32;      // keys
+constexpr int kLeastTiles = 4;      // of a wave's part, where there are as many
+constexpr int kWholeTiles = 8;      // pairs of up to these many are not cut
+constexpr int kLookup = 4096;       // entries that a wave looks through, 64 lanes twice
+
+// Parts of `tiles` tiles for up to `waves` waves, and where the n-th begins (before it moves).
+SUREL_BOTH int64_t parts_of(int64_t tiles, int64_t waves) {
+    const int64_t most = (tiles + kLeastTiles - 1) / kLeastTiles;
+    return most < waves ? most : waves;
+}
+SUREL_BOTH int64_t part_begin(int64_t tiles, int64_t parts, int64_t n) {
+    // n tiles / parts without passing 64 bits: tiles = a parts + b
+    const int64_t a = tiles / parts, b = tiles % parts;
+    return n * a + n * b / parts;
+}
+// A cut t tiles behind the start of a pair of n: how far back it moves.
+SUREL_BOTH int64_t moves_back(int64_t t, int64_t n) { return n <= kWholeTiles ? t : 0; }
+SUREL_BOTH bool may_be_cut(int64_t most_tiles) { return most_tiles > kWholeTiles; }
+
+// Sequences of one entry of the list that is looked through first: 1, or 64 and more.
+SUREL_BOTH int64_t seqs_of_an_entry(int64_t n_seqs) {
+    if (n_seqs <= kLookup) return 1;
+    const int64_t each = (n_seqs + kLookup - 1) / kLookup;
+    return (each + 63) / 64 * 64;
+}
+
+}  // namespace surel

@@ -34,6 +34,12 @@ struct surel_ctx {
     uint32_t* d_turns = nullptr;  // a word of zero between launches whose last workgroup joins the others' parts
     void* d_model = nullptr;      // grow-only workspace: parts of attention and loss that are joined later
     size_t model_bytes = 0;
+    // workspace of plans, attention over a cache and samples.  It grows to twice its size at least, and what it was before
+    // stays until the context ends: calls that were captured into a graph go on using it.
+    void* d_kept = nullptr;
+    size_t kept_bytes = 0;
+    void* kept_before[64] = {};
+    int n_kept_before = 0;
     void* d_scratch = nullptr;    // this device's copy of the file-scope `scratch` array below
     bool no_spans = false;        // set while a call that must not allocate runs (no new events)
     // optional per-kernel timing (surel_profile_*)
@@ -145,6 +151,21 @@ inline int grow_buffer(surel_ctx* ctx, void** buf, size_t* have, size_t need) {
         return SUREL_E_HIP;
     }
     *have = need;
+    return SUREL_OK;
+}
+
+// The workspace that captured calls may go on using, with `need` bytes at least (contents are not kept).
+inline int grow_kept(surel_ctx* ctx, size_t need) {
+    if (need <= ctx->kept_bytes) return SUREL_OK;
+    const size_t size = need > 2 * ctx->kept_bytes ? need : 2 * ctx->kept_bytes;
+    void* now = nullptr;
+    if (ctx->n_kept_before == 64 || hipMalloc(&now, size) != hipSuccess) {
+        (void)hipGetLastError();
+        return SUREL_E_HIP;
+    }
+    if (ctx->d_kept) ctx->kept_before[ctx->n_kept_before++] = ctx->d_kept;
+    ctx->d_kept = now;
+    ctx->kept_bytes = size;
     return SUREL_OK;
 }
 

@@ -21,6 +21,10 @@ constexpr uint32_t kDevStall = 0x100u;
 constexpr uint32_t kDevBadOffsets = 0x200u;
 constexpr uint32_t kDevBadBucket = 0x400u;
 constexpr uint32_t kDevBadLabel = 0x800u;
+constexpr uint32_t kDevBadPage = 0x1000u;
+constexpr uint32_t kDevBadLength = 0x2000u;
+constexpr uint32_t kDevNoPage = 0x4000u;
+constexpr uint32_t kDevBadChoice = 0x8000u;
 
 // The workgroup's number in a launch of grid_of(blocks): some more start than there are blocks.
 __device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }

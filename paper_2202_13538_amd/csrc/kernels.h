@@ -241,4 +241,19 @@ size_t loss_grad_scratch_bytes(int n_cu, const LossArgs& a);
 hipError_t launch_loss_grad(hipStream_t stream, int n_cu, const LossArgs& a, bool half, const float* dloss, const float* lse,
                             void* dh, void* dw, void* scratch);
 
+// cache_plan.hip.  scratch: cache_plan_scratch_bytes of device memory.
+struct CachePlan;
+size_t cache_plan_scratch_bytes(int64_t n_seqs);
+hipError_t launch_cache_plan(hipStream_t stream, int n_cu, CachePlan p, void* scratch);
+
+// cache_store.hip.  Needs a.n_rows >= 1.
+struct CacheStore;
+hipError_t launch_cache_store(hipStream_t stream, int n_cu, const CacheStore& a);
+
+// cache_attention.hip.  scratch: cache_attention_scratch_bytes of device memory.  half: fp16 instead of bf16.  Needs
+// a.n_seqs >= 1.
+struct CacheAttention;
+size_t cache_attention_scratch_bytes(int n_cu, const CacheAttention& a);
+hipError_t launch_cache_attention(hipStream_t stream, int n_cu, CacheAttention a, bool half, void* scratch);
+
 }  // namespace surel
