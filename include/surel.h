@@ -626,6 +626,33 @@ typedef struct surel_cache_attention_args {
 int surel_cache_attention(surel_ctx* ctx, const surel_cache* cache, const surel_cache_attention_args* args, void* d_out,
                           float* d_lse);
 
+/* A class (the next node) for every row of logits, drawn with a given uniform number.  With T the row's temperature, a class
+ * c has the weight w_c = exp((z_c - max z) / T).  Classes in the order of their logits, the largest first and equal ones by
+ * their numbers: kept are the first top_k, of these the fewest, from the first on, whose weights add up to top_p times what
+ * all of these add up to, and of those the ones with w_c >= min_p; the first always.  Drawn is, in the order of numbers, the
+ * first kept class up to which the kept classes' weights add up to more than u times what all of them add up to.
+ *   type           SUREL_BF16, SUREL_FP16 or SUREL_FP32.
+ *   d_logits       [n_rows][n_classes] of `type` (device, read-only); `row` is the elements between rows (any, >= 0, where
+ *                  there is one).  Minus infinity: the class cannot be drawn.
+ *   d_u            float[n_rows] (device, read-only), 0 <= u < 1.
+ *   d_temperature  float[n_rows] or NULL for 1 (device, read-only): finite, >= 0; 0 takes the first of the largest.
+ *   d_top_k        int32[n_rows] or NULL (device, read-only); < 1: not in use.
+ *   d_top_p        float[n_rows] or NULL (device, read-only), >= 0; 1 and more: not in use.
+ *   d_min_p        float[n_rows] or NULL (device, read-only), 0 <= min_p <= 1; 0: not in use.
+ *   d_class        int32[n_rows] (device, written): -1 for rows whose logits are minus infinity throughout, or have NaN or plus
+ *                  infinity among them, and for rows with a parameter that is none of these (BAD_CHOICE, but for the
+ *                  former).
+ *   d_logp         float[n_rows] (device, written): the logarithm of the probability that the class was drawn
+ *                  with, log(w_c / the kept classes' sum); minus infinity for -1.
+ * Weights and sums are 64-bit (borders that sums are compared with are between other classes in 32 bits); weights
+ * below e^-64 of the largest count as zero.  Results are the same every time.  The context's workspace grows by up to 128 KB a
+ * row where rows are too few to fill the device, and by 12 bytes for every 512 16-byte parts of a row.
+ * Limits: 0 <= n_rows <= SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, row up to 2^40.  Asynchronous.
+ * Device-detected: BAD_CHOICE. */
+int surel_sample_classes(surel_ctx* ctx, int32_t type, const void* d_logits, int64_t row, int64_t n_rows,
+                         int32_t n_classes, const float* d_u, const float* d_temperature, const int32_t* d_top_k,
+                         const float* d_top_p, const float* d_min_p, int32_t* d_class, float* d_logp);
+
 /* Every wait inside the fused kernel of surel_sample_walks_rpe and surel_sample_walks_rpe_ids (a
  * wave waiting for an offset, the offset scan waiting for a row count) and inside the pruning (a
  * lane waiting for another to finish writing a hash slot) gives up after `spins` polls, raises

@@ -114,6 +114,7 @@ SIGNATURES = {
     "surel_cache_plan": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i64, _i32, _i32, _i64] + 7 * [_vp]),
     "surel_cache_store": (ctypes.c_int, [_vp, ctypes.POINTER(Cache), _vp, _vp, _i64, _i64, _i64, _i64, _vp, _i64]),
     "surel_cache_attention": (ctypes.c_int, [_vp, ctypes.POINTER(Cache), ctypes.POINTER(CacheAttentionArgs), _vp, _vp]),
+    "surel_sample_classes": (ctypes.c_int, [_vp, _i32, _vp, _i64, _i64, _i32] + 7 * [_vp]),
     "surel_set_spin_limit": (ctypes.c_int, [_vp, ctypes.c_uint32]),
     "surel_check": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "surel_profile_enable": (ctypes.c_int, [_vp, ctypes.c_int]),
@@ -856,3 +857,32 @@ def cache_attention(ctx: Context, q: torch.Tensor, k_pages: torch.Tensor, v_page
     if rc != OK:
         raise SurelError(rc, "surel_cache_attention")
     return out, lse
+
+
+def sample_classes(ctx: Context, logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor | None = None,
+                   top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None):
+    """(classes int32[rows], logp float32[rows]) on the GPU: a class for every row of logits [rows][classes] (bfloat16,
+    float16 or float32; rows may lie apart), drawn with the uniform numbers u float32[rows] in [0, 1), and the logarithm of the
+    probability that it had.  temperature float32[rows] (0: the largest logit's first class), top_k int32[rows] (below 1: not
+    in use), top_p (1: not in use) and min_p float32[rows] (0: not in use); see surel_sample_classes for what they keep.
+    A row without a class to draw has -1."""
+    kinds = {**_TYPES, torch.float32: FP32}
+    if logits.dtype not in kinds:
+        raise TypeError(f"logits must be torch.bfloat16, torch.float16 or torch.float32, got {logits.dtype}")
+    if not logits.is_cuda:
+        raise ValueError("logits must live on the GPU")
+    if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be [rows][classes], the classes of a row contiguous")
+    n, classes = logits.shape
+    if any(t is not None and t.shape != (n,) for t in (u, temperature, top_k, top_p, min_p)):
+        raise ValueError("u, temperature, top_k, top_p and min_p must have one entry a row")
+    chosen = u.new_empty(n, dtype=torch.int32)
+    logp = u.new_empty(n)
+    _beside(ctx, logits, u, temperature, top_k, top_p, min_p, chosen, logp)
+    rc = load().surel_sample_classes(
+        ctx.handle, kinds[logits.dtype], logits.data_ptr(), logits.stride(0), n, classes, _ptr(u, torch.float32, "u"),
+        _ptr(temperature, torch.float32, "temperature"), _ptr(top_k, torch.int32, "top_k"),
+        _ptr(top_p, torch.float32, "top_p"), _ptr(min_p, torch.float32, "min_p"), chosen.data_ptr(), logp.data_ptr())
+    if rc != OK:
+        raise SurelError(rc, "surel_sample_classes")
+    return chosen, logp

@@ -9,6 +9,7 @@
 #include "cache.h"
 #include "context.h"
 #include "kernels.h"
+#include "sample.h"
 
 namespace {
 
@@ -137,6 +138,31 @@ int surel_cache_attention(surel_ctx* ctx, const surel_cache* cache, const surel_
     KernelSpan span(ctx, SUREL_K_CACHE_ATTENTION);
     return surel::launch_cache_attention(ctx->stream, ctx->n_cu, a, cache->type == SUREL_FP16, ctx->d_kept) == hipSuccess
                ? SUREL_OK : SUREL_E_HIP;
+}
+
+int surel_sample_classes(surel_ctx* ctx, int32_t type, const void* d_logits, int64_t row, int64_t n_rows,
+                         int32_t n_classes, const float* d_u, const float* d_temperature, const int32_t* d_top_k,
+                         const float* d_top_p, const float* d_min_p, int32_t* d_class, float* d_logp) {
+    if (type != SUREL_BF16 && type != SUREL_FP16 && type != SUREL_FP32) return SUREL_E_RANGE;
+    if (n_rows < 0 || n_rows > SUREL_MAX_ROWS || n_classes < 1 || n_classes > SUREL_MAX_NODES) return SUREL_E_RANGE;
+    if (row < 0 || (n_rows > 1 && row > kMostPage)) return SUREL_E_RANGE;
+    if (n_rows > 0 && (!d_logits || !d_u || !d_class || !d_logp)) return SUREL_E_NULL;
+    const int64_t size = type == SUREL_FP32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(d_logits) % (uintptr_t)size != 0) return SUREL_E_RANGE;
+    if (!ctx) return SUREL_E_CTX;
+    if (n_rows == 0) return SUREL_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SUREL_E_HIP;
+    surel::SampleArgs a;
+    a.logits = static_cast<const char*>(d_logits);
+    a.row = n_rows > 1 ? row * size : 0;
+    a.n_rows = (int32_t)n_rows, a.n_classes = n_classes;
+    a.u = d_u, a.temperature = d_temperature, a.top_k = d_top_k, a.top_p = d_top_p, a.min_p = d_min_p;
+    a.chosen = d_class, a.logp = d_logp;
+    a.err = ctx->d_err;
+    if (int rc = grow_kept(ctx, surel::sample_scratch_bytes(ctx->n_cu, a, type))) return rc;
+    KernelSpan span(ctx, SUREL_K_SAMPLE);
+    return surel::launch_sample(ctx->stream, ctx->n_cu, a, type, ctx->d_kept) == hipSuccess ? SUREL_OK : SUREL_E_HIP;
 }
 
 }  // extern "C"

@@ -256,4 +256,10 @@ struct CacheAttention;
 size_t cache_attention_scratch_bytes(int n_cu, const CacheAttention& a);
 hipError_t launch_cache_attention(hipStream_t stream, int n_cu, CacheAttention a, bool half, void* scratch);
 
+// sample.hip.  scratch: sample_scratch_bytes of device memory.  type: SUREL_BF16, SUREL_FP16 or SUREL_FP32.  Needs a.n_rows,
+// a.n_classes >= 1.
+struct SampleArgs;
+size_t sample_scratch_bytes(int n_cu, const SampleArgs& a, int type);
+hipError_t launch_sample(hipStream_t stream, int n_cu, const SampleArgs& a, int type, void* scratch);
+
 }  // namespace surel
