@@ -1,0 +1,150 @@
+// What the kernels of attention over a cache share: which wave goes over which keys.
+#pragma once
+
+#include "attention.h"
+#include "cache.h"
+#include "cache_share.h"
+
+namespace surel {
+
+// What the waves share, beside the call's arguments.
+struct Share {
+    const int64_t* entries = nullptr;    // tiles of every `each` sequences, or null: each is 1, a sequence's length says it
+    int32_t n_entries = 0, each = 1;
+    int32_t waves = 0;
+    int32_t head_tiles = 1, columns = 1; // units of a key head, query heads of a unit (the last has fewer)
+    bool cuts = false;                   // some pair may be cut
+    int64_t* cut = nullptr;              // [waves]: the pair that a wave's part begins inside of, or -1
+    float *part_o = nullptr, *part_ml = nullptr;   // [waves][2][columns][dim], [waves][2][columns][2]: maximum (base 2), sum
+};
+
+__device__ __forceinline__ int64_t lane_of(int64_t x, int lane) { return __shfl(x, lane); }
+__device__ __forceinline__ int64_t sum_till(int64_t x) {   // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(x, d);
+        if (lane_id() >= d) x += y;
+    }
+    return x;
+}
+
+__device__ __forceinline__ int length_of(const CacheAttention& a, int s) {
+    const int n = a.length[s];
+    return n < 0 || n > a.width * (int64_t)a.page_rows.d ? 0 : n;
+}
+__device__ __forceinline__ int tiles_of(int length) { return (length + kCacheTile - 1) / kCacheTile; }
+
+// A list of n <= kLookup counts: its sums by 64 lanes, then the entry that `target` falls into and what is left of it there.
+struct Lookup {
+    int64_t till, mine;   // lanes' sums
+    int per;
+    template <class Count>
+    __device__ __forceinline__ int64_t sums(int n, Count count) {
+        per = (n + 63) / 64;
+        const int from = lane_id() * per;
+        mine = 0;
+#pragma unroll 8
+        for (int i = 0; i < per; ++i) mine += from + i < n ? count(min(from + i, n - 1)) : 0;
+        till = sum_till(mine);
+        return lane_of(till, 63);
+    }
+    template <class Count>   // target below the list's sum
+    __device__ __forceinline__ int find(int n, int64_t target, int64_t* left, Count count) const {
+        const int l = min((int)__popcll(__ballot(till <= target)), 63);
+        const int64_t rest = target - lane_of(till - mine, l);
+        const int at = l * per + lane_id();
+        const int64_t x = lane_id() < per && at < n ? count(min(at, n - 1)) : 0;
+        const int64_t up_to = sum_till(x);
+        const int e = min((int)__popcll(__ballot(lane_id() < per && up_to <= rest)), per - 1);
+        *left = rest - lane_of(up_to - x, e);
+        return l * per + e;
+    }
+};
+
+// A tile of a pair: sequence, unit, tile.
+struct Place {
+    int seq, unit, tile, tiles, length;
+};
+
+// Writes zeros for sequences of no keys; every wave takes some.
+__device__ __forceinline__ void write_empty(const CacheAttention& a, const Share& o, int wave) {
+    const int lane = lane_id();
+    for (int64_t s = wave; s < a.n_seqs; s += o.waves) {
+        const int n = uniform(a.length[s]);
+        if (n > 0 && n <= a.width * (int64_t)a.page_rows.d) continue;
+        if (n != 0 && lane == 0) atomicOr(a.err, kDevBadLength);
+        uint32_t* const out = static_cast<uint32_t*>(a.out) + s * a.heads * (a.dim / 2);
+        for (int i = lane; i < a.heads * (a.dim / 2); i += 64) out[i] = 0;
+        for (int i = lane; i < a.heads; i += 64) a.lse[s * a.heads + i] = -INFINITY;
+    }
+}
+
+// A wave's part: where it begins, and how many tiles it has.  Notes where it begins inside a pair.
+struct Course {
+    Place at;
+    int64_t tiles;   // 0: no part
+};
+__device__ __forceinline__ Course course_of(const CacheAttention& a, const Share& o, int wave) {
+    const int units = a.kv_heads * o.head_tiles;
+    auto tiles_of_seq = [&](int s) { return (int64_t)tiles_of(length_of(a, s)) * units; };
+    auto tiles_of_entry = [&](int e) { return o.entries == nullptr ? tiles_of_seq(e) : o.entries[e] * units; };
+    Course c;
+    c.tiles = 0;
+    Lookup list;
+    const int64_t tiles = list.sums(o.n_entries, tiles_of_entry);
+    const int64_t parts = parts_of(tiles, o.waves);
+    if (wave < parts) {
+        auto place_of = [&](int64_t target) {   // the place of a tile by its number
+            int64_t left;
+            int s = list.find(o.n_entries, target, &left, tiles_of_entry);
+            if (o.entries != nullptr) {
+                const int first = s * o.each, n = min(o.each, a.n_seqs - first);
+                Lookup inner;
+                auto count = [&](int i) { return tiles_of_seq(first + i); };
+                (void)inner.sums(n, count);
+                s = first + inner.find(n, left, &left, count);
+            }
+            Place p;
+            p.seq = uniform(s);
+            p.length = uniform(length_of(a, p.seq));
+            p.tiles = tiles_of(p.length);
+            p.unit = uniform((int)(left / p.tiles));
+            p.tile = uniform((int)(left - (int64_t)p.unit * p.tiles));
+            return p;
+        };
+        int64_t begin = part_begin(tiles, parts, wave), end = part_begin(tiles, parts, wave + 1);
+        c.at = place_of(begin);
+        const int64_t back = moves_back(c.at.tile, c.at.tiles);
+        begin -= back, c.at.tile -= (int)back;
+        if (wave + 1 < parts) {
+            const Place behind = place_of(end);
+            end -= moves_back(behind.tile, behind.tiles);
+        }
+        c.tiles = end - begin;
+    }
+    if (o.cuts && lane_id() == 0) o.cut[wave] = c.tiles > 0 && c.at.tile > 0 ? (int64_t)c.at.seq * units + c.at.unit : -1;
+    return c;
+}
+
+// The place behind one, in the same part.
+__device__ __forceinline__ Place following(const CacheAttention& a, int units, const Place& p) {
+    Place n = p;
+    if (++n.tile < p.tiles) return n;
+    n.tile = 0;
+    if (++n.unit < units) return n;
+    n.unit = 0;
+    do {
+        if (++n.seq >= a.n_seqs) break;
+        n.length = uniform(length_of(a, n.seq));
+    } while (n.length == 0);
+    n.tiles = tiles_of(n.length);
+    return n;
+}
+
+// cache_lanes.hip: rows that few query heads share a key head with, by the vector units.
+bool lanes_serve(int group, int dim);
+int lanes_waves(int group, int dim);   // of a compute unit
+template <class T>
+hipError_t launch_lanes(hipStream_t stream, const CacheAttention& a, const Share& o);
+
+}  // namespace surel

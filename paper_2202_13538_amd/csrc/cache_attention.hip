@@ -1,11 +1,15 @@
 // Attention of one row a sequence to its keys in a paged cache (surel_cache_attention).
-#include "attention.h"
-#include "cache.h"
-#include "cache_share.h"
+#include "cache_attention.h"
 #include "kernels.h"
 
 namespace surel {
 namespace {
+
+constexpr int kJoinThreads = 256;
+constexpr int kMostDim = 128;
+
+constexpr int kThreads = 256;
+constexpr int kMostTable = 4096;   // biases of all heads by distance that are kept in LDS
 
 // fp16: weights are relative to 2^-7 of the largest, so that those down to 2^-21 of it keep all their bits, and stay below 2^15;
 // bf16 has the range of 32-bit floats.  What a lane's weights of a tile may add up to before a larger maximum is looked for:
@@ -14,317 +18,296 @@ constexpr float kBelow = T::kNarrow ? 7.f : 0.f;
 template <class T>
 constexpr float kMost = T::kNarrow ? 32768.f : 1024.f;
 
-constexpr int kJoinThreads = 256;
-constexpr int kMostDim = 128;
-
-// What the waves share, beside the call's arguments.
-struct Share {
-    const int64_t* entries = nullptr;    // tiles of every `each` sequences, or null: each is 1, a sequence's length says it
-    int32_t n_entries = 0, each = 1;
-    int32_t waves = 0;
-    int32_t head_tiles = 1, columns = 1; // units of a key head, query heads of a unit (the last has fewer)
-    bool cuts = false;                   // some pair may be cut
-    int64_t* cut = nullptr;              // [waves]: the pair that a wave's part begins inside of, or -1
-    float *part_o = nullptr, *part_ml = nullptr;   // [waves][2][columns][dim], [waves][2][columns][2]: maximum (base 2), sum
-};
-
-__device__ __forceinline__ int64_t lane_of(int64_t x, int lane) { return __shfl(x, lane); }
-__device__ __forceinline__ int64_t sum_till(int64_t x) {   // of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane_id() >= d) x += y;
-    }
-    return x;
+// C[16 x 16] += A[16 x 32] B[32 x 16] of one wave: lane l holds the row (of A) or column (of B) l % 16 and the inner values
+// 8 (l / 16) .. + 7; of C it holds column l % 16 and rows 4 (l / 16) .. + 3.
+__device__ __forceinline__ f32x4 mma16(Bf16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16::x8, a), __builtin_bit_cast(Bf16::x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(Fp16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Fp16::x8, a), __builtin_bit_cast(Fp16::x8, b), c, 0, 0, 0);
+}
+// The values of the lanes 16, 32 and 48 further on, with op.
+template <class Op>
+__device__ __forceinline__ float over_quarters(float x, Op op) {
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const uint32_t w = __float_as_uint(x);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-__device__ __forceinline__ int length_of(const CacheAttention& a, int s) {
-    const int n = a.length[s];
-    return n < 0 || n > a.width * (int64_t)a.page_rows.d ? 0 : n;
+// Waves of a SIMD: what registers have room for, and a compute unit's 160 KB of LDS, with two buffers of a tile's values each.
+constexpr int waves_of_a_simd(int padded, int blocks) {
+    return blocks == 2 ? (padded > 64 ? 1 : 2) : padded > 64 ? 2 : padded > 32 ? 3 : 4;
 }
-__device__ __forceinline__ int tiles_of(int length) { return (length + kCacheTile - 1) / kCacheTile; }
 
-// A list of n <= kLookup counts: its sums by 64 lanes, then the entry that `target` falls into and what is left of it there.
-struct Lookup {
-    int64_t till, mine;   // lanes' sums
-    int per;
-    template <class Count>
-    __device__ __forceinline__ int64_t sums(int n, Count count) {
-        per = (n + 63) / 64;
-        const int from = lane_id() * per;
-        mine = 0;
-#pragma unroll 8
-        for (int i = 0; i < per; ++i) mine += from + i < n ? count(min(from + i, n - 1)) : 0;
-        till = sum_till(mine);
-        return lane_of(till, 63);
-    }
-    template <class Count>   // target below the list's sum
-    __device__ __forceinline__ int find(int n, int64_t target, int64_t* left, Count count) const {
-        const int l = min((int)__popcll(__ballot(till <= target)), 63);
-        const int64_t rest = target - lane_of(till - mine, l);
-        const int at = l * per + lane_id();
-        const int64_t x = lane_id() < per && at < n ? count(min(at, n - 1)) : 0;
-        const int64_t up_to = sum_till(x);
-        const int e = min((int)__popcll(__ballot(lane_id() < per && up_to <= rest)), per - 1);
-        *left = rest - lane_of(up_to - x, e);
-        return l * per + e;
-    }
-};
-
-// A tile of a pair: sequence, unit, tile.
-struct Place {
-    int seq, unit, tile, tiles, length;
-};
-
-template <class T, int DP>
-__global__ __launch_bounds__(64) void cache_attention_kernel(CacheAttention a, Share o) {
-    constexpr int NB = DP / 32, kRowBytes = Tile<DP>::kRowBytes, kTileBytes = kCacheTile * kRowBytes;
+// One wave: up to 16 BLOCKS query heads that share a key head, over its part of all keys (cache_share.h), 32 at a time.
+// Scores are K q^T, so that a head's lie in the four lanes of a column, its softmax runs inside lanes, and the weights are the
+// operand of out^T += V^T p^T as they come.  Keys go from memory to registers, as the first product's operand lies; values, which
+// the second needs transposed, through LDS, without passing through registers.
+template <class T, int DP, int BLOCKS>
+__global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_attention_kernel(CacheAttention a, Share o, int in_table) {
+    constexpr int NB = DP / 16, NK = DP / 32, kRowBytes = Tile<DP>::kRowBytes, kTileBytes = kCacheTile * kRowBytes;
     constexpr int kChunks = Tile<DP>::kChunks, kCopies = kCacheTile * kChunks / 64;
-    extern __shared__ __align__(256) char lds[];   // [buffer][keys, values]
-    const int lane = threadIdx.x, g = lane >> 5, col = lane & 31;
-    const int wave = (int)block_number();
+    extern __shared__ __align__(256) char lds[];   // [wave][buffer], then biases [heads][reach + 1] by distance
+    const int lane = threadIdx.x & 63, in_group = uniform((int)(threadIdx.x >> 6));
+    const int g = lane >> 4, col = lane & 15, of_tile = lane & 31;
+    const int wave = (int)block_number() * (kThreads / 64) + in_group;
+    float* const table = reinterpret_cast<float*>(lds + kThreads / 64 * 2 * kTileBytes);
+    const int far = a.reach, width = far + 1;
+    auto bias_at = [&](int head, int distance) {
+        int b = a.bucket[far - distance];
+        if (b < 0 || b >= a.n_buckets) {
+            atomicOr(a.err, kDevBadBucket);
+            b = 0;
+        }
+        const float x = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head];
+        return x <= -65504.f ? -INFINITY : x * kLog2e;
+    };
+    if (in_table) {
+        for (int i = threadIdx.x; i < a.heads * width; i += kThreads) table[i] = bias_at(i / width, i % width);
+        __syncthreads();
+    }
     if (wave >= o.waves) return;
     const int units = a.kv_heads * o.head_tiles, group = a.heads / a.kv_heads;
-
-    // sequences of no keys: zeros
-    for (int64_t s = wave; s < a.n_seqs; s += o.waves) {
-        const int n = uniform(a.length[s]);
-        if (n > 0 && n <= a.width * (int64_t)a.page_rows.d) continue;
-        if (n != 0 && lane == 0) atomicOr(a.err, kDevBadLength);
-        uint32_t* const out = static_cast<uint32_t*>(a.out) + s * a.heads * (a.dim / 2);
-        for (int i = lane; i < a.heads * (a.dim / 2); i += 64) out[i] = 0;
-        for (int i = lane; i < a.heads; i += 64) a.lse[s * a.heads + i] = -INFINITY;
-    }
-
-    // the wave's part
-    auto tiles_of_seq = [&](int s) { return (int64_t)tiles_of(length_of(a, s)) * units; };
-    auto tiles_of_entry = [&](int e) { return o.entries == nullptr ? tiles_of_seq(e) : o.entries[e] * units; };
-    Lookup list;
-    const int64_t tiles = list.sums(o.n_entries, tiles_of_entry);
-    const int64_t parts = parts_of(tiles, o.waves);
-    if (wave >= parts) {
-        if (o.cuts && lane == 0) o.cut[wave] = -1;
-        return;
-    }
-    auto place_of = [&](int64_t target) {   // the place of a tile by its number
-        int64_t left;
-        int s = list.find(o.n_entries, target, &left, tiles_of_entry);
-        if (o.entries != nullptr) {
-            const int first = s * o.each, n = min(o.each, a.n_seqs - first);
-            Lookup inner;
-            auto count = [&](int i) { return tiles_of_seq(first + i); };
-            (void)inner.sums(n, count);
-            s = first + inner.find(n, left, &left, count);
-        }
-        Place p;
-        p.seq = uniform(s);
-        p.length = uniform(length_of(a, p.seq));
-        p.tiles = tiles_of(p.length);
-        p.unit = uniform((int)(left / p.tiles));
-        p.tile = uniform((int)(left - (int64_t)p.unit * p.tiles));
-        return p;
-    };
-    int64_t begin = part_begin(tiles, parts, wave), end = part_begin(tiles, parts, wave + 1);
-    Place next = place_of(begin);
-    {
-        const int64_t back = moves_back(next.tile, next.tiles);
-        begin -= back, next.tile -= (int)back;
-        if (wave + 1 < parts) {
-            const Place behind = place_of(end);
-            end -= moves_back(behind.tile, behind.tiles);
-        }
-    }
-    if (o.cuts && lane == 0) o.cut[wave] = begin < end && next.tile > 0 ? (int64_t)next.seq * units + next.unit : -1;
-    if (begin >= end) return;
+    write_empty(a, o, wave);
+    const Course course = course_of(a, o, wave);
+    if (course.tiles <= 0) return;
 
     const float c = a.scale * kLog2e;   // scores in units of log 2
-    const bool padded = a.dim != DP;
-    auto zero_pads = [&](char* tile) {  // columns at and beyond dim: copies leave them out
-        for (int i = lane; i < kCacheTile * kChunks; i += 64) {
-            const int r = i / kChunks, ch = i % kChunks;
-            if (ch * 8 >= a.dim) *reinterpret_cast<u32x4*>(tile + r * kRowBytes + ((ch ^ Tile<DP>::permuted(r)) * 16)) = u32x4{0, 0, 0, 0};
+    char* const tiles = lds + in_group * 2 * kTileBytes;
+    if (a.dim != DP) {                  // columns at and beyond dim: copies leave them out
+        for (int i = lane; i < 2 * kCacheTile * kChunks; i += 64) {
+            const int r = i / kChunks, ch = i % kChunks ^ Tile<DP>::permuted(r % kCacheTile);
+            if (ch * 8 >= a.dim) *reinterpret_cast<u32x4*>(tiles + i * 16) = u32x4{0, 0, 0, 0};
         }
-    };
-    if (padded)
-        for (int i = 0; i < 4; ++i) zero_pads(lds + i * kTileBytes);
+    }
+    // where a lane's transposed values begin: 4 rows of its quarter, 4 elements of 16 columns each
+    const int tr_row = 4 * g + (col >> 2), tr_chunk = (col & 3) >> 1;
 
-    // Three tiles are on their way at a time: one in LDS, one coming there, and the pages of one looked up.
-    auto follow = [&](const Place& p) {   // the place behind this one, in the same part
-        Place n = p;
-        if (++n.tile < p.tiles) return n;
-        n.tile = 0;
-        if (++n.unit < units) return n;
-        n.unit = 0;
-        do {
-            if (++n.seq >= a.n_seqs) break;
-            n.length = uniform(length_of(a, n.seq));
-        } while (n.length == 0);
-        n.tiles = tiles_of(n.length);
-        return n;
-    };
-    auto look_up = [&](const Place& p) {   // the page of the tile's key of number `col`
-        const int key = min(p.tile * kCacheTile + col, p.length - 1);
-        return a.pages[(int64_t)p.seq * a.width + a.page_rows.of((uint32_t)key)];
+    auto look_up = [&](const Place& p) {   // the page of the tile's key of number `of_tile`
+        const int key = p.tile * kCacheTile + of_tile;
+        return key < p.length ? a.pages[(int64_t)p.seq * a.width + a.page_rows.of((uint32_t)key)] : 0;
     };
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef const __attribute__((address_space(1))) void* global_ptr;
-    auto fetch = [&](const Place& p, int page, int buffer) {   // returns which keys lie in no page, a bit each
+    // Sends a tile's keys to registers and its values to LDS; returns which keys there are, a bit each.
+    auto fetch = [&](const Place& p, int page, u32x4 (&k)[2][NK], int buffer) {
+        const int key = p.tile * kCacheTile + of_tile;
         const bool bad = page < 0 || page >= a.n_pages;
-        const int key = min(p.tile * kCacheTile + col, p.length - 1);
+        raise_error(a.err, bad, kDevBadPage);
         const uint32_t in_page = (uint32_t)key - a.page_rows.of((uint32_t)key) * a.page_rows.d;
-        const int64_t from = bad ? 0 : page * a.page + (int64_t)in_page * a.row;
+        const bool there = !bad && key < p.length;
+        const int64_t from = there ? page * a.page + (int64_t)in_page * a.row : 0;
+        const uint32_t seen = (uint32_t)__ballot(there);
         const uint32_t lo = (uint32_t)from, hi = (uint32_t)(from >> 32);
         const int64_t head = (int64_t)(p.unit / o.head_tiles) * a.head;
-        char* const k_tile = lds + buffer * 2 * kTileBytes;
+        const char* const k_src = a.k_pages + head;
+        const char* const v_src = a.v_pages + head;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const char* const row = k_src + (int64_t)((uint64_t)(uint32_t)__shfl((int)hi, 16 * h + col) << 32 | (uint32_t)__shfl((int)lo, 16 * h + col));
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) {
+                k[h][ks] = u32x4{0, 0, 0, 0};
+                if ((seen >> (16 * h + col) & 1) && (4 * ks + g) * 8 < a.dim) k[h][ks] = *reinterpret_cast<const u32x4*>(row + (4 * ks + g) * 16);
+            }
+        }
+        char* const tile = tiles + buffer * kTileBytes;
 #pragma unroll
         for (int n = 0; n < kCopies; ++n) {
             const int id = lane + 64 * n, row = id / kChunks, ch = (id % kChunks) ^ Tile<DP>::permuted(row);
-            const uint64_t at = ((uint64_t)__shfl(hi, row) << 32 | __shfl(lo, row)) + head + ch * 16;
-            if (ch * 8 < a.dim) {
-                __builtin_amdgcn_global_load_lds((global_ptr)(a.k_pages + at), (lds_ptr)(k_tile + n * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_ptr)(a.v_pages + at), (lds_ptr)(k_tile + kTileBytes + n * 1024), 16, 0, 0);
-            }
+            const uint64_t at = (uint64_t)(uint32_t)__shfl((int)hi, row) << 32 | (uint32_t)__shfl((int)lo, row);
+            if (ch * 8 < a.dim && (seen >> row & 1))
+                __builtin_amdgcn_global_load_lds((global_ptr)(v_src + at + ch * 16), (lds_ptr)(tile + n * 1024), 16, 0, 0);
         }
-        return (uint32_t)__ballot(bad);
+        return seen;
     };
-    auto head_of = [&](const Place& p) { return p.unit / o.head_tiles * group + p.unit % o.head_tiles * o.columns + col; };
-    auto counts_in = [&](const Place& p) { return col < min(o.columns, group - p.unit % o.head_tiles * o.columns); };
+    auto columns_of = [&](const Place& p) { return min(o.columns, group - p.unit % o.head_tiles * o.columns); };
+    auto head_of = [&](const Place& p) { return p.unit / o.head_tiles * group + p.unit % o.head_tiles * o.columns; };
+    auto load_q = [&](const Place& p, u32x4 (&q)[BLOCKS][NK]) {
+        const int columns = columns_of(p), head = head_of(p);
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) {
+                q[b][ks] = u32x4{0, 0, 0, 0};
+                if (16 * b + col < columns && (4 * ks + g) * 8 < a.dim)
+                    q[b][ks] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)p.seq * a.q_row + (int64_t)(head + 16 * b + col) * a.q_head +
+                                                               (4 * ks + g) * 16);
+            }
+    };
 
-    f32x16 acc[NB];
-    float top = -INFINITY, sum = 0.f;
-    Stationary<DP> q, q_next;
-    int page = look_up(next), first_tile = next.tile;
-    Place now = next;
-    int64_t left = end - begin;   // tiles of the part, the present one among them
-    uint32_t gone = fetch(now, page, 0), gone_next = 0;
-    q_next.load(a.q + (int64_t)now.seq * a.q_row + (int64_t)head_of(now) * a.q_head, counts_in(now), a.dim, lane);
-    if (left > 1) {
-        next = follow(now);
-        page = look_up(next);
-    }
+    f32x4 acc[BLOCKS][NB];
+    float top[BLOCKS], sum[BLOCKS];
+    u32x4 k[2][2][NK], q[BLOCKS][NK], q_next[BLOCKS][NK];
+    Place now = course.at, next = now, after;
+    int64_t left = course.tiles;   // tiles of the part, the present one among them
+    uint32_t there[2] = {0, 0};
+    int page = look_up(now), page_next = 0, first_tile = 0;
+    if (left > 1) next = following(a, units, now), page_next = look_up(next);
+    load_q(now, q_next);
+    there[0] = fetch(now, page, k[0], 0);
+    page = page_next;
+    after = next;
     bool fresh = true;
-    int buffer = 0;
-#pragma unroll 1
-    for (;; buffer ^= 1) {
+
+    // Three tiles are on their way at a time: one here, one coming, and the pages of one looked up.
+    auto turn = [&](auto of) __attribute__((always_inline)) {
+        constexpr int buffer = decltype(of)::value;
         __builtin_amdgcn_s_waitcnt(0x0070);   // everything on its way is here, and what was read from LDS
         wave_sync();
-        if (gone != 0) {   // keys in no page: zeros, since what is copied in their place need not be finite
-            if (lane == 0) atomicOr(a.err, kDevBadPage);
-            for (int i = lane; i < 2 * kCacheTile * kChunks; i += 64)
-                if (gone >> (i / kChunks % kCacheTile) & 1) *reinterpret_cast<u32x4*>(lds + buffer * 2 * kTileBytes + i * 16) = u32x4{0, 0, 0, 0};
-            wave_sync();
-        }
         if (fresh) {
-            q = q_next;
-            top = -INFINITY, sum = 0.f, first_tile = now.tile;
+            first_tile = now.tile;
 #pragma unroll
-            for (int db = 0; db < NB; ++db) acc[db] = f32x16{};
-        }
-        Place after = next;
-        if (left > 1) {
-            gone_next = fetch(next, page, buffer ^ 1);
-            if (next.tile == 0)
-                q_next.load(a.q + (int64_t)next.seq * a.q_row + (int64_t)head_of(next) * a.q_head, counts_in(next), a.dim, lane);
-            if (left > 2) {
-                after = follow(next);
-                page = look_up(after);
+            for (int b = 0; b < BLOCKS; ++b) {
+                top[b] = -INFINITY, sum[b] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) q[b][ks] = q_next[b][ks];
+#pragma unroll
+                for (int db = 0; db < NB; ++db) acc[b][db] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
+        }
+        if (left > 1) {
+            if (left > 2) after = following(a, units, next), page_next = look_up(after);
+            if (next.tile == 0) load_q(next, q_next);
+            there[buffer ^ 1] = fetch(next, page, k[buffer ^ 1], buffer ^ 1);
         }
 
-        const uint32_t kt = buffer * 2 * kTileBytes, vt = kt + kTileBytes;
-        const int key0 = now.tile * kCacheTile, head = head_of(now);
-        const bool counts = counts_in(now);
-        f32x16 s = scores<T, DP>(lds, kt, q, lane);
-        if (a.bias == nullptr) {
-            s *= c;
-        } else {
-            const int ahead = key0 + 4 * g - (now.length - 1) + a.reach;   // place in the list of buckets, of the lane's first key
+        const uint32_t seen = there[buffer];
+        char* const tile = tiles + buffer * kTileBytes;
+        if (seen != ~0u) {   // values in places of no key: what is there need not be finite
+            for (int i = lane; i < kCacheTile * kChunks; i += 64)
+                if (!(seen >> (i / kChunks) & 1)) *reinterpret_cast<u32x4*>(tile + i * 16) = u32x4{0, 0, 0, 0};
+            wave_sync();
+        }
+        const int nearest = now.length - 1 - now.tile * kCacheTile;   // distance of the tile's first key
+        const int head = head_of(now), columns = columns_of(now);
+        u32x4 weights[BLOCKS];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                int b = a.bucket[max(min(ahead + row_of(i, 0), a.reach), 0)];
-                if (b < 0 || b >= a.n_buckets) {
-                    atomicOr(a.err, kDevBadBucket);
-                    b = 0;
+        for (int b = 0; b < BLOCKS; ++b) {
+            f32x4 s[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) s[h] = mma16(T(), k[buffer][h][ks], q[b][ks], s[h]);
+            }
+            const int my_head = head + min(16 * b + col, columns - 1);
+            if (a.bias == nullptr) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[h] *= c;
+            } else if (nearest - (kCacheTile - 1) >= far) {   // all of its keys are as far as the farthest bucket
+                const float x = in_table ? table[my_head * width + far] : bias_at(my_head, far);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[h][i] = __builtin_fmaf(s[h][i], c, x);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int d = min(max(nearest - (16 * h + 4 * g + i), 0), far);
+                        s[h][i] = __builtin_fmaf(s[h][i], c, in_table ? table[my_head * width + d] : bias_at(my_head, d));
+                    }
+            }
+            if (seen != ~0u) {
+                const uint32_t mine = seen >> (4 * g);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[h][i] = mine >> (16 * h + i) & 1 ? s[h][i] : -INFINITY;
+            }
+            // Weights are relative to a maximum of earlier keys, and as exact for being up to some hundreds: the maximum of
+            // these keys is looked for only where their weights add up to kMost or a head meets its first key.
+            auto raise_top = [&](bool mine) {
+                float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+                most = over_quarters(most, [](float x, float y) { return fmaxf(x, y); });
+                const float to = mine ? fmaxf(top[b], most - kBelow<T>) : top[b];
+                const float shrink = to == top[b] ? 1.f : exp2_fast(top[b] - to);
+                top[b] = to;
+                sum[b] *= shrink;
+#pragma unroll
+                for (int db = 0; db < NB; ++db) acc[b][db] *= shrink;
+            };
+            float p[8];
+            auto weigh = [&] {   // returns their sum
+                const float base = top[b] == -INFINITY ? 0.f : top[b];
+                float part = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = exp2_fast(s[i >> 2][i & 3] - base);
+                    part += p[i];
                 }
-                const float x = counts ? (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head] : 0.f;
-                s[i] = __builtin_fmaf(s[i], c, x <= -65504.f ? -INFINITY : x * kLog2e);
+                return part;
+            };
+            if (__any(top[b] == -INFINITY)) raise_top(top[b] == -INFINITY);
+            float part = weigh();
+            const bool over = !(over_quarters(part, [](float x, float y) { return fmaxf(x, y); }) < kMost<T>);
+            if (__any(over)) {
+                raise_top(over);
+                part = weigh();
             }
+            sum[b] += part;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) weights[b][e] = pack2<T>(p[2 * e], p[2 * e + 1]);
         }
-        if (key0 + kCacheTile > now.length || gone != 0) {
-            const uint32_t none = gone | (key0 + kCacheTile > now.length ? ~0u << (now.length - key0) : 0u);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = none >> row_of(i, g) & 1 ? -INFINITY : s[i];
-        }
-        auto largest = [&] {
-            float most = s[0];
+        for (int db = 0; db < NB; ++db) {
+            typedef short v4i16 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) v4i16* tr_ptr;
+            u32x4 x;
 #pragma unroll
-            for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
-            return fmaxf(most, from_other_half(most));
-        };
-        auto raise_top = [&](bool mine) {
-            const float most = largest();
-            const float to = mine ? fmaxf(top, most - kBelow<T>) : top;
-            const float shrink = to == top ? 1.f : exp2_fast(top - to);
-            top = to;
-            sum *= shrink;
-#pragma unroll
-            for (int db = 0; db < NB; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[db][i] *= shrink;
-        };
-        f32x16 p;
-        auto weights = [&] {   // returns their sum
-            const float base = top == -INFINITY ? 0.f : top;
-            float part = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = exp2_fast(s[i] - base);
-                part += p[i];
+            for (int h = 0; h < 2; ++h) {
+                const int r = 16 * h + tr_row;
+                const char* const place = tile + r * kRowBytes + (((2 * db + tr_chunk) ^ Tile<DP>::permuted(r)) * 16) + (col & 1) * 8;
+                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)place));
+                x[2 * h] = y[0], x[2 * h + 1] = y[1];
             }
-            return part;
-        };
-        if (__any(top == -INFINITY)) raise_top(top == -INFINITY);
-        float part = weights();
-        const bool over = !(fmaxf(part, from_other_half(part)) < kMost<T>);
-        if (__any(over)) {
-            raise_top(over);
-            part = weights();
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) acc[b][db] = mma16(T(), x, weights[b], acc[b][db]);
         }
-        sum += part;
-        accumulate<T, DP>(acc, lds, vt, p, lane);
 
         const bool ends = now.tile + 1 == now.tiles || left == 1;
         if (ends) {
-            const float all = sum + from_other_half(sum);
-            if (first_tile > 0 || now.tile + 1 < now.tiles) {   // a part of a pair
-                const int64_t at = ((int64_t)wave * 2 + (first_tile > 0 ? 0 : 1)) * o.columns + col;
-                if (counts) {
-                    if (g == 0) o.part_ml[2 * at] = top, o.part_ml[2 * at + 1] = all;
+            const bool part = first_tile > 0 || now.tile + 1 < now.tiles;   // of a pair
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const float all = over_quarters(sum[b], [](float x, float y) { return x + y; });
+                const int column = 16 * b + col;
+                if (column >= columns) continue;
+                if (part) {
+                    const int64_t at = ((int64_t)wave * 2 + (first_tile > 0 ? 0 : 1)) * o.columns + column;
+                    if (g == 0) o.part_ml[2 * at] = top[b], o.part_ml[2 * at + 1] = all;
 #pragma unroll
                     for (int db = 0; db < NB; ++db)
+                        if (16 * db + 4 * g < a.dim) *reinterpret_cast<f32x4*>(o.part_o + at * a.dim + 16 * db + 4 * g) = acc[b][db];
+                } else {
+                    const int64_t row = (int64_t)now.seq * a.heads + head + column;
+                    if (g == 0) a.lse[row] = (top[b] + log2_fast(all)) * kLn2;
+                    const bool none = all == 0.f;   // all that it sees is masked by a bias, or in no page
+                    const float scale = none ? 0.f : 1.f / all;
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const int d = 32 * db + row_of(i, g);
-                            if (d < a.dim)   // dim is a multiple of 8, d of 4
-                                *reinterpret_cast<f32x4*>(o.part_o + at * a.dim + d) =
-                                    f32x4{acc[db][i], acc[db][i + 1], acc[db][i + 2], acc[db][i + 3]};
-                        }
+                    for (int db = 0; db < NB; ++db)
+                        if (16 * db + 4 * g < a.dim)
+                            *reinterpret_cast<u32x2*>(static_cast<char*>(a.out) + (row * a.dim + 16 * db + 4 * g) * 2) =
+                                none ? u32x2{0, 0}
+                                     : u32x2{pack2<T>(acc[b][db][0] * scale, acc[b][db][1] * scale), pack2<T>(acc[b][db][2] * scale, acc[b][db][3] * scale)};
                 }
-            } else {
-                const int64_t row = (int64_t)now.seq * a.heads;
-                if (counts && g == 0) a.lse[row + head] = (top + log2_fast(all)) * kLn2;
-                const bool none = all == 0.f;   // all that it sees is masked by a bias, or in no page
-                const int columns = min(o.columns, group - now.unit % o.head_tiles * o.columns);
-                store_rows<T, DP>(acc, none ? 0.f : 1.f / all, none, lds + kt, a.dim, lane, [&](int r) -> char* {
-                    if (r >= columns) return nullptr;
-                    return static_cast<char*>(a.out) + (row + head - col + r) * a.dim * 2;
-                });
-                if (padded) zero_pads(lds + kt);
             }
         }
-        if (--left == 0) break;
+        --left;
         fresh = ends;
-        now = next, next = after, gone = gone_next;
+        now = next, next = after, page = page_next;
+    };
+#pragma unroll 1
+    while (true) {
+        turn(Constant<0>());
+        if (left == 0) break;
+        turn(Constant<1>());
+        if (left == 0) break;
     }
 }
 
@@ -404,10 +387,7 @@ __global__ __launch_bounds__(256) void cache_entries_kernel(CacheAttention a, in
     if ((threadIdx.x & 63) == 0) entries[e] = n;
 }
 
-// Waves of a compute unit: as many as its 160 KB of LDS have room for, two buffers of keys and values each.
 int padded_dim(int dim) { return (dim + 31) / 32 * 32; }
-int tile_bytes(int dim) { return 4 * kCacheTile * 2 * padded_dim(dim); }
-int waves_of_a_unit(int dim) { return 163840 / tile_bytes(dim) < 16 ? 163840 / tile_bytes(dim) : 16; }
 
 struct Plan {
     Share o;
@@ -423,7 +403,8 @@ Plan plan_of(int n_cu, const CacheAttention& a) {
     p.o.n_entries = (int32_t)((a.n_seqs + p.o.each - 1) / p.o.each);
     const int64_t most_tiles = ((int64_t)a.width * a.page_rows.d + kCacheTile - 1) / kCacheTile;
     p.o.cuts = may_be_cut(most_tiles);
-    const int64_t waves = parts_of(most_tiles * a.kv_heads * p.o.head_tiles * a.n_seqs, (int64_t)n_cu * waves_of_a_unit(a.dim));
+    const int of_a_unit = lanes_serve(group, a.dim) ? lanes_waves(group, a.dim) : 4 * waves_of_a_simd(padded_dim(a.dim), group > 16 ? 2 : 1);
+    const int64_t waves = parts_of(most_tiles * a.kv_heads * p.o.head_tiles * a.n_seqs, (int64_t)n_cu * of_a_unit);
     p.o.waves = (int32_t)waves;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     if (p.o.each > 1) p.entry_bytes = up((size_t)p.o.n_entries * 8);
@@ -435,18 +416,31 @@ Plan plan_of(int n_cu, const CacheAttention& a) {
     return p;
 }
 
-template <class T, int DP>
+template <class T, int DP, int BLOCKS>
 hipError_t launch(hipStream_t stream, const CacheAttention& a, const Share& o) {
-    hipLaunchKernelGGL((cache_attention_kernel<T, DP>), grid_of(o.waves), dim3(64), tile_bytes(DP), stream, a, o);
+    const int64_t entries = a.bias == nullptr ? 0 : (int64_t)a.heads * (a.reach + 1);
+    const bool in_table = entries > 0 && entries <= kMostTable;
+    const size_t bytes = kThreads / 64 * 2 * kCacheTile * Tile<DP>::kRowBytes + (in_table ? entries * sizeof(float) : 0);
+    auto kernel = cache_attention_kernel<T, DP, BLOCKS>;
+    if (bytes > 65536) {
+        const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (rc != hipSuccess) return rc;
+    }
+    hipLaunchKernelGGL(kernel, grid_of((o.waves + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), bytes, stream, a, o, in_table ? 1 : 0);
     return hipGetLastError();
+}
+template <class T, int DP>
+hipError_t launch_blocks(hipStream_t stream, const CacheAttention& a, const Share& o) {
+    return a.heads / a.kv_heads > 16 ? launch<T, DP, 2>(stream, a, o) : launch<T, DP, 1>(stream, a, o);
 }
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const CacheAttention& a, const Share& o) {
-    hipError_t rc = a.dim <= 32   ? launch<T, 32>(stream, a, o)
-                    : a.dim <= 64 ? launch<T, 64>(stream, a, o)
-                    : a.dim <= 96 ? launch<T, 96>(stream, a, o)
-                                  : launch<T, 128>(stream, a, o);
+    hipError_t rc = lanes_serve(a.heads / a.kv_heads, a.dim) ? launch_lanes<T>(stream, a, o)
+                    : a.dim <= 32 ? launch_blocks<T, 32>(stream, a, o)
+                    : a.dim <= 64 ? launch_blocks<T, 64>(stream, a, o)
+                    : a.dim <= 96 ? launch_blocks<T, 96>(stream, a, o)
+                                  : launch_blocks<T, 128>(stream, a, o);
     if (rc != hipSuccess || !o.cuts) return rc;
     hipLaunchKernelGGL(cache_attention_join_kernel<T>, grid_of((int64_t)o.waves * o.columns), dim3(kJoinThreads), 0, stream, a, o);
     return hipGetLastError();

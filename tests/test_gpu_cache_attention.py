@@ -45,7 +45,7 @@ SHAPES = [  # lengths, heads, kv_heads, dim, rows of a page, heads first
     ([1], 1, 1, 8, 1, False), ([0], 2, 1, 16, 4, True), ([1, 2, 0, 31, 32, 33], 4, 2, 64, 16, False),
     ([64, 63, 65, 5], 3, 1, 40, 5, True), ([255, 256, 257, 1], 8, 8, 32, 16, False), ([300, 7, 0, 0], 6, 2, 96, 24, True),
     ([1000], 16, 1, 128, 64, False), ([2000, 3], 32, 1, 128, 100, True), ([700, 1501], 40, 1, 72, 16, False),
-    ([513], 66, 2, 24, 7, True), ([9] * 200, 4, 4, 80, 8, False), ([40, 0, 17, 5000], 12, 4, 104, 256, True),
+    ([513], 66, 2, 24, 7, True), ([500, 3, 77], 6, 3, 128, 16, False), ([100, 2000], 8, 2, 64, 16, True), ([90, 31], 4, 2, 16, 8, False), ([77, 900], 34, 2, 128, 16, False), ([31, 1, 40], 10, 2, 88, 16, True), ([9] * 200, 4, 4, 80, 8, False), ([40, 0, 17, 5000], 12, 4, 104, 256, True),
     ([128] * 3, 5, 5, 56, 1024, False), ([3001] * 2, 2, 2, 128, 3, True), ([33, 600], 1, 1, 120, 1, False),
 ]
 
@@ -113,6 +113,12 @@ def test_scales_and_large_scores(ctx):
     args = cache([500, 40, 3], 4, 1, 64, 16, BF, seed=7)
     args[0].mul_(1000.0)
     check(ctx, *args)
+    for heads, kv_heads in ((2, 2), (8, 1), (20, 1)):         # keys and values below 16-bit floats' normal ones
+        q, k, v, k_off, k_pages, v_pages, pages, length = cache([500, 40, 3], heads, kv_heads, 64, 16, HF, seed=8)
+        q.mul_(10_000.0)
+        for x in (k, v, k_pages, v_pages):
+            x.mul_(2.0 ** -18)
+        check(ctx, q, k, v, k_off, k_pages, v_pages, pages, length, scale=3.0)
 
 
 def test_a_bias_that_masks(ctx):
@@ -128,10 +134,11 @@ def test_a_bias_that_masks(ctx):
         assert not out.any() and (lse == -math.inf).all()
 
 
-def test_what_is_not_finite(ctx):
+@pytest.mark.parametrize("group", [2, 5, 20])
+def test_what_is_not_finite(ctx, group):
     """A sequence's keys that are not finite are its own affair, and heads' own."""
     lengths = [100, 40, 70, 33]
-    args = list(cache(lengths, 4, 2, 80, 16, BF, seed=9))
+    args = list(cache(lengths, 2 * group, 2, 80, 16, BF, seed=9))
     q, k, v, k_off, k_pages, v_pages, pages, length = args
 
     def put(s, j, head, d, x, which):
@@ -140,16 +147,16 @@ def test_what_is_not_finite(ctx):
         (k if which == "k" else v)[int(k_off[s]) + j, head, d] = x
 
     put(0, 99, 1, 3, math.nan, "k")
-    put(1, 5, 0, 0, math.inf, "v")
-    q[2, 0:2] = q[2, 0:2].abs() + 0.1
+    put(1, 32, 0, 0, math.inf, "v")                  # the first of a tile that is not full
+    q[2, :group] = q[2, :group].abs() + 0.1
     put(2, 64, 0, 7, -math.inf, "k")                 # scores of minus infinity: the key has no weight
     got = binding.cache_attention(ctx, q, k_pages, v_pages, pages, length)
     r = reference(q, k, v, torch.arange(5), k_off, True, 80 ** -0.5)
     out, lse = (x.cpu().double().numpy() for x in got)
-    assert np.isnan(out[0, 2:]).all() and np.isnan(lse[0, 2:]).all() and np.isfinite(out[0, :2]).all()
-    assert np.isinf(out[1, :2, 0]).all() and np.isfinite(out[1, :2, 1:]).all() and np.isfinite(out[1, 2:]).all()
+    assert np.isnan(out[0, group:]).all() and np.isnan(lse[0, group:]).all() and np.isfinite(out[0, :group]).all()
+    assert np.isinf(out[1, :group, 0]).all() and np.isfinite(out[1, :group, 1:]).all() and np.isfinite(out[1, group:]).all()
     b_out, b_lse = bounds(r, BF, 80, 100)
-    for s, heads in ((0, slice(0, 2)), (1, slice(2, 4)), (2, slice(0, 4)), (3, slice(0, 4))):
+    for s, heads in ((0, slice(0, group)), (1, slice(group, None)), (2, slice(None)), (3, slice(None))):
         # (the score of minus infinity makes its row's largest sum of products infinite, and no bound of it)
         b = np.where(np.isfinite(b_out[s, heads]), b_out[s, heads], 2.25 * 2 ** -8 * r["abs_out"][s, heads] + 1e-4)
         assert (np.abs(out[s, heads] - r["out"][s, heads]) <= b).all(), s
@@ -157,8 +164,9 @@ def test_what_is_not_finite(ctx):
         assert (np.abs(lse[s, heads] - r["lse"][s, heads]) <= b).all(), s
 
 
-def test_lengths_and_pages_that_are_none(ctx):
-    args = cache([100, 40, 70], 4, 2, 64, 16, BF, seed=10)
+@pytest.mark.parametrize("heads", [4, 16, 50])
+def test_lengths_and_pages_that_are_none(ctx, heads):
+    args = cache([100, 40, 70], heads, 2, 64, 16, BF, seed=10)
     q, k, v, k_off, k_pages, v_pages, pages, length = args
     whole = binding.cache_attention(ctx, q, k_pages, v_pages, pages, length)
     for bad in (-1, pages.shape[1] * 16 + 1, 2 ** 31 - 1, -2 ** 31):
@@ -181,9 +189,10 @@ def test_lengths_and_pages_that_are_none(ctx):
         near(lse[:1], r["lse"], b_lse, "lse")
 
 
-def test_a_bucket_that_is_none(ctx):
-    q, k, v, k_off, k_pages, v_pages, pages, length = cache([100], 2, 1, 32, 16, BF, seed=11)
-    how = biased(2, 20, 12, BF)
+@pytest.mark.parametrize("heads", [2, 8, 300])
+def test_a_bucket_that_is_none(ctx, heads):
+    q, k, v, k_off, k_pages, v_pages, pages, length = cache([100], heads, 1, 32, 16, BF, seed=11)
+    how = biased(heads, 20, 12, BF)
     right = how["bucket"].clone()
     right[5] = 0
     want = binding.cache_attention(ctx, q, k_pages, v_pages, pages, length, bias=how["bias"], bucket=right)
