@@ -11,10 +11,10 @@ namespace surel {
 struct Share {
     const int64_t* entries = nullptr;    // tiles of every `each` sequences, or null: each is 1, a sequence's length says it
     int32_t n_entries = 0, each = 1;
-    int32_t waves = 0;
+    int32_t waves = 0, units = 1;        // wave w: part w / units of unit w % units
     int32_t head_tiles = 1, columns = 1; // units of a key head, query heads of a unit (the last has fewer)
-    bool cuts = false;                   // some pair may be cut
-    int64_t* cut = nullptr;              // [waves]: the pair that a wave's part begins inside of, or -1
+    bool cuts = false;                   // some sequence may be cut
+    int32_t* cut = nullptr;              // [waves]: the sequence that a wave's part begins inside of, or -1
     float *part_o = nullptr, *part_ml = nullptr;   // [waves][2][columns][dim], [waves][2][columns][2]: maximum (base 2), sum
 };
 
@@ -61,9 +61,9 @@ struct Lookup {
     }
 };
 
-// A tile of a pair: sequence, unit, tile.
+// A tile of a sequence.
 struct Place {
-    int seq, unit, tile, tiles, length;
+    int seq, tile, tiles, length;
 };
 
 // Writes zeros for sequences of no keys; every wave takes some.
@@ -79,21 +79,20 @@ __device__ __forceinline__ void write_empty(const CacheAttention& a, const Share
     }
 }
 
-// A wave's part: where it begins, and how many tiles it has.  Notes where it begins inside a pair.
+// A wave's part: where it begins, and how many tiles it has.  Notes where it begins inside a sequence.
 struct Course {
     Place at;
     int64_t tiles;   // 0: no part
 };
 __device__ __forceinline__ Course course_of(const CacheAttention& a, const Share& o, int wave) {
-    const int units = a.kv_heads * o.head_tiles;
-    auto tiles_of_seq = [&](int s) { return (int64_t)tiles_of(length_of(a, s)) * units; };
-    auto tiles_of_entry = [&](int e) { return o.entries == nullptr ? tiles_of_seq(e) : o.entries[e] * units; };
+    auto tiles_of_seq = [&](int s) { return (int64_t)tiles_of(length_of(a, s)); };
+    auto tiles_of_entry = [&](int e) { return o.entries == nullptr ? tiles_of_seq(e) : o.entries[e]; };
     Course c;
     c.tiles = 0;
     Lookup list;
     const int64_t tiles = list.sums(o.n_entries, tiles_of_entry);
-    const int64_t parts = parts_of(tiles, o.waves);
-    if (wave < parts) {
+    const int64_t parts = parts_of(tiles, o.waves / o.units), part = wave / o.units;
+    if (part < parts) {
         auto place_of = [&](int64_t target) {   // the place of a tile by its number
             int64_t left;
             int s = list.find(o.n_entries, target, &left, tiles_of_entry);
@@ -108,31 +107,28 @@ __device__ __forceinline__ Course course_of(const CacheAttention& a, const Share
             p.seq = uniform(s);
             p.length = uniform(length_of(a, p.seq));
             p.tiles = tiles_of(p.length);
-            p.unit = uniform((int)(left / p.tiles));
-            p.tile = uniform((int)(left - (int64_t)p.unit * p.tiles));
+            p.tile = uniform((int)left);
             return p;
         };
-        int64_t begin = part_begin(tiles, parts, wave), end = part_begin(tiles, parts, wave + 1);
+        int64_t begin = part_begin(tiles, parts, part), end = part_begin(tiles, parts, part + 1);
         c.at = place_of(begin);
         const int64_t back = moves_back(c.at.tile, c.at.tiles);
         begin -= back, c.at.tile -= (int)back;
-        if (wave + 1 < parts) {
+        if (part + 1 < parts) {
             const Place behind = place_of(end);
             end -= moves_back(behind.tile, behind.tiles);
         }
         c.tiles = end - begin;
     }
-    if (o.cuts && lane_id() == 0) o.cut[wave] = c.tiles > 0 && c.at.tile > 0 ? (int64_t)c.at.seq * units + c.at.unit : -1;
+    if (o.cuts && lane_id() == 0) o.cut[wave] = c.tiles > 0 && c.at.tile > 0 ? c.at.seq : -1;
     return c;
 }
 
 // The place behind one, in the same part.
-__device__ __forceinline__ Place following(const CacheAttention& a, int units, const Place& p) {
+__device__ __forceinline__ Place following(const CacheAttention& a, const Place& p) {
     Place n = p;
     if (++n.tile < p.tiles) return n;
     n.tile = 0;
-    if (++n.unit < units) return n;
-    n.unit = 0;
     do {
         if (++n.seq >= a.n_seqs) break;
         n.length = uniform(length_of(a, n.seq));
@@ -142,7 +138,7 @@ __device__ __forceinline__ Place following(const CacheAttention& a, int units, c
 }
 
 // cache_lanes.hip: rows that few query heads share a key head with, by the vector units.
-bool lanes_serve(int group, int dim);
+bool lanes_serve(int group);
 int lanes_waves(int group, int dim);   // of a compute unit
 template <class T>
 hipError_t launch_lanes(hipStream_t stream, const CacheAttention& a, const Share& o);

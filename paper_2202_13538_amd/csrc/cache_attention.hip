@@ -5,7 +5,7 @@
 namespace surel {
 namespace {
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 512;
 constexpr int kMostDim = 128;
 
 constexpr int kThreads = 256;
@@ -70,8 +70,9 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
         __syncthreads();
     }
     if (wave >= o.waves) return;
-    const int units = a.kv_heads * o.head_tiles, group = a.heads / a.kv_heads;
     write_empty(a, o, wave);
+    const int group = a.heads / a.kv_heads, unit = wave % o.units, column0 = unit % o.head_tiles * o.columns;
+    const int columns = min(o.columns, group - column0), head = unit / o.head_tiles * group + column0;   // the unit's
     const Course course = course_of(a, o, wave);
     if (course.tiles <= 0) return;
 
@@ -92,6 +93,8 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
     };
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef const __attribute__((address_space(1))) void* global_ptr;
+    const char* const k_src = a.k_pages + (int64_t)(unit / o.head_tiles) * a.head;
+    const char* const v_src = a.v_pages + (int64_t)(unit / o.head_tiles) * a.head;
     // Sends a tile's keys to registers and its values to LDS; returns which keys there are, a bit each.
     auto fetch = [&](const Place& p, int page, u32x4 (&k)[2][NK], int buffer) {
         const int key = p.tile * kCacheTile + of_tile;
@@ -102,9 +105,6 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
         const int64_t from = there ? page * a.page + (int64_t)in_page * a.row : 0;
         const uint32_t seen = (uint32_t)__ballot(there);
         const uint32_t lo = (uint32_t)from, hi = (uint32_t)(from >> 32);
-        const int64_t head = (int64_t)(p.unit / o.head_tiles) * a.head;
-        const char* const k_src = a.k_pages + head;
-        const char* const v_src = a.v_pages + head;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const char* const row = k_src + (int64_t)((uint64_t)(uint32_t)__shfl((int)hi, 16 * h + col) << 32 | (uint32_t)__shfl((int)lo, 16 * h + col));
@@ -124,10 +124,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
         }
         return seen;
     };
-    auto columns_of = [&](const Place& p) { return min(o.columns, group - p.unit % o.head_tiles * o.columns); };
-    auto head_of = [&](const Place& p) { return p.unit / o.head_tiles * group + p.unit % o.head_tiles * o.columns; };
     auto load_q = [&](const Place& p, u32x4 (&q)[BLOCKS][NK]) {
-        const int columns = columns_of(p), head = head_of(p);
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
@@ -146,7 +143,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
     int64_t left = course.tiles;   // tiles of the part, the present one among them
     uint32_t there[2] = {0, 0};
     int page = look_up(now), page_next = 0, first_tile = 0;
-    if (left > 1) next = following(a, units, now), page_next = look_up(next);
+    if (left > 1) next = following(a, now), page_next = look_up(next);
     load_q(now, q_next);
     there[0] = fetch(now, page, k[0], 0);
     page = page_next;
@@ -170,7 +167,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
             }
         }
         if (left > 1) {
-            if (left > 2) after = following(a, units, next), page_next = look_up(after);
+            if (left > 2) after = following(a, next), page_next = look_up(after);
             if (next.tile == 0) load_q(next, q_next);
             there[buffer ^ 1] = fetch(next, page, k[buffer ^ 1], buffer ^ 1);
         }
@@ -183,7 +180,6 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
             wave_sync();
         }
         const int nearest = now.length - 1 - now.tile * kCacheTile;   // distance of the tile's first key
-        const int head = head_of(now), columns = columns_of(now);
         u32x4 weights[BLOCKS];
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
@@ -311,69 +307,77 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
     }
 }
 
-// The sums of a pair that several waves share: a workgroup for every wave whose part begins inside a pair, and column;
-// the pair's first of these joins.  Its waves take parts in turn, in a fixed order.
+// The sums of a pair that several waves share: a workgroup for every wave whose part begins inside a pair; the pair's first of
+// these joins.  A wave takes a column, or where columns are few a share of its parts, always the same ones.
 template <class T>
 __global__ __launch_bounds__(kJoinThreads) void cache_attention_join_kernel(CacheAttention a, Share o) {
     constexpr int kWaves = kJoinThreads / 64;
-    __shared__ float tops[kWaves], totals[kWaves], sums[kWaves][kMostDim];
-    const int64_t block = block_number();
-    const int w = (int)(block / o.columns), column = (int)(block % o.columns);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (w < 1 || w >= o.waves) return;
-    const int64_t pair = o.cut[w];
-    if (pair < 0 || o.cut[w - 1] == pair) return;
-    const int units = a.kv_heads * o.head_tiles, group = a.heads / a.kv_heads;
-    const int unit = (int)(pair % units), seq = (int)(pair / units), column0 = unit % o.head_tiles * o.columns;
-    if (column >= min(o.columns, group - column0)) return;
-    int last = w;   // the last wave with a part of the pair
-    for (int from = w + 1;; from += 64) {
-        const unsigned long long in = __ballot(from + lane < o.waves && o.cut[min(from + lane, o.waves - 1)] == pair);
+    __shared__ float totals[kWaves], sums[kWaves][kMostDim];
+    const int w = (int)block_number() + o.units, wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    if (w >= o.waves) return;
+    const int seq = o.cut[w];
+    if (seq < 0 || o.cut[w - o.units] == seq) return;
+    const int group = a.heads / a.kv_heads, unit = w % o.units, column0 = unit % o.head_tiles * o.columns;
+    const int columns = min(o.columns, group - column0), shares = max(kWaves / columns, 1), at_once = kWaves / shares;
+    int parts = 2;   // of the wave of the part before w's (its second), w and those behind it that begin in the sequence (their first)
+    for (int64_t from = w + o.units;; from += 64 * o.units) {
+        const int64_t at = from + (int64_t)lane * o.units;
+        const unsigned long long in = __ballot(at < o.waves && o.cut[min(at, (int64_t)o.waves - 1)] == seq);
         const int n = in == ~0ull ? 64 : (int)__builtin_ctzll(~in);
-        last += n;
+        parts += n;
         if (n < 64) break;
     }
-    const int parts = last - w + 2;   // of waves w - 1 (its second), w, .. last (their first)
-    auto part_of = [&](int i) { return ((int64_t)(w - 1 + i) * 2 + (i == 0 ? 1 : 0)) * o.columns + column; };
-    float top = -INFINITY;
-    for (int i = threadIdx.x; i < parts; i += kJoinThreads) {
-        const float2 ml = *reinterpret_cast<const float2*>(o.part_ml + 2 * part_of(i));
-        if (ml.y != 0.f) top = fmaxf(top, ml.x);   // (a part that saw nothing has no say)
-    }
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, tops[k]);
-    const float base = top == -INFINITY ? 0.f : top;
-    f32x2 x = {0.f, 0.f};
-    float total = 0.f;
     const bool mine = 2 * lane < a.dim;
-#pragma unroll 8
-    for (int i = wave; i < parts; i += kWaves) {
-        const int64_t at = part_of(i);
-        const float2 ml = *reinterpret_cast<const float2*>(o.part_ml + 2 * at);
-        const float weight = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : exp2_fast(ml.x - base);
-        const f32x2 y = mine ? *reinterpret_cast<const f32x2*>(o.part_o + at * a.dim + 2 * lane) : f32x2{0.f, 0.f};
-        total = __builtin_fmaf(weight, ml.y, total);
-        if (weight != 0.f) x[0] = __builtin_fmaf(weight, y[0], x[0]), x[1] = __builtin_fmaf(weight, y[1], x[1]);
-    }
-    if (lane == 0) totals[wave] = total;
-    if (mine) sums[wave][2 * lane] = x[0], sums[wave][2 * lane + 1] = x[1];
-    __syncthreads();
-    if (wave != 0) return;
-    total = 0.f;
-    x = f32x2{0.f, 0.f};
+    for (int c0 = 0; c0 < columns; c0 += at_once) {
+        const int column = c0 + wave / shares, share = wave % shares;
+        const bool works = wave < at_once * shares && column < columns;
+        auto part_of = [&](int i) { return ((w + (int64_t)(i - 1) * o.units) * 2 + (i == 0 ? 1 : 0)) * o.columns + column; };
+        float top = -INFINITY, total = 0.f;
+        f32x2 x = {0.f, 0.f};
+        if (works) {
+            for (int i = lane; i < parts; i += 64) {
+                const f32x2 ml = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * part_of(i));
+                if (ml[1] != 0.f) top = fmaxf(top, ml[0]);   // (a part that saw nothing has no say)
+            }
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-        total += totals[k];
-        if (mine) x[0] += sums[k][2 * lane], x[1] += sums[k][2 * lane + 1];
+            for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+            const float base = top == -INFINITY ? 0.f : top;
+            constexpr int kAhead = 8;   // parts that are read at a time
+            for (int i0 = share; i0 < parts; i0 += kAhead * shares) {
+                f32x2 ml[kAhead], y[kAhead];
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e) {
+                    const int i = i0 + e * shares;
+                    const int64_t at = part_of(min(i, parts - 1));
+                    ml[e] = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * at);
+                    y[e] = mine ? *reinterpret_cast<const f32x2*>(o.part_o + at * a.dim + 2 * lane) : f32x2{0.f, 0.f};
+                    if (i >= parts) ml[e][1] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e) {
+                    const float weight = ml[e][1] == 0.f ? 0.f : ml[e][0] == top ? 1.f : exp2_fast(ml[e][0] - base);
+                    total = __builtin_fmaf(weight, ml[e][1], total);
+                    if (weight != 0.f) x[0] = __builtin_fmaf(weight, y[e][0], x[0]), x[1] = __builtin_fmaf(weight, y[e][1], x[1]);
+                }
+            }
+        }
+        if (shares > 1) {
+            if (lane == 0) totals[wave] = total;
+            if (mine) sums[wave][2 * lane] = x[0], sums[wave][2 * lane + 1] = x[1];
+            __syncthreads();
+            if (works && share == 0)
+                for (int k = 1; k < shares; ++k) {
+                    total += totals[wave + k];
+                    if (mine) x[0] += sums[wave + k][2 * lane], x[1] += sums[wave + k][2 * lane + 1];
+                }
+        }
+        if (works && share == 0) {
+            const int64_t row = (int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column;
+            if (lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + log2_fast(total)) * kLn2;
+            const float scale = total == 0.f ? 0.f : 1.f / total;
+            if (mine) static_cast<uint32_t*>(a.out)[row * (a.dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
+        }
     }
-    const int64_t row = (int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column;
-    if (lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + log2_fast(total)) * kLn2;
-    const float scale = total == 0.f ? 0.f : 1.f / total;
-    if (mine) static_cast<uint32_t*>(a.out)[row * (a.dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
 }
 
 // Tiles of every `each` sequences: a wave an entry.
@@ -403,15 +407,17 @@ Plan plan_of(int n_cu, const CacheAttention& a) {
     p.o.n_entries = (int32_t)((a.n_seqs + p.o.each - 1) / p.o.each);
     const int64_t most_tiles = ((int64_t)a.width * a.page_rows.d + kCacheTile - 1) / kCacheTile;
     p.o.cuts = may_be_cut(most_tiles);
-    const int of_a_unit = lanes_serve(group, a.dim) ? lanes_waves(group, a.dim) : 4 * waves_of_a_simd(padded_dim(a.dim), group > 16 ? 2 : 1);
-    const int64_t waves = parts_of(most_tiles * a.kv_heads * p.o.head_tiles * a.n_seqs, (int64_t)n_cu * of_a_unit);
-    p.o.waves = (int32_t)waves;
+    const int of_a_unit = lanes_serve(group) ? lanes_waves(group, a.dim) : 4 * waves_of_a_simd(padded_dim(a.dim), group > 16 ? 2 : 1);
+    p.o.units = a.kv_heads * p.o.head_tiles;
+    const int64_t of_each = (int64_t)n_cu * of_a_unit / p.o.units;
+    p.o.waves = (int32_t)(p.o.units * parts_of(most_tiles * a.n_seqs, of_each > 1 ? of_each : 1));
+    const size_t waves = (size_t)p.o.waves;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     if (p.o.each > 1) p.entry_bytes = up((size_t)p.o.n_entries * 8);
     if (p.o.cuts) {
-        p.cut_bytes = up((size_t)waves * 8);
-        p.o_bytes = up((size_t)waves * 2 * p.o.columns * a.dim * 4);
-        p.ml_bytes = up((size_t)waves * 2 * p.o.columns * 8);
+        p.cut_bytes = up(waves * 4);
+        p.o_bytes = up(waves * 2 * p.o.columns * a.dim * 4);
+        p.ml_bytes = up(waves * 2 * p.o.columns * 8);
     }
     return p;
 }
@@ -436,13 +442,13 @@ hipError_t launch_blocks(hipStream_t stream, const CacheAttention& a, const Shar
 
 template <class T>
 hipError_t launch_type(hipStream_t stream, const CacheAttention& a, const Share& o) {
-    hipError_t rc = lanes_serve(a.heads / a.kv_heads, a.dim) ? launch_lanes<T>(stream, a, o)
+    hipError_t rc = lanes_serve(a.heads / a.kv_heads) ? launch_lanes<T>(stream, a, o)
                     : a.dim <= 32 ? launch_blocks<T, 32>(stream, a, o)
                     : a.dim <= 64 ? launch_blocks<T, 64>(stream, a, o)
                     : a.dim <= 96 ? launch_blocks<T, 96>(stream, a, o)
                                   : launch_blocks<T, 128>(stream, a, o);
     if (rc != hipSuccess || !o.cuts) return rc;
-    hipLaunchKernelGGL(cache_attention_join_kernel<T>, grid_of((int64_t)o.waves * o.columns), dim3(kJoinThreads), 0, stream, a, o);
+    hipLaunchKernelGGL(cache_attention_join_kernel<T>, grid_of(max(o.waves - o.units, 1)), dim3(kJoinThreads), 0, stream, a, o);
     return hipGetLastError();
 }
 
@@ -461,7 +467,7 @@ hipError_t launch_cache_attention(hipStream_t stream, int n_cu, CacheAttention a
         at += p.entry_bytes;
     }
     if (p.o.cuts) {
-        p.o.cut = reinterpret_cast<int64_t*>(at);
+        p.o.cut = reinterpret_cast<int32_t*>(at);
         p.o.part_o = reinterpret_cast<float*>(at + p.cut_bytes);
         p.o.part_ml = reinterpret_cast<float*>(at + p.cut_bytes + p.o_bytes);
     }

@@ -1,7 +1,7 @@
 // Attention of one row a sequence to its keys in a paged cache, where few query heads share a key head: by the vector
 // units, without LDS.
 //
-// A matrix product's 32 columns would hold one to four heads.  Here lanes hold 16 bytes of a key's row each, 64 / LPK keys at a
+// A matrix product's 16 columns would hold one or two heads.  Here lanes hold 16 bytes of a key's row each, 64 / LPK keys at a
 // time, as they come from memory: products of pairs of elements, sums over the LPK lanes of a key, and every group
 // of lanes keeps the softmax and the sum over its own keys.  Groups are joined at a pair's end: halves of what two lanes hold
 // are exchanged, so that each then adds half as much.
@@ -61,7 +61,7 @@ __device__ __forceinline__ float halves_of_16(float x, float y) {
 }
 
 // Waves of a SIMD: what two tiles of keys and values and the sums of G heads leave room for in its registers.
-constexpr int waves_of_a_simd(int lpk, int g) { return lpk == 16 ? (g == 4 ? 1 : 2) : lpk == 8 ? (g == 1 ? 3 : 2) : g == 4 ? 3 : 4; }
+constexpr int waves_of_a_simd(int lpk, int g) { return lpk == 16 ? 2 : lpk == 8 ? 3 : 4; }
 
 template <class T, int LPK, int G>
 __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes_kernel(CacheAttention a, Share o, int in_table) {
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
         __syncthreads();
     }
     if (wave >= o.waves) return;
-    const int units = a.kv_heads, group = a.heads / a.kv_heads;
+    const int unit = wave % o.units, group = a.heads / a.kv_heads;   // (a unit is a key head here)
     write_empty(a, o, wave);
     const Course course = course_of(a, o, wave);
     if (course.tiles <= 0) return;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
         const uint32_t in_page = (uint32_t)key - a.page_rows.of((uint32_t)key) * a.page_rows.d;
         const int64_t from = bad || key >= p.length ? -1 : page * a.page + (int64_t)in_page * a.row;
         const uint32_t lo = (uint32_t)from, hi = (uint32_t)(from >> 32);
-        const int64_t head = (int64_t)p.unit * a.head + chunk * 16;
+        const int64_t head = (int64_t)unit * a.head + chunk * 16;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int src = s * kKeys + in_step;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
         for (int h = 0; h < G; ++h) {
             q[h] = u32x4{0, 0, 0, 0};
             if (mine && h < group)
-                q[h] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)p.seq * a.q_row + (int64_t)(p.unit * group + h) * a.q_head + chunk * 16);
+                q[h] = *reinterpret_cast<const u32x4*>(a.q + (int64_t)p.seq * a.q_row + (int64_t)(unit * group + h) * a.q_head + chunk * 16);
         }
     };
 
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
     int64_t left = course.tiles;
     uint32_t there[2] = {0, 0};
     int page = look_up(now), page_next = 0, first_tile = 0;
-    if (left > 1) next = following(a, units, now), page_next = look_up(next);
+    if (left > 1) next = following(a, now), page_next = look_up(next);
     load_q(now, q_next);
     there[0] = fetch(now, page, k[0], v[0]);
     page = page_next;
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
             }
         }
         if (left > 1) {
-            if (left > 2) after = following(a, units, next), page_next = look_up(after);
+            if (left > 2) after = following(a, next), page_next = look_up(after);
             if (next.tile == 0) load_q(next, q_next);
             there[buffer ^ 1] = fetch(next, page, k[buffer ^ 1], v[buffer ^ 1]);
         }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
 #pragma unroll
         for (int h = 0; h < G; ++h) {
             if (h >= group) break;
-            const int head = now.unit * group + h;
+            const int head = unit * group + h;
             float most = -INFINITY;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
                 // this lane has elements 4 (lane / 32) + 2 (lane / 16 % 2) and the next one of its chunk's
                 const int d = 8 * chunk + 4 * (lane >> 5) + 2 * ((lane >> 4) & 1);
                 const bool writes = mine && (lane & 15) < LPK;
-                const int64_t row = (int64_t)now.seq * a.heads + now.unit * group + h;
+                const int64_t row = (int64_t)now.seq * a.heads + unit * group + h;
                 if (part) {
                     const int64_t at = ((int64_t)wave * 2 + (first_tile > 0 ? 0 : 1)) * o.columns + h;
                     if (lane == 0) o.part_ml[2 * at] = most, o.part_ml[2 * at + 1] = all;
@@ -275,13 +275,13 @@ hipError_t launch(hipStream_t stream, const CacheAttention& a, const Share& o) {
 template <class T, int LPK>
 hipError_t launch_group(hipStream_t stream, const CacheAttention& a, const Share& o) {
     const int group = a.heads / a.kv_heads;
-    return group == 1 ? launch<T, LPK, 1>(stream, a, o) : group == 2 ? launch<T, LPK, 2>(stream, a, o) : launch<T, LPK, 4>(stream, a, o);
+    return group == 1 ? launch<T, LPK, 1>(stream, a, o) : launch<T, LPK, 2>(stream, a, o);
 }
 
 }  // namespace
 
-bool lanes_serve(int group, int dim) { return group <= 4; }
-int lanes_waves(int group, int dim) { return 4 * waves_of_a_simd(lanes_a_key(dim), group > 2 ? 4 : group); }
+bool lanes_serve(int group) { return group <= 2; }
+int lanes_waves(int group, int dim) { return 4 * waves_of_a_simd(lanes_a_key(dim), group); }
 
 template <class T>
 hipError_t launch_lanes(hipStream_t stream, const CacheAttention& a, const Share& o) {

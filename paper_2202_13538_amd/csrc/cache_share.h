@@ -1,8 +1,9 @@
-// How the keys of a cache's sequences are shared out over waves (cache_attention.hip).
+// How the keys of a cache's sequences are shared out over waves (cache_attention.hip, cache_lanes.hip).
 //
-// A sequence's keys make tiles of 32, once for every unit of it (a key head and up to 32 query heads that read it); a
-// sequence's unit is a pair.  All pairs' tiles in a row, sequences outermost, are cut into equal parts, one a wave; a cut
-// inside a pair of few tiles moves to the pair's start, so that only pairs of many tiles have several waves' sums to join.
+// A sequence's keys make tiles of 32.  All sequences' tiles in a row are cut into equal parts, one a wave, and once so for
+// every unit (a key head and up to 32 query heads that read it): waves of neighbouring numbers take the same keys for
+// different heads, which lie beside one another in memory.  A cut inside a sequence of few tiles moves to its start, so that
+// only long ones have several waves' sums to join.
 #pragma once
 
 #include <stdint.h>
@@ -17,7 +18,7 @@ namespace surel {
 
 constexpr int kCacheTile = 32;      // keys
 constexpr int kLeastTiles = 4;      // of a wave's part, where there are as many
-constexpr int kWholeTiles = 8;      // pairs of up to these many are not cut
+constexpr int kWholeTiles = 8;      // sequences of up to these many are not cut
 constexpr int kLookup = 4096;       // entries that a wave looks through, 64 lanes twice
 
 // Parts of `tiles` tiles for up to `waves` waves, and where the n-th begins (before it moves).
@@ -30,7 +31,7 @@ SUREL_BOTH int64_t part_begin(int64_t tiles, int64_t parts, int64_t n) {
     const int64_t a = tiles / parts, b = tiles % parts;
     return n * a + n * b / parts;
 }
-// A cut t tiles behind the start of a pair of n: how far back it moves.
+// A cut t tiles behind the start of a sequence of n: how far back it moves.
 SUREL_BOTH int64_t moves_back(int64_t t, int64_t n) { return n <= kWholeTiles ? t : 0; }
 SUREL_BOTH bool may_be_cut(int64_t most_tiles) { return most_tiles > kWholeTiles; }
 
