@@ -608,7 +608,7 @@ int surel_cache_store(surel_ctx* ctx, const surel_cache* cache, const void* d_k,
  * surel_attention.  What lies behind a sequence's last key in its last page has no influence, whatever it holds.
  * Sequences' keys are shared out evenly over the device by their lengths, which only the device knows, so a
  * captured call serves any lengths that fit max_pages; sums of sequences that several workgroups share are joined in a
- * fixed order.  The context's workspace grows by at most 8 (dim + 3) min(heads / kv_heads, 32) bytes for each of 16
+ * fixed order.  The context's workspace grows by at most 8 (dim + 4) min(heads / kv_heads, 32) bytes for each of 16
  * wavefronts a compute unit (for each key head, where there are more of these), and by 32 KB where there are more than 4,096
  * sequences.  Results are the same every time.
  * Limits: 0 <= n_seqs <= SUREL_MAX_SEQS, 1 <= max_pages, max_pages * page_rows <= SUREL_MAX_ROWS, heads a multiple of

@@ -14,7 +14,8 @@ struct Share {
     int32_t waves = 0, units = 1;        // wave w: part w / units of unit w % units
     int32_t head_tiles = 1, columns = 1; // units of a key head, query heads of a unit (the last has fewer)
     bool cuts = false;                   // some sequence may be cut
-    int32_t* cut = nullptr;              // [waves]: the sequence that a wave's part begins inside of, or -1
+    int2* cut = nullptr;                 // [waves]: where a wave's is the first part that begins inside a sequence, that one, and
+                                         // how many parts have some of it; else -1
     float *part_o = nullptr, *part_ml = nullptr;   // [waves][2][columns][dim], [waves][2][columns][2]: maximum (base 2), sum
 };
 
@@ -79,16 +80,16 @@ __device__ __forceinline__ void write_empty(const CacheAttention& a, const Share
     }
 }
 
-// A wave's part: where it begins, and how many tiles it has.  Notes where it begins inside a sequence.
+// A wave's part: where it begins, and how many tiles it has.  Notes where it is the first that begins inside a sequence.
 struct Course {
     Place at;
-    int64_t tiles;   // 0: no part
+    int64_t first, tiles;   // its first tile's number; 0 tiles: no part
 };
 __device__ __forceinline__ Course course_of(const CacheAttention& a, const Share& o, int wave) {
     auto tiles_of_seq = [&](int s) { return (int64_t)tiles_of(length_of(a, s)); };
     auto tiles_of_entry = [&](int e) { return o.entries == nullptr ? tiles_of_seq(e) : o.entries[e]; };
     Course c;
-    c.tiles = 0;
+    c.first = c.tiles = 0;
     Lookup list;
     const int64_t tiles = list.sums(o.n_entries, tiles_of_entry);
     const int64_t parts = parts_of(tiles, o.waves / o.units), part = wave / o.units;
@@ -118,9 +119,13 @@ __device__ __forceinline__ Course course_of(const CacheAttention& a, const Share
             const Place behind = place_of(end);
             end -= moves_back(behind.tile, behind.tiles);
         }
-        c.tiles = end - begin;
+        c.first = begin, c.tiles = end - begin;
     }
-    if (o.cuts && lane_id() == 0) o.cut[wave] = c.tiles > 0 && c.at.tile > 0 ? c.at.seq : -1;
+    if (o.cuts && lane_id() == 0) {
+        const int64_t first = c.tiles > 0 ? c.first - c.at.tile : 0;   // the sequence's first tile
+        const bool is_first = c.tiles > 0 && c.at.tile > 0 && part_with(tiles, parts, first) == part - 1;
+        o.cut[wave] = is_first ? int2{c.at.seq, (int)(part_with(tiles, parts, first + c.at.tiles - 1) - part + 2)} : int2{-1, 0};
+    }
     return c;
 }
 

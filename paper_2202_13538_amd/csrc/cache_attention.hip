@@ -6,7 +6,6 @@ namespace surel {
 namespace {
 
 constexpr int kJoinThreads = 512;
-constexpr int kMostDim = 128;
 
 constexpr int kThreads = 256;
 constexpr int kMostTable = 4096;   // biases of all heads by distance that are kept in LDS
@@ -307,77 +306,79 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
     }
 }
 
-// The sums of a pair that several waves share: a workgroup for every wave whose part begins inside a pair; the pair's first of
-// these joins.  A wave takes a column, or where columns are few a share of its parts, always the same ones.
+// The sums of sequences that several waves share: a workgroup for every wave but the first parts', which works where that
+// one's is the first part that begins inside a sequence.  Waves take the maximum and the sum of columns, then threads
+// take pairs of elements, and where these are few a share of the parts, always the same ones.
+// What bounds it: a launch of mostly idle workgroups (4 us), a few trips to memory, and its own code, which hardly any compute
+// unit has read before: loops are kept short (with sums of 16 parts unrolled 6 single rows over 85 parts each took 34 us).
 template <class T>
 __global__ __launch_bounds__(kJoinThreads) void cache_attention_join_kernel(CacheAttention a, Share o) {
     constexpr int kWaves = kJoinThreads / 64;
-    __shared__ float totals[kWaves], sums[kWaves][kMostDim];
-    const int w = (int)block_number() + o.units, wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    __shared__ float tops[32], totals[32];
+    __shared__ f32x2 sums[kJoinThreads];
+    const int w = (int)block_number() + o.units, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
     if (w >= o.waves) return;
-    const int seq = o.cut[w];
-    if (seq < 0 || o.cut[w - o.units] == seq) return;
-    const int group = a.heads / a.kv_heads, unit = w % o.units, column0 = unit % o.head_tiles * o.columns;
-    const int columns = min(o.columns, group - column0), shares = max(kWaves / columns, 1), at_once = kWaves / shares;
-    int parts = 2;   // of the wave of the part before w's (its second), w and those behind it that begin in the sequence (their first)
-    for (int64_t from = w + o.units;; from += 64 * o.units) {
-        const int64_t at = from + (int64_t)lane * o.units;
-        const unsigned long long in = __ballot(at < o.waves && o.cut[min(at, (int64_t)o.waves - 1)] == seq);
-        const int n = in == ~0ull ? 64 : (int)__builtin_ctzll(~in);
-        parts += n;
-        if (n < 64) break;
-    }
-    const bool mine = 2 * lane < a.dim;
-    for (int c0 = 0; c0 < columns; c0 += at_once) {
-        const int column = c0 + wave / shares, share = wave % shares;
-        const bool works = wave < at_once * shares && column < columns;
-        auto part_of = [&](int i) { return ((w + (int64_t)(i - 1) * o.units) * 2 + (i == 0 ? 1 : 0)) * o.columns + column; };
+    const int2 note = o.cut[w];
+    if (note.x < 0) return;
+    const int seq = note.x, parts = note.y, group = a.heads / a.kv_heads;
+    const int unit = w % o.units, column0 = unit % o.head_tiles * o.columns, columns = min(o.columns, group - column0);
+    // A part's sums: of the wave of the part before w's the second, of w and those behind it the first.
+    const int64_t first = ((int64_t)(w - o.units) * 2 + 1) * o.columns, step = 2 * (int64_t)o.units * o.columns;
+    auto part_of = [&](int i) { return first + i * step - (i > 0 ? o.columns : 0); };
+    for (int column = wave; column < columns; column += kWaves) {
         float top = -INFINITY, total = 0.f;
-        f32x2 x = {0.f, 0.f};
-        if (works) {
-            for (int i = lane; i < parts; i += 64) {
-                const f32x2 ml = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * part_of(i));
-                if (ml[1] != 0.f) top = fmaxf(top, ml[0]);   // (a part that saw nothing has no say)
-            }
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-            const float base = top == -INFINITY ? 0.f : top;
-            constexpr int kAhead = 8;   // parts that are read at a time
-            for (int i0 = share; i0 < parts; i0 += kAhead * shares) {
-                f32x2 ml[kAhead], y[kAhead];
-#pragma unroll
-                for (int e = 0; e < kAhead; ++e) {
-                    const int i = i0 + e * shares;
-                    const int64_t at = part_of(min(i, parts - 1));
-                    ml[e] = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * at);
-                    y[e] = mine ? *reinterpret_cast<const f32x2*>(o.part_o + at * a.dim + 2 * lane) : f32x2{0.f, 0.f};
-                    if (i >= parts) ml[e][1] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < kAhead; ++e) {
-                    const float weight = ml[e][1] == 0.f ? 0.f : ml[e][0] == top ? 1.f : exp2_fast(ml[e][0] - base);
-                    total = __builtin_fmaf(weight, ml[e][1], total);
-                    if (weight != 0.f) x[0] = __builtin_fmaf(weight, y[e][0], x[0]), x[1] = __builtin_fmaf(weight, y[e][1], x[1]);
-                }
-            }
+#pragma unroll 1
+        for (int i = lane; i < parts; i += 64) {
+            const f32x2 ml = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * (part_of(i) + column));
+            if (ml[1] == 0.f) continue;   // (a part that saw nothing has no say)
+            const float most = fmaxf(top, ml[0]);
+            total = total * (top == most ? 1.f : exp2_fast(top - most)) + ml[1] * (ml[0] == most ? 1.f : exp2_fast(ml[0] - most));
+            top = most;
         }
-        if (shares > 1) {
-            if (lane == 0) totals[wave] = total;
-            if (mine) sums[wave][2 * lane] = x[0], sums[wave][2 * lane + 1] = x[1];
-            __syncthreads();
-            if (works && share == 0)
-                for (int k = 1; k < shares; ++k) {
-                    total += totals[wave + k];
-                    if (mine) x[0] += sums[wave + k][2 * lane], x[1] += sums[wave + k][2 * lane + 1];
-                }
+#pragma unroll 1
+        for (int m = 1; m < 64; m <<= 1) {
+            const float other = __shfl_xor(top, m), other_total = __shfl_xor(total, m), most = fmaxf(top, other);
+            total = (total == 0.f ? 0.f : total * (top == most ? 1.f : exp2_fast(top - most))) +
+                    (other_total == 0.f ? 0.f : other_total * (other == most ? 1.f : exp2_fast(other - most)));
+            top = most;
         }
-        if (works && share == 0) {
-            const int64_t row = (int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column;
-            if (lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + log2_fast(total)) * kLn2;
-            const float scale = total == 0.f ? 0.f : 1.f / total;
-            if (mine) static_cast<uint32_t*>(a.out)[row * (a.dim / 2) + lane] = pack2<T>(x[0] * scale, x[1] * scale);
+        if (lane == 0) {
+            tops[column] = top, totals[column] = total;
+            a.lse[(int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column] =
+                total == 0.f ? -INFINITY : (top + log2_fast(total)) * kLn2;
         }
     }
+    __syncthreads();
+    const int pairs = columns * (a.dim / 2), shares = max(kJoinThreads / pairs, 1);
+    const int share = shares > 1 ? tid / pairs : 0;
+#pragma unroll 1
+    for (int p = shares > 1 ? tid % pairs : tid; p < pairs && share < shares; p += kJoinThreads) {
+        const int column = p / (a.dim / 2), d = 2 * (p - column * (a.dim / 2));
+        const float total = totals[column], base = tops[column] == -INFINITY ? 0.f : tops[column];
+        f32x2 x = {0.f, 0.f};
+#pragma unroll 8   // (no branches: loads of eight parts are under way at a time)
+        for (int i = share; i < parts; i += shares) {
+            const int64_t at = part_of(i) + column;
+            const f32x2 ml = *reinterpret_cast<const f32x2*>(o.part_ml + 2 * at), y = *reinterpret_cast<const f32x2*>(o.part_o + at * a.dim + d);
+            const float weight = exp2_fast(ml[0] - base);   // (a part that saw nothing has a maximum of minus infinity)
+            x[0] = __builtin_fmaf(weight, y[0], x[0]), x[1] = __builtin_fmaf(weight, y[1], x[1]);
+        }
+        if (shares > 1) sums[tid] = x;
+        else {
+            const float scale = total == 0.f ? 0.f : 1.f / total;
+            static_cast<uint32_t*>(a.out)[(((int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column) * a.dim + d) / 2] =
+                total == 0.f ? 0u : pack2<T>(x[0] * scale, x[1] * scale);
+        }
+    }
+    if (shares == 1) return;
+    __syncthreads();
+    if (tid >= pairs) return;
+    f32x2 x = sums[tid];
+    for (int k = 1; k < shares; ++k) x += sums[tid + k * pairs];
+    const int column = tid / (a.dim / 2), d = 2 * (tid - column * (a.dim / 2));
+    const float total = totals[column], scale = total == 0.f ? 0.f : 1.f / total;
+    static_cast<uint32_t*>(a.out)[(((int64_t)seq * a.heads + unit / o.head_tiles * group + column0 + column) * a.dim + d) / 2] =
+        total == 0.f ? 0u : pack2<T>(x[0] * scale, x[1] * scale);
 }
 
 // Tiles of every `each` sequences: a wave an entry.
@@ -415,7 +416,7 @@ Plan plan_of(int n_cu, const CacheAttention& a) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     if (p.o.each > 1) p.entry_bytes = up((size_t)p.o.n_entries * 8);
     if (p.o.cuts) {
-        p.cut_bytes = up(waves * 4);
+        p.cut_bytes = up(waves * sizeof(int2));
         p.o_bytes = up(waves * 2 * p.o.columns * a.dim * 4);
         p.ml_bytes = up(waves * 2 * p.o.columns * 8);
     }
@@ -467,7 +468,7 @@ hipError_t launch_cache_attention(hipStream_t stream, int n_cu, CacheAttention a
         at += p.entry_bytes;
     }
     if (p.o.cuts) {
-        p.o.cut = reinterpret_cast<int32_t*>(at);
+        p.o.cut = reinterpret_cast<int2*>(at);
         p.o.part_o = reinterpret_cast<float*>(at + p.cut_bytes);
         p.o.part_ml = reinterpret_cast<float*>(at + p.cut_bytes + p.o_bytes);
     }

@@ -31,6 +31,8 @@ SUREL_BOTH int64_t part_begin(int64_t tiles, int64_t parts, int64_t n) {
     const int64_t a = tiles / parts, b = tiles % parts;
     return n * a + n * b / parts;
 }
+// The part that a tile is of, before cuts move: the last that begins at it or before.
+SUREL_BOTH int64_t part_with(int64_t tiles, int64_t parts, int64_t tile) { return ((tile + 1) * parts - 1) / tiles; }
 // A cut t tiles behind the start of a sequence of n: how far back it moves.
 SUREL_BOTH int64_t moves_back(int64_t t, int64_t n) { return n <= kWholeTiles ? t : 0; }
 SUREL_BOTH bool may_be_cut(int64_t most_tiles) { return most_tiles > kWholeTiles; }

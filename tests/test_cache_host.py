@@ -156,6 +156,9 @@ def shared_out(tmp_path, lists):
         for b in begins[:-1]:
             s, n = next((s, n) for s, n in place if s <= b < s + n)
             ask.append((b - s, n))
+        tiles = sorted({random.Random(2).randrange(total) for _ in range(40)} | {0, total - 1})
+        own = evaluate_list(tmp_path, ["cache_share.h"], "part_with(x[0], x[1], x[2])", [(total, parts, t) for t in tiles])
+        assert all(begins[n] <= t < begins[n + 1] for n, t in zip(own, tiles))
         backs = evaluate_list(tmp_path, ["cache_share.h"], "moves_back(x[0], x[1])", ask)
         starts = [b - m for b, m in zip(begins, backs)] + [total]
         out.append((parts, place, starts))
