@@ -127,6 +127,18 @@ def test_narrow_wide_and_lopsided_rows(ctx, classes):
             check(ctx, z, u, temperature)
             check(ctx, z, u, temperature, top_k=k)
             check(ctx, z, u, temperature, top_p=torch.tensor([0.0, 0.1, 0.5, 0.9, 0.99, 0.999999], device="cuda"))
+    # logits that hardly differ from zero, and the largest ones there are
+    z = (torch.randn(6, classes, device="cuda").double() * 1e-41).float()
+    k = torch.tensor([1, 2, 50, classes // 2, classes - 1, classes], dtype=torch.int32, device="cuda")
+    p = torch.tensor([0.0, 0.1, 0.5, 0.9, 0.99, 0.999], device="cuda")
+    for t in (1.0, 1e-41, 1e-45):
+        check(ctx, z, u, torch.full((6,), t, device="cuda"), top_k=k)
+        check(ctx, z, u, torch.full((6,), t, device="cuda"), top_p=p)
+    z = torch.where(torch.randn(6, classes, device="cuda") > 0, 3e38, -3e38)
+    z[:, 3] = 1e38
+    for t in (1.0, 2e38, 3e38):
+        check(ctx, z, u, torch.full((6,), t, device="cuda"), top_k=k, top_p=p)
+        check(ctx, z, u, torch.full((6,), t, device="cuda"), top_p=p, min_p=torch.full((6,), 0.2, device="cuda"))
     # one class far above all others, and one below
     z = torch.zeros(4, classes, device="cuda")
     z[:, 77] = torch.tensor([40.0, 5.0, -60.0, -1e30], device="cuda")
