@@ -23,6 +23,7 @@ constexpr double kFar = 64.0;      // in x: e^-64 of 2^28 classes is 2^-64 of th
 constexpr int kSub = 1024;         // bins of logits of a list
 constexpr int kList = 4096;        // logits of a list, at most
 constexpr int kMostChunks = 1024;  // of a row that one workgroup draws from alone
+constexpr int kMostParted = 2048;  // and of one that several do
 
 __device__ __forceinline__ int threads() { return (int)blockDim.x; }
 
@@ -229,6 +230,27 @@ __device__ __forceinline__ void add_mass(uint64_t* at, uint64_t x) {
     (void)__hip_atomic_fetch_add(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
+// Sums over the lanes up to this one, by moves inside the vector unit (through LDS each of the six steps takes ten times as
+// long, and one workgroup's sums are what a row waits for).
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double moved_from(double x) {   // zero for lanes without a source
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    return __longlong_as_double((long long)((uint64_t)dpp_move<CTRL, ROWS>(0u, (uint32_t)(u >> 32)) << 32 | dpp_move<CTRL, ROWS>(0u, (uint32_t)u)));
+}
+__device__ __forceinline__ double sum_till(double x) {
+    x += moved_from<0x111>(x);        // row_shr:1, 2, 4, 8
+    x += moved_from<0x112>(x);
+    x += moved_from<0x114>(x);
+    x += moved_from<0x118>(x);
+    x += moved_from<0x142, 0xA>(x);   // row_bcast:15 to rows 1 and 3
+    x += moved_from<0x143, 0xC>(x);   // row_bcast:31 to rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ double of_last_lane(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    return __longlong_as_double((long long)((uint64_t)wave_bcast_u32((uint32_t)(u >> 32), 63) << 32 | wave_bcast_u32((uint32_t)u, 63)));
+}
+
 // Sums over the workgroup of what its threads before this one have; *all: of all threads.
 __device__ __forceinline__ uint32_t counts_before(Bench& l, uint32_t mine, uint32_t* all) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -237,8 +259,9 @@ __device__ __forceinline__ uint32_t counts_before(Bench& l, uint32_t mine, uint3
     if (lane == 63) l.counts_of_wave[wave] = x;
     __syncthreads();
     uint32_t before = 0, total = 0;
-    for (int w = 0; w < threads() / 64; ++w) {
-        const uint32_t y = l.counts_of_wave[w];
+#pragma unroll
+    for (int w = 0; w < kMostWaves; ++w) {
+        const uint32_t y = w < threads() / 64 ? l.counts_of_wave[w] : 0;
         before += w < wave ? y : 0;
         total += y;
     }
@@ -247,24 +270,19 @@ __device__ __forceinline__ uint32_t counts_before(Bench& l, uint32_t mine, uint3
 }
 __device__ __forceinline__ double masses_before(Bench& l, double mine, double* all) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    double x = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    const double till = __shfl_up(x, 1);
+    const double x = sum_till(mine), till = moved_from<0x138>(x);   // wave_shr:1
     __syncthreads();
     if (lane == 63) l.of_wave[wave] = x;
     __syncthreads();
     double before = 0.0, total = 0.0;
-    for (int w = 0; w < threads() / 64; ++w) {
-        const double y = l.of_wave[w];
+#pragma unroll
+    for (int w = 0; w < kMostWaves; ++w) {
+        const double y = w < threads() / 64 ? l.of_wave[w] : 0.0;
         if (w < wave) before += y;
         total += y;
     }
     *all = total;
-    return before + (lane == 0 ? 0.0 : till);
+    return before + till;
 }
 
 // The workgroup's bench for a row whose ends every thread has a part of.
@@ -476,9 +494,7 @@ __device__ __forceinline__ void chunk_sums(const Bench& l, const How& h, const R
             n += z == d.at;
         }
     }
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) w += __shfl_xor(w, m), n += __shfl_xor((int)n, m);
-    *mass = w, *ties = n;
+    *mass = of_last_lane(sum_till(w)), *ties = wave_bcast_u32(wave_incl_sum(n), 63);
 }
 
 // The class, from the chunks' sums.
@@ -537,10 +553,12 @@ __device__ __forceinline__ void choose(Bench& l, const SampleArgs& a, int row, c
     till = l.mass_before;
     ties = l.before;
 
-    // inside the chunk, some slots a thread
+    // inside the chunk, some slots a thread.  (Loops that are not unrolled: one workgroup a row comes here, and reads this code
+    // for the first time.  With three loops of eight elements it took 17 us, of 43 for 64 rows of 235,000.)
     const int each = (r.chunk + threads() - 1) / threads(), begin = chunk * r.chunk + (int)threadIdx.x * each;
     const int stop = min(min(begin + each, (chunk + 1) * r.chunk), r.slots);
     n = 0;
+#pragma unroll 1
     for (int s = begin; s < stop; ++s) {
         const u32x4 x = r.load(s);
 #pragma unroll
@@ -548,22 +566,21 @@ __device__ __forceinline__ void choose(Bench& l, const SampleArgs& a, int row, c
     }
     ties += counts_before(l, n, &unused);
     auto weight_in = [&](float z, uint32_t& t) { return z == d.at ? (t++ < kept ? on : 0.0) : kept_weight(l, h, d, z); };
+    auto each_weight = [&](auto act) {
+        uint32_t t = ties;
+#pragma unroll 1
+        for (int s = begin; s < stop; ++s) {
+            const u32x4 x = r.load(s);
+#pragma unroll 1
+            for (int e = 0; e < L::kPer; ++e) act(s * L::kPer + e, weight_in(L::at(x, e), t));
+        }
+    };
     w = 0.0;
-    t = ties;
-    for (int s = begin; s < stop; ++s) {
-        const u32x4 x = r.load(s);
-#pragma unroll
-        for (int e = 0; e < L::kPer; ++e) w += weight_in(L::at(x, e), t);
-    }
+    each_weight([&](int, double m) { w += m; });
     double unused_mass;
     till += masses_before(l, w, &unused_mass);
     mine.at = full.at = -1;
-    t = ties;
-    for (int s = begin; s < stop; ++s) {
-        const u32x4 x = r.load(s);
-#pragma unroll
-        for (int e = 0; e < L::kPer; ++e) take(s * L::kPer + e, weight_in(L::at(x, e), t), 0);
-    }
+    each_weight([&](int at, double m) { take(at, m, 0); });
     if (agree()) {
         a.chosen[row] = mine.at - r.skip;
         a.logp[row] = (float)log(mine.w / total);
@@ -905,6 +922,8 @@ __global__ __launch_bounds__(kThreads) void sample_alone_kernel(SampleArgs a, Pa
 template <class L>
 __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Parts p) {
     __shared__ Bench l;
+    __shared__ double chunk_mass[kMostParted];
+    __shared__ uint32_t chunk_ties[kMostParted];
     const int64_t block = block_number();
     const int row = (int)(block / p.parts), part = (int)(block % p.parts);
     if (row >= a.n_rows) return;
@@ -929,7 +948,9 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Par
         if ((threadIdx.x & 63) == 0) put(&masses[c], mass), put(&ties[c], n);
     }
     if (!last_of(l, &p.turns[4 * row + kDrawTurn], p.parts)) return;
-    choose<L>(l, a, row, r, d, how.first ? 1u : b.ties, [&](int c) { return get_mass(&masses[c]); }, [&](int c) { return get(&ties[c]); });
+    for (int c = threadIdx.x; c < r.chunks; c += kThreads) chunk_mass[c] = get_mass(&masses[c]), chunk_ties[c] = get(&ties[c]);
+    __syncthreads();
+    choose<L>(l, a, row, r, d, how.first ? 1u : b.ties, [&](int c) { return chunk_mass[c]; }, [&](int c) { return chunk_ties[c]; });
 }
 
 struct Plan {
@@ -952,6 +973,7 @@ Plan plan_of(int n_cu, const SampleArgs& a, int type) {
         return x;
     }
     x.p.chunk = 512;
+    while ((slots + x.p.chunk - 1) / x.p.chunk > kMostParted) x.p.chunk *= 2;
     x.p.chunks = (slots + x.p.chunk - 1) / x.p.chunk;
     const int64_t wanted = (2 * (int64_t)n_cu + a.n_rows - 1) / a.n_rows;   // (two fit a compute unit)
     x.p.parts = (int)(wanted < x.p.chunks ? wanted : x.p.chunks);

@@ -219,6 +219,17 @@ def test_many_rows_over_three_classes(ctx):
     assert (logp.double() - p).abs().max() < 1e-6
 
 
+def test_a_row_of_more_classes_than_a_graph_s(ctx):
+    """20 million classes: chunks of several slots a thread."""
+    classes = 20_000_003
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = (torch.randn(1, classes, device="cuda", generator=g) * 2).to(BF)
+    for u in (0.1, 0.77):
+        check(ctx, z, torch.tensor([u], device="cuda"))
+        check(ctx, z, torch.tensor([u], device="cuda"), top_k=torch.tensor([100_000], dtype=torch.int32, device="cuda"),
+              top_p=torch.tensor([0.7], device="cuda"))
+
+
 def test_no_rows(ctx):
     chosen, logp = binding.sample_classes(ctx, torch.empty(0, 5, device="cuda"), torch.empty(0, device="cuda"))
     assert chosen.shape == logp.shape == (0,) and ctx.check() == 0
