@@ -6,38 +6,16 @@
 // slot has to wait for another workgroup's writes.
 #include "cache.h"
 #include "kernels.h"
+#include "wave_sums.h"
 
 namespace surel {
 namespace {
 
-constexpr int kThreads = 1024, kEach = 4;
-constexpr int kChunk = kThreads * kEach;   // sequences whose sums one workgroup makes at a time
+constexpr int kMostThreads = 1024, kFewThreads = 256, kEach = 4;
+constexpr int kChunk = kMostThreads * kEach;   // sequences whose sums one workgroup makes at a time
 
 // Sums of earlier chunks of sequences, where there are several: [chunk][3] of rows, new pages, pages given back.
 enum { kRows = 0, kFresh = 1, kBack = 2, kSums = 3 };
-
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
-
-// What comes before the thread's `mine` in the workgroup, and the workgroup's sum.
-__device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* of_wave, int64_t* all) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int64_t x = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    __syncthreads();   // (of_wave may still be read from an earlier sum)
-    if (lane == 63) of_wave[wave] = x;
-    __syncthreads();
-    const int64_t other = lane < kThreads / 64 ? of_wave[lane] : 0;
-    *all = wave_sum(other);
-    return wave_sum(lane < wave ? other : 0) + x - mine;
-}
 
 // The last i of n with from[i] <= x (from[0] <= x).
 __device__ __forceinline__ int last_at_most(const int32_t* from, int n, int32_t x) {
@@ -50,22 +28,24 @@ __device__ __forceinline__ int last_at_most(const int32_t* from, int n, int32_t 
     return lo;
 }
 
+template <int SEQS>
 struct Lists {              // in LDS, of a chunk's sequences
-    int32_t off[kChunk + 4];     // of rows
-    int32_t fresh[kChunk + 4];   // of new pages
-    int32_t back[kChunk + 4];    // of pages given back
-    int32_t length[kChunk];
-    int32_t after[kChunk];
-    int64_t of_wave[kThreads / 64];
+    int32_t off[SEQS];      // of rows
+    int32_t fresh[SEQS];    // of new pages
+    int32_t back[SEQS];     // of pages given back
+    int32_t length[SEQS];
+    int32_t after[SEQS];
+    double of_wave[16];
 };
 
 // STEP 0: a chunk's rows; 1: its pages, new and given back; 2: everything, `parts` workgroups a chunk.  With one chunk
 // there is step 2 only.  What bounds it: a launch and the sums, three of two barriers each (256 sequences that add a row
 // each: see the measured cases), then the slots that are written.
-template <int STEP>
+// Few threads for few sequences and rows: 256 sequences that add a row each 14 us with 1,024, of which most have nothing to do.
+template <int STEP, int kThreads>
 __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64_t* sums, int chunks, int parts) {
     extern __shared__ __align__(16) char lds[];
-    Lists& l = *reinterpret_cast<Lists*>(lds);
+    Lists<kEach * kThreads>& l = *reinterpret_cast<Lists<kEach * kThreads>*>(lds);
     const int tid = threadIdx.x, chunk = blockIdx.x / parts, part = blockIdx.x % parts;
     const int s0 = chunk * kChunk, n = min(p.n_seqs - s0, kChunk);   // (n may be 0: of no sequences at all)
     const uint32_t page_rows = p.page_rows.d;
@@ -82,8 +62,10 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
         if (length[e] < 0 || length[e] > most) bad = true, length[e] = added[e] = 0;
         rows += max(added[e], 0);
     }
-    int64_t all_rows;
-    int64_t off = sum_before(rows, l.of_wave, &all_rows);
+    // (sums as 64-bit floats: 4,096 numbers below 2^31 add up to less than 2^53)
+    double all;
+    int64_t off = (int64_t)before_in_group((double)rows, l.of_wave, &all);
+    const int64_t all_rows = (int64_t)all;
     if (STEP == 0) {
         if (tid == 0) sums[kSums * chunk + kRows] = all_rows;
         return;
@@ -94,7 +76,8 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
         for (int k = 0; k < (STEP == 1 ? 1 : (int)kSums); ++k) {
             int64_t x = 0;
             for (int c = tid; c < chunk; c += kThreads) x += sums[kSums * c + k];
-            (void)sum_before(x, l.of_wave, &before[k]);
+            (void)before_in_group((double)x, l.of_wave, &all);
+            before[k] = (int64_t)all;
         }
     }
     off += before[kRows];
@@ -116,9 +99,10 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
         back_pages += added[e] < 0 ? held[e] : 0;
     }
     first[kEach] = (int32_t)min(off, (int64_t)p.n_rows);
-    int64_t all_new, all_back;
-    int64_t at_new = sum_before(new_pages, l.of_wave, &all_new) + before[kFresh];
-    int64_t at_back = sum_before(back_pages, l.of_wave, &all_back) + before[kBack];
+    int64_t at_new = (int64_t)before_in_group((double)new_pages, l.of_wave, &all) + before[kFresh];
+    const int64_t all_new = (int64_t)all;
+    int64_t at_back = (int64_t)before_in_group((double)back_pages, l.of_wave, &all) + before[kBack];
+    const int64_t all_back = (int64_t)all;
     if (STEP == 1) {
         if (tid == 0) sums[kSums * chunk + kFresh] = all_new, sums[kSums * chunk + kBack] = all_back;
         return;
@@ -179,7 +163,8 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
         return -1;
     };
     const int32_t some_new = (int32_t)min(before[kFresh], (int64_t)0x7FFFFFFF), till_new = (int32_t)min(end_new, (int64_t)0x7FFFFFFF);
-    for (int64_t f = (int64_t)some_new + part * kThreads + tid; f < till_new; f += parts * kThreads) {
+    // (the three lists begin with different waves, so that small ones do not wait for each other)
+    for (int64_t f = (int64_t)some_new + part * kThreads + (tid ^ kThreads / 2); f < till_new; f += parts * kThreads) {
         const int i = last_at_most(l.fresh, n, (int32_t)f);
         const int32_t at = (int32_t)p.page_rows.of((uint32_t)l.length[i] + page_rows - 1) + (int32_t)f - l.fresh[i];
         p.pages[(int64_t)(s0 + i) * p.width + at] = page_of_ring((int32_t)f);
@@ -187,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
     // pages given back
     const int64_t till_back = min(end_back, (int64_t)room);
     if (part == 0 && tid == 0 && end_back > room) bad_page = true;
-    for (int64_t f = min(before[kBack], (int64_t)0x7FFFFFFF) + part * kThreads + tid; f < till_back; f += parts * kThreads) {
+    for (int64_t f = min(before[kBack], (int64_t)0x7FFFFFFF) + part * kThreads + (tid ^ kThreads / 4 * 3); f < till_back; f += parts * kThreads) {
         const int i = last_at_most(l.back, n, (int32_t)f);
         const int32_t page = p.pages[(int64_t)(s0 + i) * p.width + ((int32_t)f - l.back[i])];
         if (page < 0 || page >= p.n_pages) bad_page = true;
@@ -230,13 +215,14 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
 
 int chunks_of(int64_t n_seqs) { return n_seqs > kChunk ? (int)((n_seqs + kChunk - 1) / kChunk) : 1; }
 
-template <int STEP>
+template <int STEP, int kThreads>
 hipError_t launch_step(hipStream_t stream, const CachePlan& p, int64_t* sums, int chunks, int parts) {
-    auto kernel = cache_plan_kernel<STEP>;
+    auto kernel = cache_plan_kernel<STEP, kThreads>;
+    constexpr size_t bytes = sizeof(Lists<kEach * kThreads>);
     const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)sizeof(Lists));
+                                              (int)bytes);
     if (rc != hipSuccess) return rc;
-    hipLaunchKernelGGL(kernel, dim3(chunks * parts), dim3(kThreads), sizeof(Lists), stream, p, sums, chunks, parts);
+    hipLaunchKernelGGL(kernel, dim3(chunks * parts), dim3(kThreads), bytes, stream, p, sums, chunks, parts);
     return hipGetLastError();
 }
 
@@ -250,13 +236,15 @@ size_t cache_plan_scratch_bytes(int64_t n_seqs) {
 hipError_t launch_cache_plan(hipStream_t stream, int n_cu, CachePlan p, void* scratch) {
     int64_t* const sums = static_cast<int64_t*>(scratch);
     const int chunks = chunks_of(p.n_seqs);
-    // every workgroup makes its chunk's sums first, so it gets four turns of slots to write beside them; two fit a compute unit
-    const int64_t turns = ((int64_t)p.n_rows / chunks + 16 * kThreads - 1) / (16 * kThreads);
-    const int parts = (int)max((int64_t)1, min(turns, (int64_t)(2 * n_cu / chunks)));
+    // every workgroup makes its chunk's sums first, so it gets two turns of slots to write beside them at least; one fits a compute
+    // unit (4.2 million slots by 257 workgroups 29 us)
+    const int64_t turns = ((int64_t)p.n_rows / chunks + 8 * kMostThreads - 1) / (8 * kMostThreads);
+    const int parts = (int)max((int64_t)1, min(turns, (int64_t)(n_cu / chunks)));
+    if (p.n_seqs <= kEach * kFewThreads && parts == 1) return launch_step<2, kFewThreads>(stream, p, sums, 1, 1);
     hipError_t rc = hipSuccess;
-    if (chunks > 1) rc = launch_step<0>(stream, p, sums, chunks, 1);
-    if (chunks > 1 && rc == hipSuccess) rc = launch_step<1>(stream, p, sums, chunks, 1);
-    return rc == hipSuccess ? launch_step<2>(stream, p, sums, chunks, parts) : rc;
+    if (chunks > 1) rc = launch_step<0, kMostThreads>(stream, p, sums, chunks, 1);
+    if (chunks > 1 && rc == hipSuccess) rc = launch_step<1, kMostThreads>(stream, p, sums, chunks, 1);
+    return rc == hipSuccess ? launch_step<2, kMostThreads>(stream, p, sums, chunks, parts) : rc;
 }
 
 }  // namespace surel

@@ -13,6 +13,7 @@
 
 #include "kernels.h"
 #include "matrix_tile.h"
+#include "wave_sums.h"
 
 namespace surel {
 namespace {
@@ -160,8 +161,8 @@ struct Bench {
     How how;
     double roots[16];
     Ends ends[kMostWaves];
-    double of_wave[kMostWaves];
-    uint32_t counts_of_wave[kMostWaves];
+    double of_wave[16];
+    uint32_t counts_of_wave[16];
     int hit, last;                  // what a search found, or the last that is not empty
     uint32_t before;                // counts and weights before it
     double mass_before;
@@ -230,60 +231,11 @@ __device__ __forceinline__ void add_mass(uint64_t* at, uint64_t x) {
     (void)__hip_atomic_fetch_add(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
-// Sums over the lanes up to this one, by moves inside the vector unit (through LDS each of the six steps takes ten times as
-// long, and one workgroup's sums are what a row waits for).
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ double moved_from(double x) {   // zero for lanes without a source
-    const uint64_t u = (uint64_t)__double_as_longlong(x);
-    return __longlong_as_double((long long)((uint64_t)dpp_move<CTRL, ROWS>(0u, (uint32_t)(u >> 32)) << 32 | dpp_move<CTRL, ROWS>(0u, (uint32_t)u)));
-}
-__device__ __forceinline__ double sum_till(double x) {
-    x += moved_from<0x111>(x);        // row_shr:1, 2, 4, 8
-    x += moved_from<0x112>(x);
-    x += moved_from<0x114>(x);
-    x += moved_from<0x118>(x);
-    x += moved_from<0x142, 0xA>(x);   // row_bcast:15 to rows 1 and 3
-    x += moved_from<0x143, 0xC>(x);   // row_bcast:31 to rows 2 and 3
-    return x;
-}
-__device__ __forceinline__ double of_last_lane(double x) {
-    const uint64_t u = (uint64_t)__double_as_longlong(x);
-    return __longlong_as_double((long long)((uint64_t)wave_bcast_u32((uint32_t)(u >> 32), 63) << 32 | wave_bcast_u32((uint32_t)u, 63)));
-}
-
 // Sums over the workgroup of what its threads before this one have; *all: of all threads.
 __device__ __forceinline__ uint32_t counts_before(Bench& l, uint32_t mine, uint32_t* all) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint32_t x = wave_incl_sum(mine);
-    __syncthreads();
-    if (lane == 63) l.counts_of_wave[wave] = x;
-    __syncthreads();
-    uint32_t before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kMostWaves; ++w) {
-        const uint32_t y = w < threads() / 64 ? l.counts_of_wave[w] : 0;
-        before += w < wave ? y : 0;
-        total += y;
-    }
-    *all = total;
-    return before + x - mine;
+    return before_in_group(mine, l.counts_of_wave, all);
 }
-__device__ __forceinline__ double masses_before(Bench& l, double mine, double* all) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const double x = sum_till(mine), till = moved_from<0x138>(x);   // wave_shr:1
-    __syncthreads();
-    if (lane == 63) l.of_wave[wave] = x;
-    __syncthreads();
-    double before = 0.0, total = 0.0;
-#pragma unroll
-    for (int w = 0; w < kMostWaves; ++w) {
-        const double y = w < threads() / 64 ? l.of_wave[w] : 0.0;
-        if (w < wave) before += y;
-        total += y;
-    }
-    *all = total;
-    return before + till;
-}
+__device__ __forceinline__ double masses_before(Bench& l, double mine, double* all) { return before_in_group(mine, l.of_wave, all); }
 
 // The workgroup's bench for a row whose ends every thread has a part of.
 __device__ __forceinline__ Ends over_lanes(Ends e) {
@@ -494,7 +446,7 @@ __device__ __forceinline__ void chunk_sums(const Bench& l, const How& h, const R
             n += z == d.at;
         }
     }
-    *mass = of_last_lane(sum_till(w)), *ties = wave_bcast_u32(wave_incl_sum(n), 63);
+    *mass = of_lane(sum_till(w), 63), *ties = wave_bcast_u32(wave_incl_sum(n), 63);
 }
 
 // The class, from the chunks' sums.
