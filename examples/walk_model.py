@@ -1,4 +1,4 @@
-"""A model of walks: predict the next node of a walk, then read joined sets and continue walks with it.
+"""A model of walks: predict the next node of a walk, then read joined sets, continue walks and generate them with it.
 
     python examples/walk_model.py [--graph rmat4k] [--steps 60]
 
@@ -6,7 +6,8 @@ One attention layer over the steps of sampled walks (a learned bias by step dist
 loss over all nodes of the graph; the node table is both input and output.  Afterwards
 
   - walks are continued by one step: a single query row each over the keys and values of the steps so far;
-  - every link query is pooled: one query row over the rows of its joined set, packed with join_off as they are.
+  - every link query is pooled: one query row over the rows of its joined set, packed with join_off as they are;
+  - walks are generated: their first steps taken in as packed rows, then a node drawn a step, keys and values kept in pages.
 
 Needs an MI355X and the built library.  Everything between the walks and the loss runs in this package's kernels;
 the projections around attention are torch's.
@@ -133,6 +134,54 @@ def continue_walks(lib, graph, model, seeds, m: int = 8):
     return model.read(rows[last], q[last], k, v, one, off), whole
 
 
+class Cache:
+    """Keys and values of running sequences in pages, and its bookkeeping on the device."""
+
+    def __init__(self, lib: binding.Context, n_seqs: int, most: int, heads: int, dim: int, page_rows: int = 8):
+        self.lib, self.page_rows = lib, page_rows
+        width = -(-most // page_rows)                         # pages of a sequence
+        n_pages = n_seqs * width
+        as_int = dict(dtype=torch.int32, device="cuda")
+        self.k, self.v = (torch.empty(n_pages, page_rows, heads, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.pages = torch.full((n_seqs, width), -1, **as_int)
+        self.length = torch.zeros(n_seqs, **as_int)
+        self.ring, self.turn = torch.arange(n_pages, **as_int), torch.tensor([0, n_pages], device="cuda")
+
+    def add(self, added: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
+        """Keeps the packed rows k, v, of which sequence s adds added[s] (negative: it ends).  Returns their offsets."""
+        off, slots, self.length, self.turn = binding.cache_plan(self.lib, self.length, added, self.pages, self.ring,
+                                                                self.turn, self.page_rows, len(k))
+        binding.cache_store(self.lib, k, v, slots, self.k, self.v)
+        return off
+
+
+@torch.no_grad()
+def generate(model, prompts, off, steps: int, u, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0):
+    """Walks continued by drawn nodes: int32[walks][steps].  prompts: packed first steps (node numbers, at least one a walk),
+    off their offsets; u: float32[steps][walks] uniform numbers.  Only the newest step of a walk passes through the model."""
+    lib, n = model.lib, len(off) - 1
+    table = model.table.bfloat16()
+    fill = lambda x, kind: torch.full((n,), x, dtype=kind, device="cuda")  # noqa: E731
+    how = dict(temperature=fill(temperature, torch.float32), top_k=fill(top_k, torch.int32), top_p=fill(top_p, torch.float32))
+    cache = Cache(lib, n, int((off[1:] - off[:-1]).max()) + steps, model.heads, model.head_dim)
+    rows = table[prompts.long()]
+    q, k, v = model.project(rows)
+    cache.add((off[1:] - off[:-1]).int(), k, v)
+    last = model.read(rows, q, k, v, off, off)[off[1:] - 1]   # the prompts' last rows
+    drawn = []
+    one = fill(1, torch.int32)
+    for step in range(steps):
+        node, _ = binding.sample_classes(lib, last @ table.t(), u[step], **how)
+        drawn.append(node)
+        rows = table[node.long()]
+        q, k, v = model.project(rows)
+        cache.add(one, k, v)
+        out, _ = binding.cache_attention(lib, q, cache.k, cache.v, cache.pages, cache.length, bias=model.bias.bfloat16(),
+                                         bucket=model.bucket)
+        last = rows + torch.nn.functional.linear(out.reshape(n, -1), model.mix.weight.bfloat16())
+    return torch.stack(drawn, 1)
+
+
 @torch.no_grad()
 def pool_queries(lib, graph, wl, model, queries, M: int = 50, m: int = 4):
     """A row for every query: one query row (the sum of its nodes') over its joined set."""
@@ -157,6 +206,9 @@ def main() -> None:
     single, whole = continue_walks(lib, graph, model, seeds)
     print("next nodes of 8 walks:", (single @ model.table.bfloat16().t()).argmax(1)[:8].tolist())
     print("single rows and whole walks differ by", (single - whole).abs().max().item())
+    nodes, off = walks_of(lib, graph, seeds, 1, 3, rng_seed=5)
+    walks = generate(model, nodes, off, 8, torch.rand(8, len(seeds), device="cuda"), top_k=50, top_p=0.95)
+    print("a walk of 4 steps and 8 that were drawn:", nodes[:4].tolist(), walks[0].tolist())
     queries = torch.from_numpy(synth.make_queries(wl, *(t.cpu().numpy() for t in graph))).cuda()[:1024]
     print("pooled queries:", tuple(pool_queries(lib, graph, wl, model, queries).shape))
     assert lib.check() == 0
