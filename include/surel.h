@@ -35,7 +35,10 @@
  *     partials, the walk's per-edge neighbour records, the fused kernel's look-back words,
  *     the hash tables and sort arrays of pruning and mini-batching, what attention, the softmax
  *     loss, plans and samples keep between their launches)
- *     and a device error word; nothing else is allocated.
+ *     and a device error word; nothing else is allocated.  The workspace of the calls that continue walks
+ *     (surel_cache_plan, surel_cache_attention, surel_sample_classes) grows to twice its size at least, and what it was
+ *     before is freed with the context only: such calls that were captured go on using it.  Captured calls of one context
+ *     share it like others, so they must not be replayed at the same time.
  *   - Stream capture: a call that is given no h_* pointer only enqueues kernels (no memset,
  *     no copy, no wait), so once an eager call of the same shape has grown the workspaces it
  *     can be captured into a HIP graph and replayed.  surel_prune_rpe, surel_check and the
@@ -645,9 +648,9 @@ int surel_cache_attention(surel_ctx* ctx, const surel_cache* cache, const surel_
  *                  former).
  *   d_logp         float[n_rows] (device, written): the logarithm of the probability that the class was drawn
  *                  with, log(w_c / the kept classes' sum); minus infinity for -1.
- * Weights and sums are 64-bit (borders that sums are compared with are between other classes in 32 bits); weights
- * below e^-64 of the largest count as zero.  Results are the same every time.  The context's workspace grows by up to 128 KB a
- * row where rows are too few to fill the device, and by 12 bytes for every 512 16-byte parts of a row.
+ * Weights and sums are 64-bit (in 32 bits, sums of many classes would be off by more than a class's weight); weights
+ * below e^-64 of the largest count as zero.  Results are the same every time.  Where rows are too few to fill the device, the
+ * context's workspace grows by up to 64 KB a row, 24 bytes for every workgroup that shares it among them.
  * Limits: 0 <= n_rows <= SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, row up to 2^40.  Asynchronous.
  * Device-detected: BAD_CHOICE. */
 int surel_sample_classes(surel_ctx* ctx, int32_t type, const void* d_logits, int64_t row, int64_t n_rows,

@@ -759,9 +759,10 @@ def softmax_loss_grad(ctx: Context, dloss: torch.Tensor, h: torch.Tensor, w: tor
 def _beside(ctx: Context, *tensors: torch.Tensor | None) -> None:
     """Tensors that the context's stream may read and write: on its device, and, where that is not the stream that torch
     works on at the moment, kept from being given away before the stream is done with them."""
+    index = ctx.device.index or 0
     for t in tensors:
-        if t is not None and t.device != ctx.device:
-            raise ValueError(f"every tensor must live on the context's {ctx.device}, got {t.device}")
+        if t is not None and (t.device.type != "cuda" or t.device.index != index):
+            raise ValueError(f"every tensor must live on the context's cuda:{index}, got {t.device}")
     if torch.cuda.current_stream(ctx.device) != ctx.stream:
         for t in tensors:
             if t is not None:

@@ -67,16 +67,19 @@ struct Place {
     int seq, tile, tiles, length;
 };
 
-// Writes zeros for sequences of no keys; every wave takes some.
+// Writes zeros for sequences of no keys; every wave takes some, and looks at 64 of them at a time.
 __device__ __forceinline__ void write_empty(const CacheAttention& a, const Share& o, int wave) {
     const int lane = lane_id();
-    for (int64_t s = wave; s < a.n_seqs; s += o.waves) {
-        const int n = uniform(a.length[s]);
-        if (n > 0 && n <= a.width * (int64_t)a.page_rows.d) continue;
-        if (n != 0 && lane == 0) atomicOr(a.err, kDevBadLength);
-        uint32_t* const out = static_cast<uint32_t*>(a.out) + s * a.heads * (a.dim / 2);
-        for (int i = lane; i < a.heads * (a.dim / 2); i += 64) out[i] = 0;
-        for (int i = lane; i < a.heads; i += 64) a.lse[s * a.heads + i] = -INFINITY;
+    for (int64_t first = (int64_t)wave * 64; first < a.n_seqs; first += (int64_t)o.waves * 64) {
+        const int n = first + lane < a.n_seqs ? a.length[first + lane] : 1;
+        const bool bad = n < 0 || n > a.width * (int64_t)a.page_rows.d;
+        raise_error(a.err, bad, kDevBadLength);
+        for (unsigned long long none = __ballot(n == 0 || bad); none != 0; none &= none - 1) {
+            const int64_t s = first + (int)__builtin_ctzll(none);
+            uint32_t* const out = static_cast<uint32_t*>(a.out) + s * a.heads * (a.dim / 2);
+            for (int i = lane; i < a.heads * (a.dim / 2); i += 64) out[i] = 0;
+            for (int i = lane; i < a.heads; i += 64) a.lse[s * a.heads + i] = -INFINITY;
+        }
     }
 }
 

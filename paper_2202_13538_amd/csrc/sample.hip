@@ -76,16 +76,17 @@ struct RowOf {
         const char* const at = base + (int64_t)slot * 16;
         const int first = slot * L::kPer;
         if (first >= skip && first + L::kPer <= end) return *reinterpret_cast<const u32x4*>(at);
+        // (a loop, as this is in many places: one workgroup's first pass over code that nobody has read yet is what a small
+        // row waits for)
         u32x4 x = {L::kNone, L::kNone, L::kNone, L::kNone};
+#pragma unroll 1
+        for (int e = max(skip - first, 0); e < min(end - first, L::kPer); ++e) {
+            constexpr int kBits = 128 / L::kPer, kOfWord = 32 / kBits;
+            const uint32_t z = kBits == 32 ? reinterpret_cast<const uint32_t*>(at)[e] : reinterpret_cast<const uint16_t*>(at)[e];
+            const int shift = e % kOfWord * kBits, word = e / kOfWord;
+            const uint32_t mask = (kBits == 32 ? ~0u : 0xFFFFu) << shift;
 #pragma unroll
-        for (int e = 0; e < L::kPer; ++e) {
-            if (first + e < skip || first + e >= end) continue;
-            if constexpr (L::kPer == 4) {
-                x[e] = reinterpret_cast<const uint32_t*>(at)[e];
-            } else {
-                const uint32_t z = reinterpret_cast<const uint16_t*>(at)[e];
-                x[e >> 1] = e & 1 ? (x[e >> 1] & 0xFFFFu) | z << 16 : (x[e >> 1] & 0xFFFF0000u) | z;
-            }
+            for (int w = 0; w < 4; ++w) x[w] = w == word ? (x[w] & ~mask) | z << shift : x[w];
         }
         return x;
     }
@@ -262,9 +263,9 @@ __device__ __forceinline__ void set_up(Bench& l, const SampleArgs& a, const Give
 // The first of n bins that is not empty and up to which counts reach k, or (by_mass) weights reach the target; count and mass
 // of a bin by its number, at most n / threads of them a thread.  Leaves in l.hit which, or where none is the last that is not
 // empty (by_mass: sums in another order may differ in their last places), or -1, and in l.before and l.mass_before what
-// comes before it, on top of what is given.
+// comes before it, on top of what is given.  masses: weights are asked for.
 template <class Count, class Mass>
-__device__ __forceinline__ void search(Bench& l, int bins, bool by_mass, uint32_t k, double target, uint32_t before, double mass_before,
+__device__ __forceinline__ void search(Bench& l, int bins, bool by_mass, bool masses, uint32_t k, double target, uint32_t before, double mass_before,
                                        Count count, Mass mass) {
     const int each = (bins + threads() - 1) / threads(), first = threadIdx.x * each, end = min(first + each, bins);
     uint32_t n = 0, all;
@@ -272,7 +273,7 @@ __device__ __forceinline__ void search(Bench& l, int bins, bool by_mass, uint32_
     for (int i = first; i < end; ++i) n += count(i), w += mass(i);
     if (threadIdx.x == 0) l.hit = 0x7FFFFFFF, l.last = -1;
     uint32_t till = before + counts_before(l, n, &all);
-    double till_w = mass_before + masses_before(l, w, &all_w);
+    double till_w = masses ? mass_before + masses_before(l, w, &all_w) : 0.0;
     uint32_t my_till = 0, full_till = 0;
     double my_till_w = 0.0, full_till_w = 0.0;
     int mine = -1, full = -1;
@@ -342,7 +343,7 @@ __device__ __forceinline__ void open_border(Bench& l, const uint64_t* bins, Bord
     __syncthreads();
     int hit = -1;
     if (l.how.k != 0) {
-        search(l, kBins, false, l.how.k, 0.0, 0, 0.0, [&](int i) { return i < kBins - 1 ? count_in(bins[i]) : 0u; }, [](int) { return 0.0; });
+        search(l, kBins, false, false, l.how.k, 0.0, 0, 0.0, [&](int i) { return i < kBins - 1 ? count_in(bins[i]) : 0u; }, [](int) { return 0.0; });
         hit = l.hit;
         if (hit >= 0 && threadIdx.x == 0) b->open = 1, b->from = b->to = hit, b->before = l.before;
         __syncthreads();
@@ -381,7 +382,7 @@ __device__ __forceinline__ void find_border(Bench& l, SubBins& sub, Border* b, i
             if (masses) add_mass(&sub.mass[i], whole_of(exp64(l.roots, fmax(((double)logit_of<L>(key) - (double)top) * how.inv_t, -2.0 * kFar)), one));
         });
         __syncthreads();
-        search(l, kSub, by_p, how.k, target, before, mass_before, [&](int i) { return sub.count[i]; },
+        search(l, kSub, by_p, masses, how.k, target, before, mass_before, [&](int i) { return sub.count[i]; },
                [&](int i) { return masses ? (double)sub.mass[i] * of_top : 0.0; });
         const int hit = l.hit;
         if (hit < 0) break;   // (of a list that is not empty one is found)
@@ -616,19 +617,28 @@ __device__ __forceinline__ void find_in_row(Bench& l, SubBins& sub, Border* b, c
         const int at = atomicAdd(&l.n_list, 1);
         if (at < kList) sub.list[at] = key;
     });
-    double before, all;
-    (void)masses_before(l, m.before, &before);
-    (void)masses_before(l, m.all, &all);
+    double before = 0.0, all = 0.0;
+    if (how.p < 1.0) {
+        (void)masses_before(l, m.before, &before);
+        (void)masses_before(l, m.all, &all);
+    }
     __syncthreads();
     const int n = l.n_list;
     find_border<L>(l, sub, b, n_classes, before, all, [&](auto act) {
         if (n <= kList) {
             for (int i = threadIdx.x; i < n; i += threads()) act(sub.list[i]);
         } else {
-            each_logit<L>(r, 0, r.slots, [&](float z) {
-                const int bin = bin_of(how, z);
-                if (bin >= now.from && bin <= now.to) act(key_of<L>(z));
-            });
+            // (hardly ever: loops that keep the code short)
+#pragma unroll 1
+            for (int s = threadIdx.x; s < r.slots; s += threads()) {
+                const u32x4 x = r.load(s);
+#pragma unroll 1
+                for (int e = 0; e < L::kPer; ++e) {
+                    const float z = L::at(x, e);
+                    const int bin = bin_of(how, z);
+                    if (bin >= now.from && bin <= now.to) act(key_of<L>(z));
+                }
+            }
         }
     });
 }

@@ -167,16 +167,16 @@ def shared_out(tmp_path, lists):
 
 def test_keys_are_shared_out_whole(tmp_path):
     rng = random.Random(1)
-    lists = [([1], 1), ([1], 512), ([9], 512), ([8] * 30, 7), ([2048], 1280), ([5, 2000, 1, 1, 40] * 3, 100)]
+    lists = [([1], 1), ([1], 512), ([17], 512), ([8] * 30, 7), ([2048], 1280), ([5, 2000, 1, 1, 40] * 3, 100)]
     lists += [([rng.choice([1, 2, 8, 9, 33, 300]) for _ in range(rng.randint(1, 60))], rng.choice([1, 3, 64, 1024]))
               for _ in range(12)]
     for (counts, waves), (parts, place, starts) in zip(lists, shared_out(tmp_path, lists), strict=True):
         assert 1 <= parts <= waves and starts[0] == 0 and starts == sorted(starts)
         for s, n in place:
             cuts = [b for b in set(starts) if s < b < s + n]
-            assert not cuts or n > 8                        # only long pairs are cut
+            assert not cuts or n > 16                        # only long pairs are cut
         most = max(b - a for a, b in zip(starts, starts[1:]))
-        assert most <= -(-sum(counts) // parts) + 8         # a part's own tiles and one short pair
+        assert most <= -(-sum(counts) // parts) + 16         # a part's own tiles and one short pair
 
 
 def test_lists_that_are_looked_through_are_short(tmp_path):
