@@ -45,6 +45,10 @@ constexpr int waves_of_a_simd(int padded, int blocks) {
 // Scores are K q^T, so that a head's lie in the four lanes of a column, its softmax runs inside lanes, and the weights are the
 // operand of out^T += V^T p^T as they come.  Keys go from memory to registers, as the first product's operand lies; values, which
 // the second needs transposed, through LDS, without passing through registers.
+// What bounds it: memory, and for caches of a gigabyte and less the starts and ends of parts.  256 caches of 1 to 8,192 keys, 16
+// heads to 2 of 128 elements, with a bias: 215 us, 4.8 TB/s; 1,024 of them 811 with the join, 5.4 TB/s.  (With 32-column
+// products and keys through LDS as well, 302: four times the softmax for 8 heads, and half the waves.)  Weights are rounded to
+// 16 bits for their product, as surel_attention's are; sums and statistics are 32-bit.
 template <class T, int DP, int BLOCKS>
 __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_attention_kernel(CacheAttention a, Share o, int in_table) {
     constexpr int NB = DP / 16, NK = DP / 32, kRowBytes = Tile<DP>::kRowBytes, kTileBytes = kCacheTile * kRowBytes;
@@ -309,8 +313,8 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
 // The sums of sequences that several waves share: a workgroup for every wave but the first parts', which works where that
 // one's is the first part that begins inside a sequence.  Waves take the maximum and the sum of columns, then threads
 // take pairs of elements, and where these are few a share of the parts, always the same ones.
-// What bounds it: a launch of mostly idle workgroups (4 us), a few trips to memory, and its own code, which hardly any compute
-// unit has read before: loops are kept short (with sums of 16 parts unrolled 6 single rows over 85 parts each took 34 us).
+// What bounds it: a launch of mostly idle workgroups (4 us) and a few trips to memory: 15 us for 24 sums of 85 parts, 12 for 512 of
+// five.  (A branch around a part's weight keeps loads of several parts from being under way together: 26 and 34 us.)
 template <class T>
 __global__ __launch_bounds__(kJoinThreads) void cache_attention_join_kernel(CacheAttention a, Share o) {
     constexpr int kWaves = kJoinThreads / 64;

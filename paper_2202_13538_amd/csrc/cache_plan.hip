@@ -39,8 +39,8 @@ struct Lists {              // in LDS, of a chunk's sequences
 };
 
 // STEP 0: a chunk's rows; 1: its pages, new and given back; 2: everything, `parts` workgroups a chunk.  With one chunk
-// there is step 2 only.  What bounds it: a launch and the sums, three of two barriers each (256 sequences that add a row
-// each: see the measured cases), then the slots that are written.
+// there is step 2 only.  What bounds it: a launch, three sums of two barriers each and a few trips to memory behind one another
+// (256 sequences that add a row each 12 us), then the search for every four slots' sequence (4.2 million slots 26).
 // Few threads for few sequences and rows: 256 sequences that add a row each 14 us with 1,024, of which most have nothing to do.
 template <int STEP, int kThreads>
 __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64_t* sums, int chunks, int parts) {

