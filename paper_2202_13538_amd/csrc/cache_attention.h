@@ -145,6 +145,58 @@ __device__ __forceinline__ Place following(const CacheAttention& a, const Place&
     return n;
 }
 
+// Biases by distance, in units of log 2, for a call's distances 0 .. farthest: of all heads in LDS where these are few, else
+// looked up.  (A bias of fp16's lowest value or less is a mask.)
+__host__ __device__ __forceinline__ int farthest(const CacheAttention& a) {   // beyond it biases are alike, or no key is
+    const int64_t keys = (int64_t)a.width * a.page_rows.d;
+    return a.reach < keys ? a.reach : (int)keys - 1;
+}
+template <class T>
+struct Biases {
+    const CacheAttention& a;
+    const float* table;   // [heads][far + 1], or null
+    int far;
+    __device__ __forceinline__ int bucket_of(int distance, bool* bad) const {
+        const int b = a.bucket[a.reach - distance];
+        const bool none = b < 0 || b >= a.n_buckets;
+        *bad = *bad || none;
+        return none ? 0 : b;
+    }
+    __device__ __forceinline__ float in_bucket(int b, int head) const {
+        const float x = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head];
+        return x <= -65504.f ? -INFINITY : x * kLog2e;
+    }
+    __device__ __forceinline__ float at(int head, int distance) const {
+        if (table != nullptr) return table[head * (far + 1) + distance];
+        bool bad = false;
+        const float x = in_bucket(bucket_of(distance, &bad), head);
+        if (bad) atomicOr(a.err, kDevBadBucket);
+        return x;
+    }
+    // All threads of a workgroup, four entries each at a time, so that their trips to memory are together.
+    __device__ __forceinline__ void fill(float* to) const {
+        const int n = a.heads * (far + 1), threads = (int)blockDim.x;
+        bool bad = false;
+#pragma unroll 1
+        for (int i0 = threadIdx.x; i0 < n; i0 += 4 * threads) {
+            int b[4], head[4];
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = min(i0 + e * threads, n - 1);
+                head[e] = i / (far + 1);
+                b[e] = bucket_of(i - head[e] * (far + 1), &bad);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = in_bucket(b[e], head[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i0 + e * threads < n) to[i0 + e * threads] = x[e];
+        }
+        raise_error(a.err, bad, kDevBadBucket);
+    }
+};
+
 // cache_lanes.hip: rows that few query heads share a key head with, by the vector units.
 bool lanes_serve(int group);
 int lanes_waves(int group, int dim);   // of a compute unit

@@ -53,25 +53,17 @@ template <class T, int DP, int BLOCKS>
 __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_attention_kernel(CacheAttention a, Share o, int in_table) {
     constexpr int NB = DP / 16, NK = DP / 32, kRowBytes = Tile<DP>::kRowBytes, kTileBytes = kCacheTile * kRowBytes;
     constexpr int kChunks = Tile<DP>::kChunks, kCopies = kCacheTile * kChunks / 64;
-    extern __shared__ __align__(256) char lds[];   // [wave][buffer], then biases [heads][reach + 1] by distance
+    extern __shared__ __align__(256) char lds[];   // [wave][buffer], then biases, see Biases
     const int lane = threadIdx.x & 63, in_group = uniform((int)(threadIdx.x >> 6));
     const int g = lane >> 4, col = lane & 15, of_tile = lane & 31;
     const int wave = (int)block_number() * (kThreads / 64) + in_group;
     float* const table = reinterpret_cast<float*>(lds + kThreads / 64 * 2 * kTileBytes);
-    const int far = a.reach, width = far + 1;
-    auto bias_at = [&](int head, int distance) {
-        int b = a.bucket[far - distance];
-        if (b < 0 || b >= a.n_buckets) {
-            atomicOr(a.err, kDevBadBucket);
-            b = 0;
-        }
-        const float x = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head];
-        return x <= -65504.f ? -INFINITY : x * kLog2e;
-    };
+    const Biases<T> biases = {a, in_table ? table : nullptr, farthest(a)};
     if (in_table) {
-        for (int i = threadIdx.x; i < a.heads * width; i += kThreads) table[i] = bias_at(i / width, i % width);
+        biases.fill(table);
         __syncthreads();
     }
+    const int far = biases.far;
     if (wave >= o.waves) return;
     write_empty(a, o, wave);
     const int group = a.heads / a.kv_heads, unit = wave % o.units, column0 = unit % o.head_tiles * o.columns;
@@ -198,7 +190,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
 #pragma unroll
                 for (int h = 0; h < 2; ++h) s[h] *= c;
             } else if (nearest - (kCacheTile - 1) >= far) {   // all of its keys are as far as the farthest bucket
-                const float x = in_table ? table[my_head * width + far] : bias_at(my_head, far);
+                const float x = biases.at(my_head, far);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -209,7 +201,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int d = min(max(nearest - (16 * h + 4 * g + i), 0), far);
-                        s[h][i] = __builtin_fmaf(s[h][i], c, in_table ? table[my_head * width + d] : bias_at(my_head, d));
+                        s[h][i] = __builtin_fmaf(s[h][i], c, biases.at(my_head, d));
                     }
             }
             if (seen != ~0u) {
@@ -429,7 +421,7 @@ Plan plan_of(int n_cu, const CacheAttention& a) {
 
 template <class T, int DP, int BLOCKS>
 hipError_t launch(hipStream_t stream, const CacheAttention& a, const Share& o) {
-    const int64_t entries = a.bias == nullptr ? 0 : (int64_t)a.heads * (a.reach + 1);
+    const int64_t entries = a.bias == nullptr ? 0 : (int64_t)a.heads * (farthest(a) + 1);
     const bool in_table = entries > 0 && entries <= kMostTable;
     const size_t bytes = kThreads / 64 * 2 * kCacheTile * Tile<DP>::kRowBytes + (in_table ? entries * sizeof(float) : 0);
     auto kernel = cache_attention_kernel<T, DP, BLOCKS>;

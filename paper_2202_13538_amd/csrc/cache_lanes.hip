@@ -69,23 +69,15 @@ constexpr int waves_of_a_simd(int lpk, int g) { return lpk == 16 ? 2 : lpk == 8 
 template <class T, int LPK, int G>
 __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes_kernel(CacheAttention a, Share o, int in_table) {
     constexpr int kKeys = 64 / LPK, kSteps = kCacheTile / kKeys;
-    extern __shared__ float table[];   // [heads][reach + 1], by distance, in units of log 2
+    extern __shared__ float table[];   // biases, see Biases
     const int lane = threadIdx.x & 63, wave = uniform((int)block_number() * (kThreads / 64) + (int)(threadIdx.x >> 6));
     const int chunk = lane % LPK, in_step = lane / LPK, col = lane & 31;
-    const int far = a.reach, width = far + 1;
-    auto bias_at = [&](int head, int distance) {
-        int b = a.bucket[far - distance];
-        if (b < 0 || b >= a.n_buckets) {
-            atomicOr(a.err, kDevBadBucket);
-            b = 0;
-        }
-        const float x = (float)static_cast<const typename T::elem*>(a.bias)[(int64_t)b * a.heads + head];
-        return x <= -65504.f ? -INFINITY : x * kLog2e;
-    };
+    const Biases<T> biases = {a, in_table ? table : nullptr, farthest(a)};
     if (in_table) {
-        for (int i = threadIdx.x; i < a.heads * width; i += kThreads) table[i] = bias_at(i / width, i % width);
+        biases.fill(table);
         __syncthreads();
     }
+    const int far = biases.far;
     if (wave >= o.waves) return;
     const int unit = wave % o.units, group = a.heads / a.kv_heads;   // (a unit is a key head here)
     write_empty(a, o, wave);
@@ -176,14 +168,14 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(LPK, G)) void cache_lanes
             }
             if (a.bias != nullptr) {
                 if (all_far) {
-                    const float x = in_table ? table[head * width + far] : bias_at(head, far);
+                    const float x = biases.at(head, far);
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) p[h][s] += x;
                 } else {
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) {
                         const int d = min(max(nearest - (s * kKeys + in_step), 0), far);
-                        p[h][s] += in_table ? table[head * width + d] : bias_at(head, d);
+                        p[h][s] += biases.at(head, d);
                     }
                 }
             }
@@ -269,7 +261,7 @@ int lanes_a_key(int dim) { return dim <= 16 ? 2 : dim <= 32 ? 4 : dim <= 64 ? 8 
 
 template <class T, int LPK, int G>
 hipError_t launch(hipStream_t stream, const CacheAttention& a, const Share& o) {
-    const int64_t entries = a.bias == nullptr ? 0 : (int64_t)a.heads * (a.reach + 1);
+    const int64_t entries = a.bias == nullptr ? 0 : (int64_t)a.heads * (farthest(a) + 1);
     const bool in_table = entries > 0 && entries <= kMostTable;
     hipLaunchKernelGGL((cache_lanes_kernel<T, LPK, G>), grid_of((o.waves + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads),
                        in_table ? entries * sizeof(float) : 0, stream, a, o, in_table ? 1 : 0);
