@@ -577,6 +577,7 @@ typedef struct surel_cache {
  *                for those behind the last sequence's.
  *   d_length_after, d_turn_after   int32[n_seqs], int64[2] (device, written): lengths with the added rows, 0 for
  *                sequences that end, and the ring's counters.  Neither may be the array it follows.
+ * A page belongs to one sequence (one that two hold is given back twice).
  * Pages are taken in the order of sequences, and given back in that order; those given back by a call can be taken from
  * the next one on.  Rows that find no free page (NO_PAGE), do not fit max_pages or lie beyond n_rows (CAPACITY) are not
  * added: d_length_after says how many keys a sequence has in earnest.  Given the same arguments again (d_pages and d_ring as

@@ -28,6 +28,14 @@ __device__ __forceinline__ int last_at_most(const int32_t* from, int n, int32_t 
     return lo;
 }
 
+// The same for all lanes of a wave at once, up to 4,096 numbers: 64 of them are looked at at a time.
+__device__ __forceinline__ int wave_last_at_most(const int32_t* from, int n, int32_t x) {
+    const int lane = lane_id();
+    const int group = max((int)__popcll(__ballot(64 * lane < n && from[min(64 * lane, n - 1)] <= x)) - 1, 0);
+    const int at = 64 * group + lane;
+    return 64 * group + max((int)__popcll(__ballot(at < n && from[min(at, n - 1)] <= x)) - 1, 0);
+}
+
 template <int SEQS>
 struct Lists {              // in LDS, of a chunk's sequences
     int32_t off[SEQS];      // of rows
@@ -40,7 +48,7 @@ struct Lists {              // in LDS, of a chunk's sequences
 
 // STEP 0: a chunk's rows; 1: its pages, new and given back; 2: everything, `parts` workgroups a chunk.  With one chunk
 // there is step 2 only.  What bounds it: a launch, three sums of two barriers each and a few trips to memory behind one another
-// (256 sequences that add a row each 12 us), then the search for every four slots' sequence (4.2 million slots 26).
+// (256 sequences that add a row each 12 us), and behind these the pages and slots of 256 workgroups (4.2 million slots 24).
 // Few threads for few sequences and rows: 256 sequences that add a row each 14 us with 1,024, of which most have nothing to do.
 template <int STEP, int kThreads>
 __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64_t* sums, int chunks, int parts) {
@@ -181,9 +189,17 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
     // slots, four rows a thread; behind the last sequence's rows there are none
     const int32_t row_begin = (int32_t)min(before[kRows], (int64_t)p.n_rows), row_end = last ? p.n_rows : end_rows;
     const bool wide = (reinterpret_cast<uintptr_t>(p.slots) & 15u) == 0;
-    for (int64_t r = (row_begin & ~3) + 4 * ((int64_t)part * kThreads + tid); r < row_end; r += 4 * (int64_t)parts * kThreads) {
-        int i = r < end_rows ? last_at_most(l.off, n, max((int32_t)r, row_begin)) : 0;
-        int32_t slot[4];
+    const int lane = tid & 63, first_lane = __builtin_amdgcn_readfirstlane(tid) & ~63;
+    for (int64_t wave_row = (row_begin & ~3) + 4 * ((int64_t)part * kThreads + first_lane); wave_row < row_end; wave_row += 4 * (int64_t)parts * kThreads) {
+        const int64_t r = wave_row + 4 * lane;
+        // a wave's 256 rows are of neighbouring sequences: these first, then a lane's own among them
+        int i = 0;
+        if (wave_row < end_rows && n > 0) {
+            const int lo = wave_last_at_most(l.off, n, max((int32_t)wave_row, row_begin));
+            const int hi = wave_last_at_most(l.off, n, (int32_t)min(wave_row + 255, (int64_t)end_rows - 1));
+            i = lo + last_at_most(l.off + lo, hi - lo + 1, (int32_t)min(max(r, (int64_t)row_begin), (int64_t)end_rows - 1));
+        }
+        int32_t slot[4], page = -1, page_seq = -1, page_turn = -1;   // (rows of one page look it up once)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int32_t row = (int32_t)r + e;
@@ -193,13 +209,14 @@ __global__ __launch_bounds__(kThreads) void cache_plan_kernel(CachePlan p, int64
             const int32_t length = l.length[i], at = length + (row - l.off[i]);
             if (at >= l.after[i]) continue;
             const int32_t turn = (int32_t)p.page_rows.of((uint32_t)at), have = (int32_t)p.page_rows.of((uint32_t)length + page_rows - 1);
-            int32_t page;
-            if (turn < have) {
+            if (i == page_seq && turn == page_turn) {
+            } else if (turn < have) {
                 page = p.pages[(int64_t)(s0 + i) * p.width + turn];
                 if (page < 0 || page >= p.n_pages) bad_page = true, page = -1;
             } else {
                 page = page_of_ring(l.fresh[i] + turn - have);
             }
+            page_seq = i, page_turn = turn;
             if (page >= 0) slot[e] = (int32_t)((uint32_t)page * page_rows + ((uint32_t)at - (uint32_t)turn * page_rows));
         }
         if (wide && r >= row_begin && r + 4 <= row_end) {
