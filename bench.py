@@ -91,10 +91,12 @@ def read_membench():
 
 
 def passes_of_case(torch, args) -> float:
-    """Microseconds of a pass of a case of perf/cases.py among others."""
-    from perf import cases
+    """Microseconds of a pass of a case of perf/cases.py or perf/more_operators.py among others."""
+    from perf import cases, more_operators
 
-    state = cases.prepare(next(c for c in cases.listed() if c["name"] == args.case), 1)
+    more_operators.own = True
+    cases, case = next((m, c) for m in (cases, more_operators) for c in m.listed() if c["name"] == args.case)
+    state = cases.prepare(case, 1)
     for _ in range(args.warmup):
         cases.run(state)
     torch.cuda.synchronize()
@@ -277,7 +279,8 @@ def main() -> int:
                          "them as one JSON line: the measured ceilings of this GPU that the "
                          "roofline.as_moved figures are compared with")
     ap.add_argument("--case",
-                    help="instead of the pipeline, run W + K passes of this case of perf/cases.py and "
+                    help="instead of the pipeline, run W + K passes of this case of perf/cases.py or "
+                         "perf/more_operators.py and "
                          "print the time of one of the K (what the traces of the cases were made with)")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="after the timed region, run three plain 1 GiB read + 1 GiB write "
