@@ -455,6 +455,12 @@ __device__ __forceinline__ void chunk_sums(const Bench& l, const How& h, const R
     *mass = of_lane(sum_till(w), 63), *ties = wave_bcast_u32(wave_incl_sum(n), 63);
 }
 
+__device__ __forceinline__ void no_class(const Bench& l, const SampleArgs& a, int row) {
+    if (threadIdx.x != 0) return;
+    a.chosen[row] = -1;
+    a.logp[row] = -INFINITY;
+    if (l.how.wrong) atomicOr(a.err, kDevBadChoice);
+}
 // The class, from the chunks' sums.
 template <class L, class Mass, class Ties>
 __device__ __forceinline__ void choose(Bench& l, const SampleArgs& a, int row, const RowOf<L>& r, const Drawn& d, uint32_t most_ties,
@@ -505,9 +511,13 @@ __device__ __forceinline__ void choose(Bench& l, const SampleArgs& a, int row, c
         take(c, of_chunk(c, ties), ties);
         ties += ties_of(c);
     }
-    if (agree()) l.lo = (uint32_t)mine.at, l.mass_before = mine.till, l.before = mine.ties;
+    if (agree()) l.mass_before = mine.till, l.before = mine.ties;
     __syncthreads();
-    const int chunk = (int)l.lo;
+    const int chunk = l.hit != 0x7FFFFFFF ? l.hit : l.last;
+    if (chunk < 0) {   // (the largest logit is always kept; but a row that changes under the call is not to lead anywhere)
+        no_class(l, a, row);
+        return;
+    }
     till = l.mass_before;
     ties = l.before;
 
@@ -545,12 +555,6 @@ __device__ __forceinline__ void choose(Bench& l, const SampleArgs& a, int row, c
     }
 }
 
-__device__ __forceinline__ void no_class(const Bench& l, const SampleArgs& a, int row) {
-    if (threadIdx.x != 0) return;
-    a.chosen[row] = -1;
-    a.logp[row] = -INFINITY;
-    if (l.how.wrong) atomicOr(a.err, kDevBadChoice);
-}
 __device__ __forceinline__ bool has_border(const How& h) { return !h.first && (h.k != 0 || h.p < 1.0); }
 
 // Goes through the slots begin .. end - 1 of a row.
