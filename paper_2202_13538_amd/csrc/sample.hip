@@ -219,9 +219,10 @@ __device__ __forceinline__ float place_of(const How& h, float z) {
     return fminf((0.5f * h.most - 0.5f * z) * h.bins, (float)(kBins - 1));
 }
 __device__ __forceinline__ int bin_of(const How& h, float z) { return (int)place_of(h, z); }
-// A bin's number of classes, 30 bits, and the sum of how far they lie in it, 34, in parts of 2^-inside_bits of its width.
+// A bin's number of classes, 30 bits, and the sum of how far they lie in it, 34, in parts of 2^-inside_bits of its width
+// (31 bits at most: a class's is a 32-bit word).
 constexpr int kInside = 34;
-__device__ __forceinline__ int inside_bits(int n_classes) { return kInside - (32 - __clz(n_classes)); }
+__device__ __forceinline__ int inside_bits(int n_classes) { return min(kInside - (32 - __clz(n_classes)), 31); }
 __device__ __forceinline__ uint32_t count_in(uint64_t bin) { return (uint32_t)(bin >> kInside); }
 
 // Weights relative to a list's largest as whole numbers: 2^unit of them are one.  Their sum stays below 2^63.
