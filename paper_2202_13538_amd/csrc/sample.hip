@@ -6,8 +6,8 @@
 // logit), and how far they lie inside them is added up.  Counts say which bin the k-th class is in; a bin's weights, by their
 // expansion up to that first moment, are known to h^2 of them (h its width, 1/64 at most), so that the border of top_p lies
 // in one of few bins.  The logits of these are put into a list, the weights before
-// them added up, and the border found in the list.  There weights are whole numbers of 44 bits and more relative to the
-// list's largest, so that their sums are the same in whatever order they are made.
+// them added up, and the border found in the list.  There weights are whole numbers of two words relative to the list's
+// largest, so that their sums are the same in whatever order they are made.
 // The draw adds weights up in 64 bits in the order of classes: by chunks, then inside the one that u falls into.
 // What bounds it: for many rows the exponentials of what is kept and the barriers of a row (4,096 rows of 10,001 classes by
 // min-p 73 us); for few long ones four to six passes over the row, of which a bare one takes 9 us for 64 rows of 235,000 in 16 bits
@@ -225,11 +225,11 @@ constexpr int kInside = 34;
 __device__ __forceinline__ int inside_bits(int n_classes) { return min(kInside - (32 - __clz(n_classes)), 31); }
 __device__ __forceinline__ uint32_t count_in(uint64_t bin) { return (uint32_t)(bin >> kInside); }
 
-// Weights relative to a list's largest as whole numbers: 2^unit of them are one.  Their sum stays below 2^63.
+// Weights relative to a list's largest as whole numbers of two words: `one` = 2^unit of the first are one, and as many of the
+// second, which is signed, one of the first.  Their sums stay below 2^63, and what is left out of a weight is at most
+// 2^-(2 unit + 1): of all of a row's 2^-39 in the longest rows, 2^-60 in those of 2.9 million.  (One word left out up to 2^-41 of each
+// there: of a tail of classes of 2^-33 of the largest some thousands too many were kept, of 20 million of 2^-38 a quarter too few.)
 __device__ __forceinline__ int unit_of(int n_classes) { return min(62 - (32 - __clz(n_classes)), 50); }
-__device__ __forceinline__ uint64_t whole_of(double w, double one) {   // rounded, by a sum whose last place is 1
-    return (uint64_t)__double_as_longlong(__builtin_fma(w, one, 0x1p52)) - 0x4330000000000000ull;
-}
 
 __device__ __forceinline__ void add_count(uint32_t* at, uint32_t n) {
     (void)__hip_atomic_fetch_add(at, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -243,6 +243,13 @@ __device__ __forceinline__ uint32_t counts_before(Bench& l, uint32_t mine, uint3
     return before_in_group(mine, l.counts_of_wave, all);
 }
 __device__ __forceinline__ double masses_before(Bench& l, double mine, double* all) { return before_in_group(mine, l.of_wave, all); }
+
+__device__ __forceinline__ void add_weight(uint64_t* first, uint64_t* second, double w, double one) {
+    const double near = __builtin_fma(w, one, 0x1p52);   // rounded, by a sum whose last place is 1
+    add_mass(first, (uint64_t)__double_as_longlong(near) - 0x4330000000000000ull);
+    const double rest = __builtin_fma(w, one, -(near - 0x1p52));
+    add_mass(second, (uint64_t)__double_as_longlong(__builtin_fma(rest, one, 0x1.8p52)) - 0x4338000000000000ull);
+}
 
 // The workgroup's bench for a row whose ends every thread has a part of.
 __device__ __forceinline__ Ends over_lanes(Ends e) {
@@ -358,9 +365,9 @@ __device__ __forceinline__ void open_border(Bench& l, const uint64_t* bins, Bord
 }
 
 // The border among the logits of its bins, which each() goes through; every thread takes some.  mass_before: the weights
-// before them, total: all there are.
+// before them, total: all there are.  rest: kSub words of LDS, weights' second ones.
 template <class L, class Each>
-__device__ __forceinline__ void find_border(Bench& l, SubBins& sub, Border* b, int n_classes, double mass_before, double total, Each each) {
+__device__ __forceinline__ void find_border(Bench& l, SubBins& sub, uint64_t* rest, Border* b, int n_classes, double mass_before, double total, Each each) {
     const How how = l.how;
     const int unit = unit_of(n_classes);
     const double one = ldexp(1.0, unit), back = ldexp(1.0, -unit);
@@ -379,17 +386,26 @@ __device__ __forceinline__ void find_border(Bench& l, SubBins& sub, Border* b, i
     const double of_top = weight_of(l, how, top) * back;
     for (;;) {
         const int shift = max(32 - (int)__clz(hi - lo) - 10, 0);   // (hi - lo) >> shift is below kSub
-        for (int i = threadIdx.x; i < kSub; i += threads()) sub.count[i] = 0, sub.mass[i] = 0;
+        const bool add = masses && shift > 0;   // (bins of one logit: their counts say what they weigh)
+        for (int i = threadIdx.x; i < kSub; i += threads()) sub.count[i] = 0, sub.mass[i] = rest[i] = 0;
         __syncthreads();
         each([&](uint32_t key) {
             if (key < lo || key > hi) return;
             const uint32_t i = (hi - key) >> shift;
             add_count(&sub.count[i], 1);
-            if (masses) add_mass(&sub.mass[i], whole_of(exp64(l.roots, fmax(((double)logit_of<L>(key) - (double)top) * how.inv_t, -2.0 * kFar)), one));
+            if (add) add_weight(&sub.mass[i], &rest[i], exp64(l.roots, fmax(((double)logit_of<L>(key) - (double)top) * how.inv_t, -2.0 * kFar)), one);
         });
         __syncthreads();
+        if (masses && shift == 0) {
+            for (int i = threadIdx.x; i < kSub; i += threads())
+                if (const uint32_t n = sub.count[i]; n != 0) sub.mass[i] = (uint64_t)__double_as_longlong((double)n * weight_of(l, how, logit_of<L>(hi - i)));
+            __syncthreads();
+        }
         search(l, kSub, by_p, masses, how.k, target, before, mass_before, [&](int i) { return sub.count[i]; },
-               [&](int i) { return masses ? (double)sub.mass[i] * of_top : 0.0; });
+               [&](int i) {
+                   return !add ? __longlong_as_double((long long)sub.mass[i])
+                               : __builtin_fma((double)(int64_t)rest[i], back, (double)sub.mass[i]) * of_top;
+               });
         const int hit = l.hit;
         if (hit < 0) break;   // (of a list that is not empty one is found)
         before = l.before, mass_before = l.mass_before;
@@ -618,7 +634,7 @@ __device__ __forceinline__ Masses border_logits(const Bench& l, const How& how, 
 
 // A row's border once its bins are known, by one workgroup: from a list of their logits if that holds them, or by the row.
 template <class L>
-__device__ __forceinline__ void find_in_row(Bench& l, SubBins& sub, Border* b, const RowOf<L>& r, int n_classes) {
+__device__ __forceinline__ void find_in_row(Bench& l, SubBins& sub, uint64_t* rest, Border* b, const RowOf<L>& r, int n_classes) {
     if (threadIdx.x == 0) l.n_list = 0;
     __syncthreads();
     const How how = l.how;
@@ -634,7 +650,7 @@ __device__ __forceinline__ void find_in_row(Bench& l, SubBins& sub, Border* b, c
     }
     __syncthreads();
     const int n = l.n_list;
-    find_border<L>(l, sub, b, n_classes, before, all, [&](auto act) {
+    find_border<L>(l, sub, rest, b, n_classes, before, all, [&](auto act) {
         if (n <= kList) {
             for (int i = threadIdx.x; i < n; i += threads()) act(sub.list[i]);
         } else {
@@ -653,10 +669,10 @@ __device__ __forceinline__ void find_in_row(Bench& l, SubBins& sub, Border* b, c
     });
 }
 template <class L>
-__device__ __forceinline__ void find_all_in_row(Bench& l, const uint64_t* bins, SubBins& sub, Border* b, const RowOf<L>& r, int n_classes) {
+__device__ __forceinline__ void find_all_in_row(Bench& l, const uint64_t* bins, SubBins& sub, uint64_t* rest, Border* b, const RowOf<L>& r, int n_classes) {
 #pragma unroll 1
     for (int open = b->open; open != 0; open = b->open) {
-        find_in_row<L>(l, sub, b, r, n_classes);
+        find_in_row<L>(l, sub, rest, b, r, n_classes);
         if (open == 1 && l.how.p < 1.0) open_p(l, bins, b, n_classes, b->whole);
     }
 }
@@ -674,7 +690,10 @@ __device__ __forceinline__ Drawn drawn_by(const How& h, const Border& b) {
 struct RowLds {
     Bench bench;
     Border border;
-    double mass[kMostChunks];
+    union {
+        double mass[kMostChunks];
+        uint64_t rest[kSub];        // (while the border is looked for.  With 8 KB more one row fits a compute unit, not two)
+    };
     uint32_t ties[kMostChunks];
 };
 struct BorderLds {
@@ -707,7 +726,7 @@ __global__ __launch_bounds__(kThreads, BORDERS ? 4 : 6) void sample_row_kernel(S
         count_bins<L>(l.bench, w.bins, r, 0, r.slots, a.n_classes);
         __syncthreads();
         open_border(l.bench, w.bins, &l.border, a.n_classes);
-        find_all_in_row<L>(l.bench, w.bins, w.sub, &l.border, r, a.n_classes);
+        find_all_in_row<L>(l.bench, w.bins, w.sub, l.rest, &l.border, r, a.n_classes);
     }
     __syncthreads();
     const Drawn d = drawn_by<L>(how, l.border);
@@ -825,6 +844,7 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a, Par
     extern __shared__ __align__(16) char dynamic[];
     __shared__ Bench l;
     __shared__ Border b;
+    __shared__ uint64_t rest[kSub];
     const int64_t block = block_number();
     const int row = (int)(block / p.parts), part = (int)(block % p.parts);
     if (row >= a.n_rows) return;
@@ -858,7 +878,7 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a, Par
     (void)masses_before(l, my_before, &before);
     (void)masses_before(l, my_all, &all);
     __syncthreads();
-    find_border<L>(l, w.sub, &b, a.n_classes, before, all, [&](auto act) {
+    find_border<L>(l, w.sub, rest, &b, a.n_classes, before, all, [&](auto act) {
         for (int i = threadIdx.x; i < (int)n; i += kThreads) act(w.sub.list[i]);
     });
     if (now.open == 1 && l.how.p < 1.0) {
@@ -878,6 +898,7 @@ __global__ __launch_bounds__(kThreads) void sample_alone_kernel(SampleArgs a, Pa
     extern __shared__ __align__(16) char dynamic[];
     __shared__ Bench l;
     __shared__ Border b;
+    __shared__ uint64_t rest[kSub];
     const int64_t place = block_number();
     if (place >= a.n_rows || p.border[place].alone == 0) return;
     const int row = (int)place;
@@ -887,7 +908,7 @@ __global__ __launch_bounds__(kThreads) void sample_alone_kernel(SampleArgs a, Pa
     for (int i = threadIdx.x; i < kBins; i += kThreads) w.bins[i] = p.bins[(int64_t)row * kBins + i];
     if (threadIdx.x == 0) b = p.border[row];
     __syncthreads();
-    find_all_in_row<L>(l, w.bins, w.sub, &b, r, a.n_classes);
+    find_all_in_row<L>(l, w.bins, w.sub, rest, &b, r, a.n_classes);
     if (threadIdx.x == 0) p.border[row] = b;
 }
 
