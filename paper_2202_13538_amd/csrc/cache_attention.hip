@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
     int64_t left = course.tiles;   // tiles of the part, the present one among them
     uint32_t there[2] = {0, 0};
     int page = look_up(now), page_next = 0, first_tile = 0;
-    if (left > 1) next = following(a, now), page_next = look_up(next);
+    if (left > 1) next = following(a, o, now), page_next = look_up(next);
     load_q(now, q_next);
     there[0] = fetch(now, page, k[0], 0);
     page = page_next;
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_a
             }
         }
         if (left > 1) {
-            if (left > 2) after = following(a, next), page_next = look_up(after);
+            if (left > 2) after = following(a, o, next), page_next = look_up(after);
             if (next.tile == 0) load_q(next, q_next);
             there[buffer ^ 1] = fetch(next, page, k[buffer ^ 1], buffer ^ 1);
         }
