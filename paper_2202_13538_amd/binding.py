@@ -756,17 +756,27 @@ def softmax_loss_grad(ctx: Context, dloss: torch.Tensor, h: torch.Tensor, w: tor
     return dh, dw
 
 
-def _beside(ctx: Context, *tensors: torch.Tensor | None) -> None:
-    """Tensors that the context's stream may read and write: on its device, and, where that is not the stream that torch
-    works on at the moment, kept from being given away before the stream is done with them."""
+def _beside(ctx: Context, tensors, *outputs):
+    """Tensors that the context's stream may read and write: the given ones have to be on its device, and new ones, a (shape,
+    dtype) each, are made there and returned.  Where torch works on another stream at the moment, the given ones are kept from
+    being given away before the context's is done with them, and the new ones are that stream's own memory, kept likewise:
+    memory of torch's present stream may be what its unfinished work still reads or writes."""
     index = ctx.device.index or 0
     for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != index):
+        if t is not None and t.get_device() != index:   # (-1: not on a GPU)
             raise ValueError(f"every tensor must live on the context's cuda:{index}, got {t.device}")
-    if torch.cuda.current_stream(ctx.device) != ctx.stream:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(ctx.stream)
+    some = tensors[0]
+    present = torch.cuda.current_stream(ctx.device)
+    if present == ctx.stream:
+        return [some.new_empty(shape, dtype=dtype) for shape, dtype in outputs]
+    for t in tensors:
+        if t is not None:
+            t.record_stream(ctx.stream)
+    with torch.cuda.stream(ctx.stream):
+        made = [some.new_empty(shape, dtype=dtype) for shape, dtype in outputs]
+    for t in made:
+        t.record_stream(present)
+    return made
 
 
 def cache_plan(ctx: Context, length: torch.Tensor, added: torch.Tensor, pages: torch.Tensor, ring: torch.Tensor,
@@ -784,10 +794,8 @@ def cache_plan(ctx: Context, length: torch.Tensor, added: torch.Tensor, pages: t
     if ring.dim() != 1 or turn.shape != (2,):
         raise ValueError("ring must have an entry a page, turn two")
     n, width = pages.shape
-    off = length.new_empty(n + 1, dtype=torch.int64)
-    slots = length.new_empty(n_rows, dtype=torch.int32)
-    after, turn_after = torch.empty_like(length), torch.empty_like(turn)
-    _beside(ctx, length, added, pages, ring, turn, off, slots, after, turn_after)
+    off, slots, after, turn_after = _beside(ctx, (length, added, pages, ring, turn), (n + 1, torch.int64),
+                                            (n_rows, torch.int32), (n, torch.int32), (2, torch.int64))
     rc = load().surel_cache_plan(
         ctx.handle, _ptr(length, torch.int32, "length"), _ptr(added, torch.int32, "added"), n, ring.shape[0], page_rows,
         width, n_rows, _ptr(pages, torch.int32, "pages"), _ptr(ring, torch.int32, "ring"),
@@ -824,7 +832,7 @@ def cache_store(ctx: Context, k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
     v_ptr, v_row, v_head = _rows(v, k_pages, "v")
     if k.shape != v.shape or k.shape[1:] != k_pages.shape[2:] or slots.shape != k.shape[:1]:
         raise ValueError("k and v must be [rows][kv_heads][dim] of the pages' heads and dim, slots have an entry a row")
-    _beside(ctx, k, v, slots, k_pages, v_pages)
+    _beside(ctx, (k, v, slots, k_pages, v_pages))
     rc = load().surel_cache_store(ctx.handle, ctypes.byref(cache), k_ptr, v_ptr, k_row, k_head, v_row, v_head,
                                   _ptr(slots, torch.int32, "slots"), k.shape[0])
     if rc != OK:
@@ -851,9 +859,7 @@ def cache_attention(ctx: Context, q: torch.Tensor, k_pages: torch.Tensor, v_page
         q_ptr, q_row, q_head, _ptr(pages, torch.int32, "pages"), _ptr(length, torch.int32, "length"), n, pages.shape[1],
         heads, dim ** -0.5 if scale is None else scale, _ptr(bias, q.dtype, "bias"), _ptr(bucket, torch.int32, "bucket"),
         0 if bias is None else bias.shape[0], 0 if bucket is None else bucket.numel() // 2)
-    out = q.new_empty(q.shape)
-    lse = q.new_empty(q.shape[:2], dtype=torch.float32)
-    _beside(ctx, q, k_pages, v_pages, pages, length, bias, bucket, out, lse)
+    out, lse = _beside(ctx, (q, k_pages, v_pages, pages, length, bias, bucket), (q.shape, q.dtype), (q.shape[:2], torch.float32))
     rc = load().surel_cache_attention(ctx.handle, ctypes.byref(cache), ctypes.byref(args), out.data_ptr(), lse.data_ptr())
     if rc != OK:
         raise SurelError(rc, "surel_cache_attention")
@@ -877,9 +883,7 @@ def sample_classes(ctx: Context, logits: torch.Tensor, u: torch.Tensor, temperat
     n, classes = logits.shape
     if any(t is not None and t.shape != (n,) for t in (u, temperature, top_k, top_p, min_p)):
         raise ValueError("u, temperature, top_k, top_p and min_p must have one entry a row")
-    chosen = u.new_empty(n, dtype=torch.int32)
-    logp = u.new_empty(n)
-    _beside(ctx, logits, u, temperature, top_k, top_p, min_p, chosen, logp)
+    chosen, logp = _beside(ctx, (logits, u, temperature, top_k, top_p, min_p), (n, torch.int32), (n, torch.float32))
     rc = load().surel_sample_classes(
         ctx.handle, kinds[logits.dtype], logits.data_ptr(), logits.stride(0), n, classes, _ptr(u, torch.float32, "u"),
         _ptr(temperature, torch.float32, "temperature"), _ptr(top_k, torch.int32, "top_k"),
