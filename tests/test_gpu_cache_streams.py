@@ -22,39 +22,47 @@ def calls():
     return out
 
 
+def places(tensors):
+    return {b for t in tensors for b in range(t.data_ptr() // 512, (t.data_ptr() + t.nbytes + 511) // 512)}
+
+
 @pytest.mark.parametrize("name", ["plan", "attend", "sample"])
 def test_results_keep_their_memory(name):
     first, second = (x[name] for x in calls())
     big = torch.randn(8192, 8192, device="cuda").bfloat16()
-
-    def keep_busy():
-        for _ in range(60):
-            torch.mm(big, big, out=room)
-
     room = torch.empty_like(big)
     here, side = torch.cuda.current_stream(), torch.cuda.Stream()
     ctx, own = binding.Context(0), binding.Context(0, stream=side)
-    want = [x.clone() for x in first(ctx)]
+    want, want_other = ([x.clone() for x in call(ctx)] for call in (first, second))
     torch.cuda.synchronize()
-    # what torch's present stream has still to write was given back before the call
-    keep_busy()
-    passing = [torch.empty_like(x).fill_(77) for x in want]
+    # what torch's present stream has given back, and may still write, is not what a call's results get
+    passing = [torch.empty_like(x) for x in want]
+    was = places(passing)
     del passing
     got = first(own)
-    side.synchronize()
-    assert not here.query(), "the other stream's work ended too early to say anything"
+    assert not was & places(got)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want, strict=True))
-    # results that torch's present stream has still to read, given back before the next call
-    keep_busy()
-    read = [x.clone() for x in got]
-    del got
-    other = second(own)
-    side.synchronize()
-    assert not here.query(), "the other stream's work ended too early to say anything"
-    torch.cuda.synchronize()
-    assert all(torch.equal(x, y) for x, y in zip(read, want, strict=True))
-    assert all(torch.equal(x, y) for x, y in zip(other, second(ctx), strict=True))
+    for _ in range(2):
+        for _ in range(60):
+            torch.mm(big, big, out=room)
+        passing = [torch.empty_like(x).fill_(77) for x in want]
+        del passing
+        got = first(own)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want, strict=True))
+        # nor are results that it has still to read the next call's
+        for _ in range(60):
+            torch.mm(big, big, out=room)
+        read = [x.clone() for x in got]
+        was = places(got)
+        del got
+        other = second(own)
+        if not here.query():
+            assert not was & places(other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(read, want, strict=True))
+        assert all(torch.equal(x, y) for x, y in zip(other, want_other, strict=True))
     for c in (ctx, own):
         assert c.check() == 0
         c.close()
