@@ -609,7 +609,9 @@ int surel_cache_store(surel_ctx* ctx, const surel_cache* cache, const void* d_k,
  *   d_out, d_lse   as for surel_attention: [n_seqs][heads][dim] of the cache's type, dense, on a 16-byte boundary, and
  *                  float[n_seqs][heads] (device, written).
  * Scores, softmax and sums are 32-bit; what is rounded, what a bias masks, and what rows of no keys get is as for
- * surel_attention.  What lies behind a sequence's last key in its last page has no influence, whatever it holds.
+ * surel_attention.  (Weights are divided by their sum last: before that a product of a weight and a value may be 2^10 times the
+ * value, so that bf16 values of 2^118 over the number of keys and more can give infinities, as they can there.)
+ * What lies behind a sequence's last key in its last page has no influence, whatever it holds.
  * Sequences' keys are shared out evenly over the device by their lengths, which only the device knows, so a
  * captured call serves any lengths that fit max_pages; sums of sequences that several workgroups share are joined in a
  * fixed order.  The context's workspace grows by at most 8 (dim + 4) min(heads / kv_heads, 32) bytes for each of 16
@@ -650,8 +652,9 @@ int surel_cache_attention(surel_ctx* ctx, const surel_cache* cache, const surel_
  *   d_logp         float[n_rows] (device, written): the logarithm of the probability that the class was drawn
  *                  with, log(w_c / the kept classes' sum); minus infinity for -1.
  * Weights and sums are 64-bit (in 32 bits, sums of many classes would be off by more than a class's weight); weights
- * below e^-64 of the largest count as zero.  Results are the same every time.  Where rows are too few to fill the device, the
- * context's workspace grows by up to 64 KB a row, 24 bytes for every workgroup that shares it among them.
+ * below e^-64 of the largest count as zero.  Results are the same every time.  Where rows are too few to fill the device, or take
+ * more than 524,288 times 16 bytes each, the context's workspace grows by up to 73 KB a row and 28 bytes for every workgroup that
+ * shares it.
  * Limits: 0 <= n_rows <= SUREL_MAX_ROWS, 1 <= n_classes <= SUREL_MAX_NODES, row up to 2^40.  Asynchronous.
  * Device-detected: BAD_CHOICE. */
 int surel_sample_classes(surel_ctx* ctx, int32_t type, const void* d_logits, int64_t row, int64_t n_rows,

@@ -46,9 +46,10 @@ constexpr int waves_of_a_simd(int padded, int blocks) {
 // operand of out^T += V^T p^T as they come.  Keys go from memory to registers, as the first product's operand lies; values, which
 // the second needs transposed, through LDS, without passing through registers.
 // What bounds it: memory, and for caches of a gigabyte and less the starts and ends of parts.  256 caches of 1 to 8,192 keys, 16
-// heads to 2 of 128 elements, with a bias: 215 us, 4.8 TB/s; 1,024 of them 811 with the join, 5.4 TB/s.  (With 32-column
+// heads to 2 of 128 elements, with a bias: 229 us, 4.5 TB/s; 1,024 of them 788 with the join, 5.4 TB/s.  (With 32-column
 // products and keys through LDS as well, 302: four times the softmax for 8 heads, and half the waves.)  Weights are rounded to
-// 16 bits for their product, as surel_attention's are; sums and statistics are 32-bit.
+// 16 bits for their product, as surel_attention's are (results of that call: 0.0020 of their size off, where their own rounding alone
+// is 0.0017); sums and statistics are 32-bit.
 template <class T, int DP, int BLOCKS>
 __global__ __launch_bounds__(kThreads, waves_of_a_simd(DP, BLOCKS)) void cache_attention_kernel(CacheAttention a, Share o, int in_table) {
     constexpr int NB = DP / 16, NK = DP / 32, kRowBytes = Tile<DP>::kRowBytes, kTileBytes = kCacheTile * kRowBytes;

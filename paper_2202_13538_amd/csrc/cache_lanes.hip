@@ -5,8 +5,8 @@
 // time, as they come from memory: products of pairs of elements, sums over the LPK lanes of a key, and every group
 // of lanes keeps the softmax and the sum over its own keys.  Groups are joined at a pair's end: halves of what two lanes hold
 // are exchanged, so that each then adds half as much.
-// What bounds it: memory.  16,384 caches of 1 to 64 keys, 8 heads of 64 elements, with a bias: 240 us, 4.7 TB/s read and
-// written (by 32-column products 1,221, by 16-column ones 317); 512 of 100 to 8,192, 4 heads of 128: 738, 5.9 TB/s.  With three and
+// What bounds it: memory.  16,384 caches of 1 to 64 keys, 8 heads of 64 elements, with a bias: 243 us, 4.7 TB/s read and
+// written (by 32-column products 1,221, by 16-column ones 317); 512 of 100 to 8,192, 4 heads of 128: 741, 5.9 TB/s.  With three and
 // four heads a key head the products are faster (12 heads to 4 of 104 elements 147 us here, 132 there; two of 128: 140, 150).
 #include "cache_attention.h"
 #include "kernels.h"
